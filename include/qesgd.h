@@ -12,6 +12,10 @@
  *                 qesgd_decode                 decode one stream to fp32
  *   local epoch   qesgd_lr_sgd_step / qesgd_lr_local_epoch[_batch]
  *                                              logistic-regression minibatch SGD
+ *   matrices      qesgd_fp4_quantize, qesgd_fp4_dequantize, qesgd_fp4_matmul
+ *                                              products of a worker's local step on microscaled
+ *                                              4-bit operands (forward and both gradients)
+ *                 qesgd_orthogonalize          an averaged update made orthogonal before it is applied
  *
  * Conventions
  *   - Every data pointer is a DEVICE pointer owned by the caller and valid on
@@ -60,7 +64,17 @@ extern "C" {
 #define QESGD_SCALE_MAX 1u   /* scale = largest magnitude of the bucket's delta    */
 #define QESGD_SCALE_FIXED 2u /* scale = s*delta with the grid spacing delta given  */
 
-#define QESGD_STATUS_NONFINITE 1u /* a bucket held NaN/Inf or its norm overflowed fp32 */
+/* Element types of the matrix operators. */
+#define QESGD_F32 0u
+#define QESGD_BF16 1u
+#define QESGD_F16 2u
+#define QESGD_FP4_MX 0u /* blocks of 32; scale byte c stands for 2^(c - 127) (E8M0)          */
+#define QESGD_FP4_NV 1u /* blocks of 16; scale byte is an E4M3 number, times the tensor's 2^t */
+#define QESGD_ROUND_NEAREST 0u    /* ties to the even code */
+#define QESGD_ROUND_STOCHASTIC 1u /* unbiased, by the draws of qesgd_encode */
+
+#define QESGD_STATUS_NONFINITE 1u /* a bucket held NaN/Inf or its norm overflowed fp32; a block of 4-bit
+                                     numbers or a matrix to be made orthogonal held NaN/Inf */
 #define QESGD_STATUS_TIMEOUT 2u   /* a bounded wait inside the local-epoch kernel ran out   */
 #define QESGD_STATUS_RANGE 4u     /* debug build only: a codec kernel computed an index outside
                                      its buffer; the access was skipped                       */
@@ -70,6 +84,10 @@ extern "C" {
 #define QESGD_MAX_BUCKET 8192u
 #define QESGD_MAX_LR_BATCH 1024u
 #define QESGD_NOALLOC_MAX_LR_BATCH 256u /* rows per step of qesgd_lr_sgd_step_noalloc */
+#define QESGD_MAX_MATRIX_SIDE 0x7FFFFF00u   /* rows, columns of the 4-bit operators */
+#define QESGD_MAX_ORTHO_SIDE 65536u         /* rows, columns of qesgd_orthogonalize */
+#define QESGD_MAX_ORTHO_BATCH 4096u
+#define QESGD_MAX_ORTHO_STEPS 32u
 
 typedef struct qesgd_ctx qesgd_ctx;
 
@@ -310,6 +328,96 @@ int qesgd_debug_lr_plan(const qesgd_ctx *ctx, uint32_t plan[8]);
  */
 int qesgd_lr_sgd_step_noalloc(void *cuda_stream, const float *Xb, const float *yb, uint32_t m,
                               uint64_t d, float lr, float *u);
+
+/*
+ * Microscaled 4-bit floating point.  The paper sends its updates on a uniform grid; these are
+ * the operands of a worker's local step where the parameter is a matrix: weights, activations
+ * and gradients as 4-bit floats (E2M1: +-{0, .5, 1, 1.5, 2, 3, 4, 6}) with a scale for each
+ * block of consecutive elements of a row, the axis that a product contracts over.
+ *
+ * Layout of a matrix of `rows` x `cols` elements
+ *   codes   rows of qesgd_fp4_row_bytes(cols) = 16 * ceil(cols / 32) bytes; element c of a row is
+ *           the low (c even) or high (c odd) half of byte c / 2: top bit the sign, low three
+ *           bits the index into the grid.  Padding codes are 0, and so is the sign of a zero.
+ *   scales  qesgd_fp4_scale_bytes(rows, cols, format) bytes in tiles of 512: tile
+ *           (row / 128) * ceil(blocks / 4) + block / 4 holds 128 rows by 4 blocks, byte
+ *           (row % 32) * 16 + (row / 32 % 4) * 4 + block % 4 of it.  Padding bytes are 0.
+ *   t       an exponent of the whole tensor (format NV alone): one int32 on the device, read when
+ *           the kernel runs, clamped to [-126, 126]; NULL = 0.
+ * Codes and scales are 16-byte aligned.  rows and cols are at most QESGD_MAX_MATRIX_SIDE; a
+ * matrix without elements is a valid no-op.
+ */
+uint64_t qesgd_fp4_row_bytes(uint64_t cols);
+uint64_t qesgd_fp4_scale_bytes(uint64_t rows, uint64_t cols, uint32_t format);
+
+/* The exponent t for qesgd_fp4_quantize, from the tensor itself: the smallest t in [-126, 126] with
+ * max |x| <= 6 * 448 * 2^t (non-finite elements left out, QESGD_STATUS_NONFINITE set; -126 for a
+ * tensor of zeros).  x: rows of ldx elements of type dtype, cols of them used.  One memset and
+ * one kernel; nothing is written for an empty matrix. */
+int qesgd_fp4_tensor_exponent(qesgd_ctx *ctx, const void *x, uint32_t dtype, uint64_t rows, uint64_t cols,
+                              uint64_t ldx, int32_t *exponent_out);
+
+/*
+ * Quantises the rows x cols matrix x (row r at x + r * ldx elements, of type dtype).
+ * codes_out / scales_out receive the matrix with blocks along its rows, codes_t_out / scales_t_out
+ * its transpose (cols x rows) with blocks along that one's rows, as the products of a backward
+ * pass want it; either pair may be NULL (both of a pair or neither, one pair at least), and x is
+ * read once for both.  For a block of a row with largest magnitude m:
+ *   MX  scale 2^e, e the smallest integer in [-127, 126] with m <= 6 * 2^e;  q = |x| * 2^-e
+ *   NV  scale s, the smallest E4M3 number with m * 2^-t <= 6 s (at most 448);
+ *       q = fl32(|x| * 2^-t / s), at most 6
+ * NEAREST: the grid point next to q, a tie to the even code.  STOCHASTIC: with l <= q < h
+ * neighbours on the grid, h if u < (q - l) / (h - l), else l: unbiased, since no scale clips (NV: none
+ * unless m > 2688 * 2^t); u = (h_i + 1/2) / 2^16 with the draw h_i of qesgd_encode for element
+ * i = r * (32 * ceil(C / 32)) + c of the R x C matrix that is written (r, c its row and column).
+ * seed, worker and epoch are read for STOCHASTIC alone.  A block with a non-finite element is
+ * written as scale byte 0, codes 0, and QESGD_STATUS_NONFINITE is set.  All padding is written.
+ * tensor_exponent must be NULL for MX. */
+int qesgd_fp4_quantize(qesgd_ctx *ctx, const void *x, uint32_t dtype, uint64_t rows, uint64_t cols,
+                       uint64_t ldx, uint32_t format, const int32_t *tensor_exponent, uint32_t rounding,
+                       uint64_t seed, uint32_t worker, uint32_t epoch, uint8_t *codes_out,
+                       uint8_t *scales_out, uint8_t *codes_t_out, uint8_t *scales_t_out);
+
+/* The values that codes and scales stand for: out (rows of ldo elements of type dtype) =
+ * +-grid * scale * 2^t, exact in 32 bits and in BF16 (within their range), rounded once to F16. */
+int qesgd_fp4_dequantize(qesgd_ctx *ctx, const uint8_t *codes, const uint8_t *scales, uint64_t rows,
+                         uint64_t cols, uint32_t format, const int32_t *tensor_exponent, void *out,
+                         uint32_t dtype, uint64_t ldo);
+
+/* C = A B^T, or C + A B^T where accumulate is not 0: A is M x K, B is N x K, both of one format,
+ * C is M rows of ldc elements of type dtype.  A linear layer with weight W (out x in): Y = X W^T;
+ * dX = dY W as dY by the transpose of W; dW = dY^T X as the transposes of both.  Accumulation in
+ * fp32, multiplied by 2^(ta + tb), C added in fp32, rounded once to dtype.  K = 0 gives zeros (or
+ * leaves C as it is); C must not overlap an operand. */
+int qesgd_fp4_matmul(qesgd_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_scales,
+                     const int32_t *a_exponent, const uint8_t *b_codes, const uint8_t *b_scales,
+                     const int32_t *b_exponent, uint64_t M, uint64_t N, uint64_t K, uint32_t format,
+                     void *c, uint32_t dtype, uint64_t ldc, uint32_t accumulate);
+
+/*
+ * The update of a matrix made (nearly) orthogonal by Newton-Schulz products, for a server that
+ * applies O instead of the averaged delta G: with X = G / ||G||_F, `steps` times
+ *   A = X X^T,  X <- a X + (b A + c A A) X        (on the side with fewer rows)
+ * which takes every singular value s of X to p(s) = a s + b s^3 + c s^5, step by step.  The usual
+ * a, b, c = 3.4445, -4.7750, 2.0315 and five steps bring singular values between 0.01 and 1 of
+ * the largest into about [0.7, 1.2].
+ * x: `batch` matrices of rows x cols (row stride ldx, matrix stride x_stride, in elements of type
+ * dtype); out: the same in BF16 (ldo, out_stride), which may be x itself where the layouts agree.
+ * The products take fp16 operands (scaled by powers of two) and accumulate in fp32; the term a X of
+ * the first three steps carries 22 bits.  Five usual steps end 2e-3 of the result from the exact
+ * one, of which 1.7e-3 is the final rounding to BF16.  a, b, c finite, |a| <= 16, |b|, |c| <= 32; should they let
+ * singular values grow beyond 100 the result saturates.  A matrix of zeros gives zeros; one with a
+ * non-finite element gives zeros and QESGD_STATUS_NONFINITE, the others of the batch are not
+ * touched by it.
+ * workspace: qesgd_orthogonalize_workspace(rows, cols, batch) bytes of device memory, 256-byte
+ * aligned, of the caller; it holds nothing between calls, and calls that may overlap on the GPU
+ * (other streams, two captured graphs) need one each.  qesgd_orthogonalize_workspace returns 0
+ * for sizes that are not taken. */
+uint64_t qesgd_orthogonalize_workspace(uint64_t rows, uint64_t cols, uint64_t batch);
+int qesgd_orthogonalize(qesgd_ctx *ctx, const void *x, uint32_t dtype, uint64_t rows, uint64_t cols, uint64_t ldx,
+                        uint64_t batch, uint64_t x_stride, uint32_t steps, float a, float b, float c,
+                        void *out, uint64_t ldo, uint64_t out_stride, void *workspace,
+                        uint64_t workspace_bytes);
 
 /* Waits for the stream, copies the status word to *flags_out (host) and clears it. */
 int qesgd_status(qesgd_ctx *ctx, uint32_t *flags_out);

@@ -1,7 +1,7 @@
 """Compile the CUDA library in-tree: paper_1901_03040_b200/libqesgd.so (sm_100a).
 
-The codec translation unit is built with -fmad=false so that no multiply-add of
-the rounding chain is contracted; the logistic-regression unit keeps FMAs.
+The codec and the 4-bit quantiser are built with -fmad=false so that no multiply-add of
+the rounding chain is contracted; the other units keep FMAs.
 """
 import os
 import subprocess
@@ -28,6 +28,10 @@ UNITS = [
     ("qesgd_lr_epoch.cu", "qesgd_lr_epoch.o", []),
     ("qesgd_lr_tile.cu", "qesgd_lr_tile.o", []),
     ("qesgd_api.cu", "qesgd_api.o", []),
+    ("qesgd_fp4.cu", "qesgd_fp4.o", ["-fmad=false"]),
+    ("qesgd_fp4_matmul.cu", "qesgd_fp4_matmul.o", []),
+    ("qesgd_orthogonalize.cu", "qesgd_orthogonalize.o", []),
+    ("qesgd_matrix.cu", "qesgd_matrix.o", []),
 ]
 
 
@@ -61,7 +65,8 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     os.makedirs(OBJ, exist_ok=True)
     build_py_module(force)
     headers = [os.path.join(CSRC, "qesgd_internal.h"), os.path.join(CSRC, "qesgd_lr_device.cuh"),
-               os.path.join(CSRC, "qesgd_lr_tile.h"), os.path.join(ROOT, "include", "qesgd.h"),
+               os.path.join(CSRC, "qesgd_lr_tile.h"),
+               os.path.join(CSRC, "qesgd_orthogonalize.h"), os.path.join(ROOT, "include", "qesgd.h"),
                os.path.abspath(__file__)]
     nvcc = _nvcc()
     objs = []

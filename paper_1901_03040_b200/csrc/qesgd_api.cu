@@ -6,7 +6,8 @@
 
 namespace {
 
-inline bool aligned(const void *p, uintptr_t a) { return ((uintptr_t)p % a) == 0; }
+inline bool aligned(const void *p, uintptr_t a) { return qesgd_aligned(p, a); }
+inline int cuda_fail(qesgd_ctx *ctx, int err) { return qesgd_cuda_fail(ctx, err); }
 
 inline int log2_exact(uint32_t v)
 {
@@ -25,28 +26,6 @@ inline bool valid_codec(uint32_t bucket, uint32_t s, uint32_t bits)
     if (!(bits == 2 || bits == 4 || bits == 8)) return false;
     if (!valid_bucket(bucket)) return false;
     return s >= 1u && s <= (1u << (bits - 1)) - 1u;
-}
-
-// Binds the context's device for the duration of a call and restores the caller's.
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = false;
-    explicit DeviceGuard(int device)
-    {
-        if (cudaGetDevice(&prev) != cudaSuccess) return;
-        ok = (prev == device) || cudaSetDevice(device) == cudaSuccess;
-        if (prev == device) prev = -1;
-    }
-    ~DeviceGuard()
-    {
-        if (ok && prev >= 0) cudaSetDevice(prev);
-    }
-};
-
-int cuda_fail(qesgd_ctx *ctx, int err)
-{
-    ctx->last_cuda_error = err;
-    return QESGD_ECUDA;
 }
 
 }  // namespace

@@ -1,0 +1,501 @@
+// Microscaled 4-bit floats: a matrix quantised with blocks along its rows, along its columns (the transpose), or
+// both in one read; the way back; and the exponent of a whole tensor.  Definitions are stated in include/qesgd.h.
+//
+// This file must be compiled with -fmad=false: the choice of a level is a sequence of single IEEE operations.
+//
+// All of it is bound by memory.  The unit of work is an octet, 8 consecutive elements of a row in one lane: 16 or 32
+// bytes of input, one Philox4x32-10 block of 8 draws, one 32-bit word of codes.  A block of 16 is two lanes, one of 32
+// four, so its largest magnitude takes one or two shuffles.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "qesgd_internal.h"
+
+namespace {
+
+constexpr uint32_t FULL = 0xFFFFFFFFu;
+constexpr int THREADS = 256;
+constexpr int TILE_ROWS = 128;       // rows of a tile of scales
+constexpr int SCALE_TILE = 512;      // bytes of it: 128 rows by 4 blocks
+
+template <int FORMAT>
+struct Format;
+template <>
+struct Format<QESGD_FP4_MX> {
+    static constexpr int BLOCK = 32;
+};
+template <>
+struct Format<QESGD_FP4_NV> {
+    static constexpr int BLOCK = 16;
+};
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+
+// Eight elements from column c on; zeros past the last column.
+template <typename T>
+__device__ __forceinline__ void load_octet(const T *row, uint64_t c, uint64_t cols, bool vec, float (&v)[8])
+{
+    if (vec && c + 8 <= cols) {
+        if (sizeof(T) == 4) {
+            const float4 a = __ldg(reinterpret_cast<const float4 *>(row + c)), b = __ldg(reinterpret_cast<const float4 *>(row + c) + 1);
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        } else {
+            const uint4 a = __ldg(reinterpret_cast<const uint4 *>(row + c));
+            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint16_t h = (uint16_t)(w[j / 2] >> (16 * (j % 2)));
+                v[j] = to_float(*reinterpret_cast<const T *>(&h));
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? to_float(row[c + j]) : 0.0f;
+    }
+}
+
+// The eight 16-bit draws of octet `n` (Philox4x32 with 10 rounds, round keys prepared on the host), as in the encode
+// kernel: draw j is half j % 2 of word j / 2.
+__device__ __forceinline__ void draws_of(uint64_t n, const Fp4QuantizeArgs &a, uint32_t (&x)[4])
+{
+    x[0] = (uint32_t)n;
+    x[1] = (uint32_t)(n >> 32);
+    x[2] = a.worker;
+    x[3] = a.epoch;
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t p0 = (uint64_t)0xD2511F53u * x[0];
+        const uint64_t p1 = (uint64_t)0xCD9E8D57u * x[2];
+        const uint32_t n0 = (uint32_t)(p1 >> 32) ^ x[1] ^ a.round_key[r][0];
+        const uint32_t n2 = (uint32_t)(p0 >> 32) ^ x[3] ^ a.round_key[r][1];
+        x[1] = (uint32_t)p1;
+        x[3] = (uint32_t)p0;
+        x[0] = n0;
+        x[2] = n2;
+    }
+}
+
+__device__ __forceinline__ int clamp_exponent(int t) { return min(max(t, -126), 126); }
+__device__ __forceinline__ int tensor_exponent(const int32_t *p) { return p ? clamp_exponent(__ldg(p)) : 0; }
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
+
+// A block's scale, from the bits of its largest magnitude: the byte that is kept, and what its elements are multiplied by
+// (and, NV, divided by).
+struct Scale {
+    uint32_t byte;
+    float mul;    // 2^-e (MX), 2^-t (NV); 0 where the block holds nothing but zeros or something not finite
+    float div;    // s (NV)
+    float inv;    // fl32(1 / s) (NV)
+};
+template <int FORMAT>
+__device__ __forceinline__ Scale block_scale(uint32_t top, float to_tensor)
+{
+    Scale s;
+    const bool none = top == 0u || top >= 0x7F800000u;
+    if (FORMAT == QESGD_FP4_MX) {
+        // top = 1.f * 2^(E - 127) is at most 6 * 2^e = 1.5 * 2^(e + 2) from e = E - 129 on, one later where 1.f > 1.5
+        const int byte = (int)(top >> 23) - 2 + ((top & 0x7FFFFFu) > 0x400000u ? 1 : 0);
+        s.byte = none ? 0u : (uint32_t)max(byte, 0);
+        s.mul = none ? 0.0f : __uint_as_float((254u - s.byte) << 23);
+        s.div = s.inv = 1.0f;
+    } else {
+        // The bits of an E4M3 number are bits 20..26 of the float 2^-120 times it, subnormals included.  A first guess from
+        // a rounded product, right to within one number; then the smallest s with v <= 6 s, 6 s being exact.
+        const float v = __fmul_rn(__uint_as_float(none ? 0u : top), to_tensor);
+        const float g = __fmul_rn(__fmul_rn(fminf(v, 2688.0f), 0.16666667f), 0x1p-120f);
+        uint32_t code = min((__float_as_uint(g) + 0xFFFFFu) >> 20, 126u);
+        const float up = __fmul_rn(__uint_as_float(code << 20), 0x1p120f);
+        if (__fmul_rn(6.0f, up) < v) code = min(code + 1u, 126u);
+        else if (code > 0u && __fmul_rn(6.0f, __fmul_rn(__uint_as_float((code - 1u) << 20), 0x1p120f)) >= v) code -= 1u;
+        code = none ? 0u : max(code, 1u);
+        s.byte = code;
+        s.div = __fmul_rn(__uint_as_float(max(code, 1u) << 20), 0x1p120f);
+        s.inv = __frcp_rn(s.div);
+        s.mul = none ? 0.0f : to_tensor;
+    }
+    return s;
+}
+// x over the block's scale, correctly rounded.  NV: the quotient by the rounded reciprocal, corrected by its residual; s has
+// 4 significant bits, so a quotient lies on a rounding border or at least 2^-5 units in the last place from it, far
+// more than the correction is off.
+template <int FORMAT>
+__device__ __forceinline__ float over_scale(float x, const Scale &s)
+{
+    const float y = __fmul_rn(x, s.mul);
+    if (FORMAT == QESGD_FP4_MX) return y;
+    const float q = __fmul_rn(y, s.inv);
+    const float r = __fmaf_rn(__fmaf_rn(-q, s.div, y), s.inv, q);
+    return fabsf(q) < 3.402823466e38f ? r : q;   // beyond the float range: clipped to 6 either way
+}
+
+// Eight elements of one block -> their codes.
+template <int FORMAT, bool STOCHASTIC>
+__device__ __forceinline__ uint32_t quantize_octet(const float (&v)[8], const Scale &s, const uint32_t (&draw)[4])
+{
+    uint32_t w = 0u;
+    if (s.mul == 0.0f) return 0u;
+    if (!STOCHASTIC) {
+        float q[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[j] = over_scale<FORMAT>(v[j], s);
+        asm("{\n"
+            ".reg .b8 b0, b1, b2, b3;\n"
+            "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n"
+            "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n"
+            "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n"
+            "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n"
+            "mov.b32 %0, {b0, b1, b2, b3};\n"
+            "}\n"
+            : "=r"(w)
+            : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]), "f"(q[4]), "f"(q[5]), "f"(q[6]), "f"(q[7]));
+        // a zero has no sign: the top bit of a half stays where its level is 1 at least
+        return w & (0x77777777u | ((w & 0x77777777u) + 0x77777777u));
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        // the grid is linear between 0 and 2 (steps of 1/2), 2 and 4 (1), 4 and 6 (2): h counts steps, exactly
+        const float q = fminf(fabsf(over_scale<FORMAT>(v[j], s)), 6.0f);
+        const float h = __fmul_rn(q, q < 2.0f ? 2.0f : q < 4.0f ? 1.0f : 0.5f);
+        const float below = floorf(h);
+        const uint32_t u = (draw[j / 2] >> (16 * (j % 2))) & 0xFFFFu;
+        // u's value (u + 1/2) / 2^16 against the rest h - below, both times 2^17 and then exact
+        const uint32_t up = (float)(2u * u + 1u) < __fmul_rn(h - below, 131072.0f) ? 1u : 0u;
+        const uint32_t level = (uint32_t)below + (q < 2.0f ? 0u : q < 4.0f ? 2u : 4u) + up;
+        w |= (level | (v[j] < 0.0f && level ? 8u : 0u)) << (4 * j);
+    }
+    return w;
+}
+
+// Byte of (row, block) within the tiles that a CTA keeps in shared memory, one after another along the blocks.
+__device__ __forceinline__ uint32_t scale_slot(uint32_t row, uint32_t block)
+{
+    return block / 4u * SCALE_TILE + (row % 32u) * 16u + (row / 32u) * 4u + block % 4u;
+}
+
+template <int FORMAT>
+__device__ __forceinline__ uint32_t block_top(const float (&v)[8])
+{
+    uint32_t top = 0u;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7FFFFFFFu);
+    top = max(top, __shfl_xor_sync(FULL, top, 1));
+    if (FORMAT == QESGD_FP4_MX) top = max(top, __shfl_xor_sync(FULL, top, 2));
+    return top;
+}
+
+// ------------------------------------------------------- blocks along rows ----
+constexpr int ROW_COLS = 256;   // columns of a CTA's tile: a warp takes one row at a time
+
+template <typename T, int FORMAT, bool STOCHASTIC>
+__global__ __launch_bounds__(THREADS) void qesgd_fp4_quantize_rows_kernel(const __grid_constant__ Fp4QuantizeArgs a)
+{
+    constexpr int BLOCK = Format<FORMAT>::BLOCK;
+    constexpr int BLOCKS = ROW_COLS / BLOCK;
+    constexpr int UNROLL = 4;
+    __shared__ __align__(16) uint8_t scales[TILE_ROWS * BLOCKS];
+    qesgd_wait_for_previous();
+    const uint32_t lane = threadIdx.x % 32u, warp = threadIdx.x / 32u;
+    const uint64_t col_tiles = (a.cols + ROW_COLS - 1) / ROW_COLS;
+    const uint64_t tiles = col_tiles * ((a.rows + TILE_ROWS - 1) / TILE_ROWS);
+    const uint64_t padded = (a.cols + 31) / 32 * 32;
+    const uint64_t scale_tiles = (a.cols + 4 * BLOCK - 1) / (4 * BLOCK);
+    const float to_tensor = power_of_two(-tensor_exponent(a.tensor_exponent));
+    bool bad = false;
+    for (uint64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const uint64_t row0 = tile / col_tiles * TILE_ROWS, col0 = tile % col_tiles * ROW_COLS;
+        const uint32_t rows = (uint32_t)min((uint64_t)TILE_ROWS, a.rows - row0);
+        if (rows < TILE_ROWS) {
+            for (uint32_t i = threadIdx.x; i < sizeof(scales) / 4; i += THREADS) reinterpret_cast<uint32_t *>(scales)[i] = 0u;
+            __syncthreads();
+        }
+        const uint64_t c = col0 + lane * 8u;
+        for (uint32_t r0 = warp; r0 < rows; r0 += THREADS / 32 * UNROLL) {
+            float v[UNROLL][8];
+#pragma unroll
+            for (int i = 0; i < UNROLL; ++i) {
+                const uint32_t r = r0 + i * (THREADS / 32);
+                if (r < rows) load_octet(static_cast<const T *>(a.x) + (row0 + r) * a.ldx, c, a.cols, a.vec, v[i]);
+                else
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < UNROLL; ++i) {
+                const uint32_t r = r0 + i * (THREADS / 32);
+                if (r >= rows) break;
+                const uint32_t top = block_top<FORMAT>(v[i]);
+                bad |= top >= 0x7F800000u;
+                const Scale s = block_scale<FORMAT>(top, to_tensor);
+                uint32_t draw[4] = {0u, 0u, 0u, 0u};
+                if (STOCHASTIC) draws_of(((row0 + r) * padded + c) / 8, a, draw);
+                const uint32_t w = quantize_octet<FORMAT, STOCHASTIC>(v[i], s, draw);
+                if (c < padded) *reinterpret_cast<uint32_t *>(a.codes + ((row0 + r) * padded + c) / 2) = w;
+                if (lane % (BLOCK / 8) == 0) scales[scale_slot(r, lane / (BLOCK / 8))] = (uint8_t)s.byte;
+            }
+        }
+        __syncthreads();
+        const uint64_t first = col0 / (4 * BLOCK);
+        const uint32_t have = (uint32_t)min((uint64_t)(BLOCKS / 4), scale_tiles - first);
+        uint4 *out = reinterpret_cast<uint4 *>(a.scales + (row0 / TILE_ROWS * scale_tiles + first) * SCALE_TILE);
+        for (uint32_t i = threadIdx.x; i < have * (SCALE_TILE / 16); i += THREADS) out[i] = reinterpret_cast<const uint4 *>(scales)[i];
+        __syncthreads();
+    }
+    if (bad) atomicOr(a.status, QESGD_STATUS_NONFINITE);
+}
+
+// ------------------------------- blocks along columns, or along both axes ----
+constexpr int SIDE = 128;   // a CTA's tile: whole tiles of scales for either axis
+
+template <typename T, int FORMAT, bool STOCHASTIC>
+__global__ __launch_bounds__(THREADS) void qesgd_fp4_quantize_columns_kernel(const __grid_constant__ Fp4QuantizeArgs a)
+{
+    constexpr int BLOCK = Format<FORMAT>::BLOCK;
+    constexpr int BLOCKS = SIDE / BLOCK;
+    constexpr int PITCH = SIDE + 4 / (int)sizeof(T);   // elements between rows in shared memory
+    extern __shared__ __align__(16) uint8_t smem[];
+    T *const held = reinterpret_cast<T *>(smem);
+    __shared__ __align__(16) uint8_t scales[2][SIDE * BLOCKS];
+    qesgd_wait_for_previous();
+    const uint64_t col_tiles = (a.cols + SIDE - 1) / SIDE;
+    const uint64_t tiles = col_tiles * ((a.rows + SIDE - 1) / SIDE);
+    const uint64_t padded = (a.cols + 31) / 32 * 32, padded_t = (a.rows + 31) / 32 * 32;
+    const uint64_t scale_tiles = (a.cols + 4 * BLOCK - 1) / (4 * BLOCK), scale_tiles_t = (a.rows + 4 * BLOCK - 1) / (4 * BLOCK);
+    const float to_tensor = power_of_two(-tensor_exponent(a.tensor_exponent));
+    bool bad = false;
+    for (uint64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const uint64_t row0 = tile / col_tiles * SIDE, col0 = tile % col_tiles * SIDE;
+        // every row and column of the tile goes the whole way, as zeros past the matrix's edge: then padding bytes are zeros
+        for (uint32_t i = threadIdx.x / 16u; i < SIDE; i += THREADS / 16) {
+            const uint32_t o = threadIdx.x % 16u;
+            const uint64_t r = row0 + i, c = col0 + o * 8u;
+            float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+            if (r < a.rows) load_octet(static_cast<const T *>(a.x) + r * a.ldx, c, a.cols, a.vec, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) held[i * PITCH + o * 8u + j] = (T)v[j];
+            if (a.codes) {
+                const uint32_t top = block_top<FORMAT>(v);
+                bad |= top >= 0x7F800000u;
+                const Scale s = block_scale<FORMAT>(top, to_tensor);
+                uint32_t draw[4] = {0u, 0u, 0u, 0u};
+                if (STOCHASTIC) draws_of((r * padded + c) / 8, a, draw);
+                const uint32_t w = quantize_octet<FORMAT, STOCHASTIC>(v, s, draw);
+                if (r < a.rows && c < padded) *reinterpret_cast<uint32_t *>(a.codes + (r * padded + c) / 2) = w;
+                if (o % (BLOCK / 8) == 0) scales[0][scale_slot(i, o / (BLOCK / 8))] = (uint8_t)s.byte;
+            }
+        }
+        __syncthreads();
+        {
+            // a thread takes half a column: 64 elements, 32 bytes of codes
+            const uint32_t k = threadIdx.x % SIDE, half = threadIdx.x / SIDE;
+            const uint64_t c = col0 + k;
+#pragma unroll 1
+            for (uint32_t b = 0; b < 64 / 32; ++b) {
+                const uint32_t i0 = half * 64u + b * 32u;
+                uint32_t words[4];
+#pragma unroll
+                for (int g = 0; g < 32 / BLOCK; ++g) {
+                    float v[BLOCK / 8][8];
+                    uint32_t top = 0u;
+#pragma unroll
+                    for (int o = 0; o < BLOCK / 8; ++o)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            v[o][j] = to_float(held[(i0 + g * BLOCK + o * 8 + j) * PITCH + k]);
+                            top = max(top, __float_as_uint(v[o][j]) & 0x7FFFFFFFu);
+                        }
+                    bad |= top >= 0x7F800000u;
+                    const Scale s = block_scale<FORMAT>(top, to_tensor);
+#pragma unroll
+                    for (int o = 0; o < BLOCK / 8; ++o) {
+                        uint32_t draw[4] = {0u, 0u, 0u, 0u};
+                        if (STOCHASTIC) draws_of((c * padded_t + row0 + i0 + g * BLOCK + o * 8) / 8, a, draw);
+                        words[g * (BLOCK / 8) + o] = quantize_octet<FORMAT, STOCHASTIC>(v[o], s, draw);
+                    }
+                    scales[1][scale_slot(k, (i0 + g * BLOCK) / BLOCK)] = (uint8_t)s.byte;
+                }
+                if (c < a.cols && row0 + i0 < padded_t)
+                    *reinterpret_cast<uint4 *>(a.codes_t + (c * padded_t + row0 + i0) / 2) = make_uint4(words[0], words[1], words[2], words[3]);
+            }
+        }
+        __syncthreads();
+        for (int side = a.codes ? 0 : 1; side < 2; ++side) {
+            const uint64_t all = side ? scale_tiles_t : scale_tiles;
+            const uint64_t first = (side ? row0 : col0) / (4 * BLOCK), at = (side ? col0 : row0) / TILE_ROWS;
+            const uint32_t have = (uint32_t)min((uint64_t)(BLOCKS / 4), all - first);
+            uint4 *out = reinterpret_cast<uint4 *>((side ? a.scales_t : a.scales) + (at * all + first) * SCALE_TILE);
+            for (uint32_t i = threadIdx.x; i < have * (SCALE_TILE / 16); i += THREADS) out[i] = reinterpret_cast<const uint4 *>(scales[side])[i];
+        }
+        __syncthreads();
+    }
+    if (bad) atomicOr(a.status, QESGD_STATUS_NONFINITE);
+}
+
+// --------------------------------------------------------------- way back ----
+template <typename T>
+__device__ __forceinline__ T from_float(float v);
+template <>
+__device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <>
+__device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+
+// grid values of the two codes of a byte
+__device__ __forceinline__ float2 values_of(uint32_t byte)
+{
+    uint32_t h;
+    asm("{\n"
+        ".reg .b8 b;\n"
+        ".reg .b16 w;\n"
+        "cvt.u16.u32 w, %1;\n"
+        "cvt.u8.u16 b, w;\n"
+        "cvt.rn.f16x2.e2m1x2 %0, b;\n"
+        "}\n" : "=r"(h) : "r"(byte));
+    return __half22float2(*reinterpret_cast<const __half2 *>(&h));
+}
+template <int FORMAT>
+__device__ __forceinline__ float scale_value(uint32_t byte)
+{
+    // 2^(byte - 127), 2^-127 being a subnormal float; or the E4M3 number of these bits
+    if (FORMAT == QESGD_FP4_MX) return byte ? __uint_as_float(byte << 23) : __uint_as_float(0x00400000u);
+    return __fmul_rn(__uint_as_float((byte & 0x7Fu) << 20), 0x1p120f);
+}
+
+template <typename T, int FORMAT>
+__global__ __launch_bounds__(THREADS) void qesgd_fp4_dequantize_kernel(const __grid_constant__ Fp4DequantizeArgs a)
+{
+    constexpr int BLOCK = Format<FORMAT>::BLOCK;
+    qesgd_wait_for_previous();
+    const uint64_t padded = (a.cols + 31) / 32 * 32;
+    const uint64_t scale_tiles = (a.cols + 4 * BLOCK - 1) / (4 * BLOCK);
+    const uint64_t octets = (a.cols + 7) / 8, all = octets * a.rows;
+    const float tensor = power_of_two(tensor_exponent(a.tensor_exponent));
+    for (uint64_t n = (uint64_t)blockIdx.x * THREADS + threadIdx.x; n < all; n += (uint64_t)gridDim.x * THREADS) {
+        const uint64_t r = n / octets, c = n % octets * 8;
+        const uint64_t block = c / BLOCK;
+        const uint32_t byte = a.scales[(r / 128 * scale_tiles + block / 4) * SCALE_TILE + r % 32 * 16 + r / 32 % 4 * 4 + block % 4];
+        const float scale = scale_value<FORMAT>(byte);
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(a.codes + (r * padded + c) / 2);
+        T v[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 p = values_of((w >> (8 * j)) & 0xFFu);
+            v[2 * j] = from_float<T>(__fmul_rn(__fmul_rn(p.x, scale), tensor));
+            v[2 * j + 1] = from_float<T>(__fmul_rn(__fmul_rn(p.y, scale), tensor));
+        }
+        T *const out = static_cast<T *>(a.out) + r * a.ldo + c;
+        if (a.vec && c + 8 <= a.cols) {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(out)[i] = reinterpret_cast<const uint4 *>(v)[i];
+        } else {
+            for (int j = 0; j < 8; ++j)
+                if (c + j < a.cols) out[j] = v[j];
+        }
+    }
+}
+
+// ------------------------------------------------ exponent of a tensor ----
+// Every CTA raises the result, which starts below any exponent, to that of its own largest magnitude: a maximum of
+// integers, the same whatever the order.
+template <typename T>
+__global__ __launch_bounds__(THREADS) void qesgd_fp4_tensor_exponent_kernel(const T *x, uint64_t rows, uint64_t cols, uint64_t ldx, bool vec,
+                                                                            int32_t *out, uint32_t *status)
+{
+    __shared__ uint32_t tops[THREADS / 32];
+    qesgd_wait_for_previous();
+    const uint64_t octets = (cols + 7) / 8, all = octets * rows;
+    uint32_t top = 0u;
+    bool bad = false;
+    for (uint64_t n = (uint64_t)blockIdx.x * THREADS + threadIdx.x; n < all; n += (uint64_t)gridDim.x * THREADS) {
+        float v[8];
+        load_octet(x + n / octets * ldx, n % octets * 8, cols, vec, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t m = __float_as_uint(v[j]) & 0x7FFFFFFFu;
+            bad |= m >= 0x7F800000u;
+            top = max(top, m >= 0x7F800000u ? 0u : m);
+        }
+    }
+    top = __reduce_max_sync(FULL, top);
+    if (threadIdx.x % 32 == 0) tops[threadIdx.x / 32] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < THREADS / 32; ++i) top = max(top, tops[i]);
+        // top = 1.f * 2^(E - 127) is at most 2688 * 2^t = 1.3125 * 2^(t + 11) from t = E - 138 on, one later where 1.f > 1.3125
+        const int t = (int)(top >> 23) - 138 + ((top & 0x7FFFFFu) > 0x280000u ? 1 : 0);
+        atomicMax(out, top == 0u ? -126 : clamp_exponent(t));
+    }
+    if (bad) atomicOr(status, QESGD_STATUS_NONFINITE);
+}
+
+template <typename T, int FORMAT, bool STOCHASTIC>
+cudaError_t launch_quantize(const Fp4QuantizeArgs &a, cudaStream_t stream)
+{
+    const uint64_t row_tiles = qesgd_div_up(a.rows, TILE_ROWS);
+    if (!a.codes_t) {
+        const uint64_t tiles = row_tiles * qesgd_div_up(a.cols, ROW_COLS);
+        return qesgd_launch(qesgd_fp4_quantize_rows_kernel<T, FORMAT, STOCHASTIC>, dim3((unsigned)(tiles < 0x7FFFFFFF ? tiles : 0x7FFFFFFF)), dim3(THREADS), stream, a);
+    }
+    const auto kernel = qesgd_fp4_quantize_columns_kernel<T, FORMAT, STOCHASTIC>;
+    const uint64_t tiles = row_tiles * qesgd_div_up(a.cols, SIDE);
+    const int smem = SIDE * (SIDE + 4 / (int)sizeof(T)) * (int)sizeof(T);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    return qesgd_launch_smem(kernel, dim3((unsigned)(tiles < 0x7FFFFFFF ? tiles : 0x7FFFFFFF)), dim3(THREADS), smem, stream, a);
+}
+template <typename T>
+cudaError_t launch_quantize(const Fp4QuantizeArgs &a, uint32_t format, bool stochastic, cudaStream_t stream)
+{
+    if (format == QESGD_FP4_MX)
+        return stochastic ? launch_quantize<T, QESGD_FP4_MX, true>(a, stream) : launch_quantize<T, QESGD_FP4_MX, false>(a, stream);
+    return stochastic ? launch_quantize<T, QESGD_FP4_NV, true>(a, stream) : launch_quantize<T, QESGD_FP4_NV, false>(a, stream);
+}
+template <typename T>
+cudaError_t launch_dequantize(const Fp4DequantizeArgs &a, uint32_t format, cudaStream_t stream)
+{
+    const uint64_t ctas = qesgd_div_up(qesgd_div_up(a.cols, 8) * a.rows, THREADS);
+    const dim3 grid((unsigned)(ctas < 0x7FFFFFFF ? ctas : 0x7FFFFFFF));
+    if (format == QESGD_FP4_MX) return qesgd_launch(qesgd_fp4_dequantize_kernel<T, QESGD_FP4_MX>, grid, dim3(THREADS), stream, a);
+    return qesgd_launch(qesgd_fp4_dequantize_kernel<T, QESGD_FP4_NV>, grid, dim3(THREADS), stream, a);
+}
+template <typename T>
+cudaError_t launch_exponent(const void *x, uint64_t rows, uint64_t cols, uint64_t ldx, bool vec, int32_t *out, uint32_t *status,
+                            int sm_count, cudaStream_t stream)
+{
+    const uint64_t ctas = qesgd_div_up(qesgd_div_up(cols, 8) * rows, THREADS), most = (uint64_t)sm_count * 8;
+    return qesgd_launch(qesgd_fp4_tensor_exponent_kernel<T>, dim3((unsigned)(ctas < most ? ctas : most)), dim3(THREADS), stream,
+                        static_cast<const T *>(x), rows, cols, ldx, vec, out, status);
+}
+
+}  // namespace
+
+int qesgd_launch_fp4_quantize(const Fp4QuantizeArgs &a, uint32_t dtype, uint32_t format, bool stochastic, cudaStream_t stream)
+{
+    switch (dtype) {
+        case QESGD_F32: return (int)launch_quantize<float>(a, format, stochastic, stream);
+        case QESGD_BF16: return (int)launch_quantize<__nv_bfloat16>(a, format, stochastic, stream);
+        default: return (int)launch_quantize<__half>(a, format, stochastic, stream);
+    }
+}
+int qesgd_launch_fp4_dequantize(const Fp4DequantizeArgs &a, uint32_t dtype, uint32_t format, cudaStream_t stream)
+{
+    switch (dtype) {
+        case QESGD_F32: return (int)launch_dequantize<float>(a, format, stream);
+        case QESGD_BF16: return (int)launch_dequantize<__nv_bfloat16>(a, format, stream);
+        default: return (int)launch_dequantize<__half>(a, format, stream);
+    }
+}
+int qesgd_launch_fp4_tensor_exponent(const void *x, uint32_t dtype, uint64_t rows, uint64_t cols, uint64_t ldx, bool vec,
+                                     int32_t *out, uint32_t *status, int sm_count, cudaStream_t stream)
+{
+    const cudaError_t e = cudaMemsetAsync(out, 0x80, sizeof(int32_t), stream);   // below every exponent
+    if (e != cudaSuccess) return (int)e;
+    switch (dtype) {
+        case QESGD_F32: return (int)launch_exponent<float>(x, rows, cols, ldx, vec, out, status, sm_count, stream);
+        case QESGD_BF16: return (int)launch_exponent<__nv_bfloat16>(x, rows, cols, ldx, vec, out, status, sm_count, stream);
+        default: return (int)launch_exponent<__half>(x, rows, cols, ldx, vec, out, status, sm_count, stream);
+    }
+}

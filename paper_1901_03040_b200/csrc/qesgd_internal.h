@@ -29,6 +29,31 @@ struct qesgd_ctx {
     uint32_t drop_cta;      // give-up-path test hook of the local-epoch kernels (none: ~0)
     uint32_t lr_plan[8];    // qesgd_debug_lr_plan
 };
+
+inline bool qesgd_aligned(const void *p, uintptr_t a) { return ((uintptr_t)p % a) == 0; }
+
+// Binds the context's device for the duration of a call and restores the caller's.
+struct DeviceGuard {
+    int prev = -1;
+    bool ok = false;
+    explicit DeviceGuard(int device)
+    {
+        if (cudaGetDevice(&prev) != cudaSuccess) return;
+        ok = (prev == device) || cudaSetDevice(device) == cudaSuccess;
+        if (prev == device) prev = -1;
+    }
+    ~DeviceGuard()
+    {
+        if (ok && prev >= 0) cudaSetDevice(prev);
+    }
+};
+
+inline int qesgd_cuda_fail(qesgd_ctx *ctx, int err)
+{
+    ctx->last_cuda_error = err;
+    return QESGD_ECUDA;
+}
+
 static const uint64_t QESGD_DEFAULT_WAIT_NS = 1000000000ull;
 static const uint64_t QESGD_MAX_WAIT_NS = 10000000000ull;
 
@@ -55,11 +80,12 @@ static const uint64_t QESGD_LR_WORK_FLOATS = (1ull << 20) - QESGD_LR_EPOCH_FLOAT
 // 319 -> 311, and no grid was found that is slower.  (With griddepcontrol.launch_dependents at the top of
 // every kernel the successor's CTAs come early: 461 instead of 353 us for an encode of 400 000 CTAs.)
 template <typename... Params, typename... Args>
-inline cudaError_t qesgd_launch(void (*kernel)(Params...), dim3 grid, dim3 block, cudaStream_t stream, const Args &...args)
+inline cudaError_t qesgd_launch_smem(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, const Args &...args)
 {
     cudaLaunchConfig_t c = {};
     c.gridDim = grid;
     c.blockDim = block;
+    c.dynamicSmemBytes = smem;
     c.stream = stream;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -67,6 +93,11 @@ inline cudaError_t qesgd_launch(void (*kernel)(Params...), dim3 grid, dim3 block
     c.attrs = at;
     c.numAttrs = 1;
     return cudaLaunchKernelEx(&c, kernel, Params(args)...);
+}
+template <typename... Params, typename... Args>
+inline cudaError_t qesgd_launch(void (*kernel)(Params...), dim3 grid, dim3 block, cudaStream_t stream, const Args &...args)
+{
+    return qesgd_launch_smem(kernel, grid, block, 0, stream, args...);
 }
 #ifdef __CUDACC__
 __device__ __forceinline__ void qesgd_wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
@@ -121,6 +152,51 @@ struct DecodeArgs {
     uint32_t *status;
 };
 int qesgd_launch_range_selftest(uint32_t *status, cudaStream_t stream);
+
+// A matrix on its way into 4-bit floats.
+struct Fp4QuantizeArgs {
+    const void *x;
+    uint64_t rows, cols, ldx;       // elements
+    const int32_t *tensor_exponent; // device, may be null
+    uint32_t round_key[10][2];      // Philox round keys (stochastic rounding)
+    uint32_t worker, epoch;
+    uint8_t *codes, *scales;        // blocks along the rows; may be null
+    uint8_t *codes_t, *scales_t;    // the transpose; may be null
+    uint32_t vec;                   // x and its rows 16-byte aligned
+    uint32_t *status;
+};
+struct Fp4DequantizeArgs {
+    const uint8_t *codes, *scales;
+    uint64_t rows, cols, ldo;
+    const int32_t *tensor_exponent;
+    void *out;
+    uint32_t vec;                   // out and its rows 16-byte aligned
+};
+struct Fp4MatmulArgs {
+    const uint8_t *a_codes, *a_scales, *b_codes, *b_scales;
+    const int32_t *a_exponent, *b_exponent;
+    uint64_t M, N, K, ldc;
+    void *c;
+    uint32_t accumulate;
+};
+struct OrthoArgs {
+    const void *x;
+    uint32_t dtype;
+    uint64_t rows, cols, ldx, batch, x_stride;
+    uint32_t steps;
+    float a, b, c;
+    void *out;
+    uint64_t ldo, out_stride;
+    uint8_t *workspace;
+    uint32_t *status;
+};
+inline uint64_t qesgd_div_up(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
+int qesgd_launch_fp4_tensor_exponent(const void *x, uint32_t dtype, uint64_t rows, uint64_t cols, uint64_t ldx, bool vec,
+                                     int32_t *out, uint32_t *status, int sm_count, cudaStream_t stream);
+int qesgd_launch_fp4_quantize(const Fp4QuantizeArgs &a, uint32_t dtype, uint32_t format, bool stochastic, cudaStream_t stream);
+int qesgd_launch_fp4_dequantize(const Fp4DequantizeArgs &a, uint32_t dtype, uint32_t format, cudaStream_t stream);
+int qesgd_launch_fp4_matmul(const Fp4MatmulArgs &a, uint32_t dtype, uint32_t format, int sm_count, cudaStream_t stream, int *launched);
+int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t stream, int *launched);
 
 // Launchers.  Return a cudaError_t as int.  qesgd_codec.cu is compiled once per code width
 // and defines the *_2, *_4, *_8 functions; the width-dispatching wrappers are inline here.

@@ -1,0 +1,52 @@
+// Workspace of qesgd_orthogonalize, and the scales at which its intermediates are kept.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "qesgd_internal.h"
+
+// X, A = X X^T and B = b A + c A A are kept in fp16, times powers of two.  With X = G / ||G||_F elements of an n x n matrix
+// start near 1 / n and end near 1 / sqrt(n), those of A near n^-1.5: unscaled they would fall below fp16's normal
+// numbers (6e-5) from n = 128 on.  In magnitude X may reach 255, A 15, B 63.
+constexpr float ORTHO_X_SCALE = 256.0f, ORTHO_A_SCALE = 4096.0f, ORTHO_B_SCALE = 1024.0f;
+// What rounding X to fp16 leaves behind, times 2^11, is kept beside X for the term a X of the first steps.  There the
+// rounding error of the large singular values is as large as small ones and grows with them: for singular values
+// falling as 1 / i (512 x 512) five steps end 3.3e-3 off without, 1.9e-3 with two steps of it, 1.8e-3 with three (of which
+// 1.7e-3 is the result's rounding to bf16); from the fourth on it gains nothing.
+constexpr float ORTHO_LO_SCALE = 2048.0f;
+constexpr uint32_t ORTHO_LO_STEPS = 3;
+
+struct OrthoView {
+    __half *hi, *lo;
+    uint64_t ld, x_stride;
+};
+
+// m = the smaller side, n = the larger: X is m x n whichever way the matrix lies.
+struct OrthoLayout {
+    uint64_t m, n, ld_x, ld_a, x_stride, a_stride;   // elements
+    uint32_t parts;                                  // partial sums of a matrix's norm
+    uint64_t off_hi[2], off_lo[2], off_a, off_b, bytes;
+};
+inline OrthoLayout qesgd_ortho_layout(uint64_t rows, uint64_t cols, uint64_t batch)
+{
+    OrthoLayout l;
+    l.m = rows < cols ? rows : cols;
+    l.n = rows < cols ? cols : rows;
+    l.ld_x = (l.n + 7) / 8 * 8;      // rows begin on 16 bytes
+    l.ld_a = (l.m + 7) / 8 * 8;
+    l.x_stride = (l.m * l.ld_x + 63) / 64 * 64;
+    l.a_stride = (l.m * l.ld_a + 63) / 64 * 64;
+    const uint64_t parts = qesgd_div_up(l.m * l.n, 8192);
+    l.parts = (uint32_t)(parts < 256 ? parts : 256);
+    uint64_t at = (batch * l.parts * sizeof(double) + 255) / 256 * 256;
+    const uint64_t x = (batch * l.x_stride * 2 + 255) / 256 * 256, a = (batch * l.a_stride * 2 + 255) / 256 * 256;
+    for (int i = 0; i < 2; ++i) {
+        l.off_hi[i] = at;
+        l.off_lo[i] = at + x;
+        at += 2 * x;
+    }
+    l.off_a = at;
+    l.off_b = at + a;
+    l.bytes = at + 2 * a;
+    return l;
+}

@@ -84,7 +84,9 @@ struct Args {
 #define ENTRIES(X)                                                                                           \
     X(qesgd_encode) X(qesgd_encode_batch) X(qesgd_requantize) X(qesgd_lr_qesgd_step)                         \
     X(qesgd_decode_average_apply) X(qesgd_decode_average_axpy) X(qesgd_decode) X(qesgd_lr_sgd_step)          \
-    X(qesgd_lr_gradient) X(qesgd_lr_local_epoch) X(qesgd_lr_local_epoch_batch) X(qesgd_lr_sgd_step_noalloc)
+    X(qesgd_lr_gradient) X(qesgd_lr_local_epoch) X(qesgd_lr_local_epoch_batch) X(qesgd_lr_sgd_step_noalloc) \
+    X(qesgd_fp4_tensor_exponent) X(qesgd_fp4_quantize) X(qesgd_fp4_dequantize) X(qesgd_fp4_matmul)           \
+    X(qesgd_orthogonalize)
 #define DECLARE(name) decltype(&::name) f_##name;
 ENTRIES(DECLARE)
 #undef DECLARE
@@ -256,6 +258,68 @@ ENTRY(qesgd_lr_sgd_step_noalloc, 7)
     const float lr = x.f32();
     auto *u = x.tensor<float>();
 CALL(qesgd_lr_sgd_step_noalloc, stream, X, y, m, d, lr, u)
+
+ENTRY(qesgd_fp4_tensor_exponent, 7)
+    auto *ctx = (qesgd_ctx *)x.address();
+    auto *in = x.tensor<const void>();
+    const uint32_t dtype = x.u32();
+    const uint64_t rows = x.u64(), cols = x.u64(), ldx = x.u64();
+    auto *out = x.tensor<int32_t>();
+CALL(qesgd_fp4_tensor_exponent, ctx, in, dtype, rows, cols, ldx, out)
+
+ENTRY(qesgd_fp4_quantize, 16)
+    auto *ctx = (qesgd_ctx *)x.address();
+    auto *in = x.tensor<const void>();
+    const uint32_t dtype = x.u32();
+    const uint64_t rows = x.u64(), cols = x.u64(), ldx = x.u64();
+    const uint32_t format = x.u32();
+    auto *exponent = x.tensor<const int32_t>();
+    const uint32_t rounding = x.u32();
+    const uint64_t seed = x.u64();
+    const uint32_t worker = x.u32(), epoch = x.u32();
+    auto *codes = x.tensor<uint8_t>(), *scales = x.tensor<uint8_t>(), *codes_t = x.tensor<uint8_t>(), *scales_t = x.tensor<uint8_t>();
+CALL(qesgd_fp4_quantize, ctx, in, dtype, rows, cols, ldx, format, exponent, rounding, seed, worker, epoch, codes, scales,
+     codes_t, scales_t)
+
+ENTRY(qesgd_fp4_dequantize, 10)
+    auto *ctx = (qesgd_ctx *)x.address();
+    auto *codes = x.tensor<const uint8_t>(), *scales = x.tensor<const uint8_t>();
+    const uint64_t rows = x.u64(), cols = x.u64();
+    const uint32_t format = x.u32();
+    auto *exponent = x.tensor<const int32_t>();
+    auto *out = x.tensor<void>();
+    const uint32_t dtype = x.u32();
+    const uint64_t ldo = x.u64();
+CALL(qesgd_fp4_dequantize, ctx, codes, scales, rows, cols, format, exponent, out, dtype, ldo)
+
+ENTRY(qesgd_fp4_matmul, 15)
+    auto *ctx = (qesgd_ctx *)x.address();
+    auto *a_codes = x.tensor<const uint8_t>(), *a_scales = x.tensor<const uint8_t>();
+    auto *a_exponent = x.tensor<const int32_t>();
+    auto *b_codes = x.tensor<const uint8_t>(), *b_scales = x.tensor<const uint8_t>();
+    auto *b_exponent = x.tensor<const int32_t>();
+    const uint64_t M = x.u64(), N = x.u64(), K = x.u64();
+    const uint32_t format = x.u32();
+    auto *c = x.tensor<void>();
+    const uint32_t dtype = x.u32();
+    const uint64_t ldc = x.u64();
+    const uint32_t accumulate = x.u32();
+CALL(qesgd_fp4_matmul, ctx, a_codes, a_scales, a_exponent, b_codes, b_scales, b_exponent, M, N, K, format, c, dtype, ldc,
+     accumulate)
+
+ENTRY(qesgd_orthogonalize, 17)
+    auto *ctx = (qesgd_ctx *)x.address();
+    auto *in = x.tensor<const void>();
+    const uint32_t dtype = x.u32();
+    const uint64_t rows = x.u64(), cols = x.u64(), ldx = x.u64(), batch = x.u64(), x_stride = x.u64();
+    const uint32_t steps = x.u32();
+    const float a = x.f32(), b = x.f32(), c = x.f32();
+    auto *out = x.tensor<void>();
+    const uint64_t ldo = x.u64(), out_stride = x.u64();
+    auto *workspace = x.tensor<void>();
+    const uint64_t workspace_bytes = x.u64();
+CALL(qesgd_orthogonalize, ctx, in, dtype, rows, cols, ldx, batch, x_stride, steps, a, b, c, out, ldo, out_stride, workspace,
+     workspace_bytes)
 
 // bind({name: address}, by_ctypes): every entry point, before the first call
 PyObject *py_bind(PyObject *, PyObject *args)

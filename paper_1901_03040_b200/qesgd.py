@@ -16,6 +16,9 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libqesgd_debug.so" if os.environ.get("QESGD_DEBUG") == "1" else "libqesgd.so")
 
 SCALE_NORM, SCALE_MAX, SCALE_FIXED = 0, 1, 2
+F32, BF16, F16 = 0, 1, 2
+FP4_MX, FP4_NV = 0, 1
+ROUND_NEAREST, ROUND_STOCHASTIC = 0, 1
 STATUS_NONFINITE = 1
 STATUS_TIMEOUT = 2
 STATUS_RANGE = 4
@@ -23,6 +26,7 @@ LR_TWO_PASSES, LR_PERSISTENT, LR_CLUSTER, LR_GROUP, LR_PLAIN = range(5)
 OK, EINVAL, ECUDA, ENOMEM, ELIMIT = 0, -1, -2, -3, -4
 MAX_WORKERS, MIN_BUCKET, MAX_BUCKET, MAX_LR_BATCH = 64, 64, 8192, 1024
 NOALLOC_MAX_LR_BATCH = 256
+MAX_MATRIX_SIDE, MAX_ORTHO_SIDE, MAX_ORTHO_BATCH, MAX_ORTHO_STEPS = 0x7FFFFF00, 65536, 4096, 32
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(
@@ -60,6 +64,14 @@ SIGNATURES = {
     "qesgd_lr_local_epoch": (_int, [_vp, _vp, _vp, _u64, _u64, _u32, _f32, _vp]),
     "qesgd_lr_local_epoch_batch": (_int, [_vp, _vp, _vp, _u64, _u64, _u32, _u32, _f32, _vp, _u64]),
     "qesgd_lr_sgd_step_noalloc": (_int, [_vp, _vp, _vp, _u32, _u64, _f32, _vp]),
+    "qesgd_fp4_row_bytes": (_u64, [_u64]),
+    "qesgd_fp4_scale_bytes": (_u64, [_u64, _u64, _u32]),
+    "qesgd_fp4_tensor_exponent": (_int, [_vp, _vp, _u32, _u64, _u64, _u64, _vp]),
+    "qesgd_fp4_quantize": (_int, [_vp, _vp, _u32, _u64, _u64, _u64, _u32, _vp, _u32, _u64, _u32, _u32, _vp, _vp, _vp, _vp]),
+    "qesgd_fp4_dequantize": (_int, [_vp, _vp, _vp, _u64, _u64, _u32, _vp, _vp, _u32, _u64]),
+    "qesgd_fp4_matmul": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _u64, _u64, _u64, _u32, _vp, _u32, _u64, _u32]),
+    "qesgd_orthogonalize_workspace": (_u64, [_u64, _u64, _u64]),
+    "qesgd_orthogonalize": (_int, [_vp, _vp, _u32, _u64, _u64, _u64, _u64, _u64, _u32, _f32, _f32, _f32, _vp, _u64, _u64, _vp, _u64]),
     "qesgd_status": (_int, [_vp, C.POINTER(_u32)]),
     "qesgd_debug_build": (_int, []),
     "qesgd_debug_range_selftest": (_int, [_vp]),
@@ -99,6 +111,18 @@ def num_buckets(d, bucket):
 
 def code_bytes(d, bucket, bits):
     return int(lib.qesgd_code_bytes(d, bucket, bits))
+
+
+def fp4_row_bytes(cols):
+    return int(lib.qesgd_fp4_row_bytes(cols))
+
+
+def fp4_scale_bytes(rows, cols, format):
+    return int(lib.qesgd_fp4_scale_bytes(rows, cols, format))
+
+
+def orthogonalize_workspace(rows, cols, batch=1):
+    return int(lib.qesgd_orthogonalize_workspace(rows, cols, batch))
 
 
 class Context:
@@ -230,6 +254,39 @@ class Context:
         if rc:
             self._check(rc)
 
+    # -- matrices ------------------------------------------------------------
+    def qesgd_fp4_tensor_exponent(self, x, dtype, rows, cols, ldx, exponent_out):
+        rc = _native.qesgd_fp4_tensor_exponent(self._address, x, dtype, rows, cols, ldx, exponent_out)
+        if rc:
+            self._check(rc)
+
+    def qesgd_fp4_quantize(self, x, dtype, rows, cols, ldx, format, tensor_exponent, rounding, seed, worker, epoch,
+                           codes_out, scales_out, codes_t_out=None, scales_t_out=None):
+        rc = _native.qesgd_fp4_quantize(self._address, x, dtype, rows, cols, ldx, format, tensor_exponent, rounding,
+                                        seed, worker, epoch, codes_out, scales_out, codes_t_out, scales_t_out)
+        if rc:
+            self._check(rc)
+
+    def qesgd_fp4_dequantize(self, codes, scales, rows, cols, format, tensor_exponent, out, dtype, ldo):
+        rc = _native.qesgd_fp4_dequantize(self._address, codes, scales, rows, cols, format, tensor_exponent, out, dtype,
+                                          ldo)
+        if rc:
+            self._check(rc)
+
+    def qesgd_fp4_matmul(self, a_codes, a_scales, a_exponent, b_codes, b_scales, b_exponent, M, N, K, format, c, dtype,
+                         ldc, accumulate=0):
+        rc = _native.qesgd_fp4_matmul(self._address, a_codes, a_scales, a_exponent, b_codes, b_scales, b_exponent, M, N,
+                                      K, format, c, dtype, ldc, accumulate)
+        if rc:
+            self._check(rc)
+
+    def qesgd_orthogonalize(self, x, dtype, rows, cols, ldx, batch, x_stride, steps, out, ldo, out_stride, workspace,
+                            workspace_bytes, a=3.4445, b=-4.7750, c=2.0315):
+        rc = _native.qesgd_orthogonalize(self._address, x, dtype, rows, cols, ldx, batch, x_stride, steps, a, b, c, out,
+                                         ldo, out_stride, workspace, workspace_bytes)
+        if rc:
+            self._check(rc)
+
     # -- bookkeeping ---------------------------------------------------------
     def qesgd_status(self):
         flags = C.c_uint32(0)
@@ -260,3 +317,10 @@ def alloc_stream_buffers(K, d, bucket, bits, device):
     codes = torch.zeros((K, cb), dtype=torch.uint8, device=device)
     scales = torch.zeros((K, nb_pad), dtype=torch.float32, device=device)
     return codes, scales
+
+
+def alloc_fp4(rows, cols, format, device):
+    """Device buffers of a rows x cols matrix of 4-bit floats: (codes uint8[rows, row bytes], scales uint8[bytes])."""
+    import torch
+    return (torch.empty((rows, fp4_row_bytes(cols)), dtype=torch.uint8, device=device),
+            torch.empty(fp4_scale_bytes(rows, cols, format), dtype=torch.uint8, device=device))
