@@ -31,6 +31,7 @@ UNITS = [
     ("qesgd_fp4.cu", "qesgd_fp4.o", ["-fmad=false"]),
     ("qesgd_fp4_matmul.cu", "qesgd_fp4_matmul.o", []),
     ("qesgd_orthogonalize.cu", "qesgd_orthogonalize.o", []),
+    ("qesgd_mma.cu", "qesgd_mma.o", []),
     ("qesgd_matrix.cu", "qesgd_matrix.o", []),
 ]
 
@@ -66,7 +67,8 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     build_py_module(force)
     headers = [os.path.join(CSRC, "qesgd_internal.h"), os.path.join(CSRC, "qesgd_lr_device.cuh"),
                os.path.join(CSRC, "qesgd_lr_tile.h"),
-               os.path.join(CSRC, "qesgd_orthogonalize.h"), os.path.join(ROOT, "include", "qesgd.h"),
+               os.path.join(CSRC, "qesgd_orthogonalize.h"),
+               os.path.join(CSRC, "qesgd_device.cuh"), os.path.join(CSRC, "qesgd_mma.cuh"), os.path.join(ROOT, "include", "qesgd.h"),
                os.path.abspath(__file__)]
     nvcc = _nvcc()
     objs = []

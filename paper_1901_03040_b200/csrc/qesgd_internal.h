@@ -80,19 +80,28 @@ static const uint64_t QESGD_LR_WORK_FLOATS = (1ull << 20) - QESGD_LR_EPOCH_FLOAT
 // 319 -> 311, and no grid was found that is slower.  (With griddepcontrol.launch_dependents at the top of
 // every kernel the successor's CTAs come early: 461 instead of 353 us for an encode of 400 000 CTAs.)
 template <typename... Params, typename... Args>
-inline cudaError_t qesgd_launch_smem(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, const Args &...args)
+inline cudaError_t qesgd_launch_cluster(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, uint32_t cluster, cudaStream_t stream,
+                                        const Args &...args)
 {
     cudaLaunchConfig_t c = {};
     c.gridDim = grid;
     c.blockDim = block;
     c.dynamicSmemBytes = smem;
     c.stream = stream;
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     c.attrs = at;
-    c.numAttrs = 1;
+    c.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&c, kernel, Params(args)...);
+}
+template <typename... Params, typename... Args>
+inline cudaError_t qesgd_launch_smem(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, const Args &...args)
+{
+    return qesgd_launch_cluster(kernel, grid, block, smem, 1u, stream, args...);
 }
 template <typename... Params, typename... Args>
 inline cudaError_t qesgd_launch(void (*kernel)(Params...), dim3 grid, dim3 block, cudaStream_t stream, const Args &...args)

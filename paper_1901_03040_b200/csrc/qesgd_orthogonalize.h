@@ -25,7 +25,8 @@ struct OrthoView {
 struct OrthoLayout {
     uint64_t m, n, ld_x, ld_a, x_stride, a_stride;   // elements
     uint32_t parts;                                  // partial sums of a matrix's norm
-    uint64_t off_hi[2], off_lo[2], off_a, off_b, bytes;
+    uint64_t d_stride;                               // floats: a diagonal, up to whole tiles
+    uint64_t off_hi[2], off_lo[2], off_a, off_b, off_d, bytes;
 };
 inline OrthoLayout qesgd_ortho_layout(uint64_t rows, uint64_t cols, uint64_t batch)
 {
@@ -47,6 +48,8 @@ inline OrthoLayout qesgd_ortho_layout(uint64_t rows, uint64_t cols, uint64_t bat
     }
     l.off_a = at;
     l.off_b = at + a;
-    l.bytes = at + 2 * a;
+    l.d_stride = (l.m + 255) / 256 * 256;
+    l.off_d = at + 2 * a;
+    l.bytes = l.off_d + 2 * batch * l.d_stride * sizeof(float);
     return l;
 }

@@ -312,6 +312,16 @@ def test_orthogonalize(dtype, rows, cols):
     assert G.ctx().qesgd_status() == 0
 
 
+@pytest.mark.parametrize("rows,cols", [(600, 900), (900, 600), (513, 513)])
+def test_orthogonalize_of_many_larger_matrices(rows, cols):
+    """Enough tiles that pairs of SMs share them, in all three products."""
+    x = _gradient(14, rows, cols, qesgd.BF16, 2, 3)
+    got = _np(_orthogonalize(x, qesgd.BF16, rows, cols, 14))
+    for i in range(14):
+        want = ref.orthogonalize(_np(x[i, :, :cols]))
+        assert np.linalg.norm(got[i] - want) <= ORTHO_TOLERANCE * np.linalg.norm(want)
+
+
 @pytest.mark.parametrize("rows,cols", [(1, 1), (1, 50), (50, 1), (2, 3), (5, 700), (15, 15)])
 def test_orthogonalize_of_few_rows(rows, cols):
     x = _gradient(2, rows, cols, qesgd.F32, 5)
