@@ -1,27 +1,53 @@
-// C = A B^T on microscaled 4-bit operands (see include/qesgd.h for the layout).
+// C = A B^T on microscaled 4-bit operands (layout in include/qesgd.h), on the tensor cores' block-scaled products.
+//
+// Rows of B lie along the 128 lanes of tensor memory and rows of A along its columns, so that a warp that takes a finished
+// tile out holds 32 neighbouring elements of a row of C for each of its registers: stores of 64 or 128 consecutive bytes,
+// whatever C's alignment, and a single token fills the lanes with the weight's rows.
+//
+// A stage is a contraction of 256: 128 bytes of codes of each row, and the tiles of scales as they lie in memory (128 rows by 4
+// blocks, 512 bytes), which go on to tensor memory in the same order.  What lies outside the matrices arrives as zeros.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
-#include "qesgd_internal.h"
+#include "qesgd_mma.cuh"
 
 namespace {
 
-constexpr int THREADS = 256;
-constexpr int TILE = 64, DEPTH = 32;
+constexpr int WARPS = 12;                 // copies, products, 2 without work, 8 that take tiles out
+constexpr uint32_t DEPTH = 256;           // contraction of a stage
+constexpr uint32_t LANES = 128;           // rows of B of a CTA
+constexpr uint32_t SCALE_TILE = 512;
 
-__device__ __forceinline__ float grid_value(uint32_t code)
-{
-    const uint32_t l = code & 7u;
-    const float v = l < 4u ? 0.5f * (float)l : l < 6u ? (float)l - 2.0f : 2.0f * (float)l - 8.0f;
-    return code & 8u ? -v : v;
-}
-__device__ __forceinline__ float scale_value(uint32_t byte, bool mx)
-{
-    if (mx) return byte ? __uint_as_float(byte << 23) : __uint_as_float(0x00400000u);
-    return __uint_as_float((byte & 0x7Fu) << 20) * 0x1p120f;
-}
-__device__ __forceinline__ int exponent_of(const int32_t *p) { return p ? min(max(*p, -126), 126) : 0; }
+// PAIR: two CTAs on 256 rows of B by 256 of A, one tile in tensor memory at a time (its other half holds scales).
+// Else 128 rows of B by 32, 64 or 128 of A, two tiles in tensor memory, and the contraction shared out to a cluster.
+template <bool PAIR>
+struct Shape {
+    static constexpr uint32_t MOST_Q = PAIR ? 256 : 128;      // rows of A of a tile
+    static constexpr uint32_t HELD_Q = 128;                   // rows of A in a CTA's shared memory
+    static constexpr uint32_t TILES = PAIR ? 1 : 2;           // in tensor memory
+    static constexpr int STAGES = PAIR ? 5 : 6;
+    static constexpr uint32_t SCALES_P = 2048, SCALES_Q = MOST_Q / 128 * 2048;   // bytes of a stage at most (NV)
+    static constexpr uint32_t STAGE_BYTES = LANES * 128 + HELD_Q * 128 + SCALES_P + SCALES_Q;
+    static constexpr uint32_t SMEM = STAGES * STAGE_BYTES + 1024 + 256;
+    static constexpr uint32_t COLUMNS = 512;
+    static constexpr uint32_t SCALE_COLUMN = TILES * MOST_Q;  // two sets of scales behind the tiles
+    static constexpr uint32_t SET = 16 + MOST_Q / 128 * 16;
+};
 
+struct ProductArgs {
+    uint32_t M, N, steps, split;              // split: CTAs of a cluster that share the contraction
+    uint32_t q;                               // rows of A of a tile
+    uint32_t tiles_n, tiles;
+    const int32_t *a_exponent, *b_exponent;
+    void *c;
+    uint64_t ldc;
+    uint32_t dtype, accumulate;
+    uint32_t *status;
+};
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
 template <typename T>
 __device__ __forceinline__ T from_float(float v);
 template <>
@@ -31,68 +57,273 @@ __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { re
 template <>
 __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 
-// One CTA computes 64 x 64 of C from decoded operands in shared memory.
-template <typename T>
-__global__ __launch_bounds__(THREADS) void qesgd_fp4_matmul_kernel(const __grid_constant__ Fp4MatmulArgs a, bool mx)
+// Column n of `count` rows of C from row m on.
+template <typename T, int COUNT>
+__device__ __forceinline__ void store_column(const float (&v)[COUNT], T *c, uint32_t m, uint32_t M, uint64_t ldc, bool accumulate, float power_a, float power_b)
 {
-    __shared__ float as[DEPTH][TILE + 1], bs[DEPTH][TILE + 1];
-    qesgd_wait_for_previous();
-    const uint32_t block = mx ? 32u : 16u;
-    const uint64_t tiles_n = (a.N + TILE - 1) / TILE, tiles = tiles_n * ((a.M + TILE - 1) / TILE);
-    const uint64_t row_bytes = (a.K + 31) / 32 * 16, scale_tiles = (a.K + 4 * block - 1) / (4 * block);
-    const float power = ldexpf(1.0f, exponent_of(a.a_exponent)) , power2 = ldexpf(1.0f, exponent_of(a.b_exponent));
-    const uint32_t tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    for (uint64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const uint64_t m0 = tile / tiles_n * TILE, n0 = tile % tiles_n * TILE;
-        float acc[4][4] = {};
-        for (uint64_t k0 = 0; k0 < a.K; k0 += DEPTH) {
-            for (uint32_t i = threadIdx.x; i < TILE * DEPTH; i += THREADS) {
-                const uint64_t k = k0 + i % DEPTH, block_k = k / block;
-                for (int side = 0; side < 2; ++side) {
-                    const uint64_t r = (side ? n0 : m0) + i / DEPTH;
-                    float v = 0.0f;
-                    if (r < (side ? a.N : a.M) && k < a.K) {
-                        const uint32_t byte = (side ? a.b_codes : a.a_codes)[r * row_bytes + k / 2];
-                        const uint32_t s = (side ? a.b_scales : a.a_scales)[(r / 128 * scale_tiles + block_k / 4) * 512 + r % 32 * 16 + r / 32 % 4 * 4 + block_k % 4];
-                        v = grid_value(k % 2 ? byte >> 4 : byte & 15u) * scale_value(s, mx);
-                    }
-                    (side ? bs : as)[i % DEPTH][i / DEPTH] = v;
-                }
-            }
-            __syncthreads();
-            for (int k = 0; k < DEPTH; ++k)
+    constexpr int GROUP = COUNT < 8 ? COUNT : 8;   // loads of C in flight
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+    for (int g = 0; g < COUNT; g += GROUP) {
+        float old[GROUP];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[i][j] += as[k][ty + 16 * i] * bs[k][tx + 16 * j];
-            __syncthreads();
+        for (int k = 0; k < GROUP; ++k) old[k] = accumulate && m + g + k < M ? to_float(c[(g + k) * ldc]) : 0.0f;
+#pragma unroll
+        for (int k = 0; k < GROUP; ++k) {
+            const float p = v[g + k] * power_a * power_b;
+            if (m + g + k < M) c[(g + k) * ldc] = from_float<T>(accumulate ? old[k] + p : p);
         }
-        for (int i = 0; i < 4; ++i)
-            for (int j = 0; j < 4; ++j) {
-                const uint64_t r = m0 + ty + 16 * i, c = n0 + tx + 16 * j;
-                if (r >= a.M || c >= a.N) continue;
-                T *const out = static_cast<T *>(a.c) + r * a.ldc + c;
-                const float v = acc[i][j] * power * power2;
-                *out = from_float<T>(a.accumulate ? (float)*out + v : v);
-            }
     }
 }
-
-template <typename T>
-cudaError_t launch(const Fp4MatmulArgs &a, uint32_t format, cudaStream_t stream)
+template <int COUNT>
+__device__ __forceinline__ void store_column(const float (&v)[COUNT], uint32_t m, uint32_t n, const ProductArgs &a, float power_a, float power_b)
 {
-    const uint64_t tiles = qesgd_div_up(a.M, TILE) * qesgd_div_up(a.N, TILE);
-    return qesgd_launch(qesgd_fp4_matmul_kernel<T>, dim3((unsigned)(tiles < 0x7FFFFFFF ? tiles : 0x7FFFFFFF)), dim3(THREADS), stream, a, format == QESGD_FP4_MX);
+    if (n >= a.N || m >= a.M) return;
+    const uint64_t at = m * a.ldc + n;
+    if (a.dtype == QESGD_F32) store_column(v, static_cast<float *>(a.c) + at, m, a.M, a.ldc, a.accumulate, power_a, power_b);
+    else if (a.dtype == QESGD_BF16) store_column(v, static_cast<__nv_bfloat16 *>(a.c) + at, m, a.M, a.ldc, a.accumulate, power_a, power_b);
+    else store_column(v, static_cast<__half *>(a.c) + at, m, a.M, a.ldc, a.accumulate, power_a, power_b);
+}
+__device__ __forceinline__ float power_of(const int32_t *exponent)
+{
+    const int t = exponent ? min(max(__ldcg(exponent), -126), 126) : 0;
+    return __uint_as_float((uint32_t)(t + 127) << 23);
+}
+
+template <bool PAIR, bool MX>
+__global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const __grid_constant__ ProductArgs a, const __grid_constant__ CUtensorMap map_p,
+                                                                         const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_sp,
+                                                                         const __grid_constant__ CUtensorMap map_sq)
+{
+    using S = Shape<PAIR>;
+    constexpr uint32_t SCALE_TILES = MX ? 2 : 4;                     // tiles of scales along a stage
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    const uint32_t bars = base + S::STAGES * S::STAGE_BYTES;
+    const uint32_t full = bars, empty = bars + 8 * S::STAGES, done = empty + 8 * S::STAGES, free_ = done + 16, slot = free_ + 16;
+    volatile uint32_t *const stop = reinterpret_cast<volatile uint32_t *>(raw + (slot + 8 - smem_u32(raw)));
+    const uint32_t warp = threadIdx.x / 32u, lane = threadIdx.x % 32u;
+    const uint32_t share = PAIR ? 2u : a.split;                      // CTAs of a cluster
+    const uint32_t rank = share > 1 ? cluster_rank() : 0u;
+    const uint32_t group = blockIdx.x / share, groups = gridDim.x / share;
+    const uint32_t q_rows = PAIR ? S::MOST_Q : a.q;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::STAGES; ++s) {
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(full + 8 * s), "r"(1u) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(empty + 8 * s), "r"(1u) : "memory");
+        }
+        for (int s = 0; s < 2; ++s) {
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(done + 8 * s), "r"(1u) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(free_ + 8 * s), "r"(PAIR ? 16u : 8u) : "memory");
+        }
+        *stop = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        prefetch_map(&map_p);
+        prefetch_map(&map_q);
+        prefetch_map(&map_sp);
+        prefetch_map(&map_sq);
+    }
+    if (PAIR) cluster_sync_all();   // both CTAs of the pair are there
+    if (warp == 2) tmem_alloc<PAIR>(slot, S::COLUMNS);
+    fence_before_sync();
+    __syncthreads();
+    if (PAIR) cluster_sync_all();
+    fence_after_sync();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(raw + (slot - smem_u32(raw)));
+    // this CTA's part of the contraction (of a pair: all of it)
+    const uint32_t part = PAIR ? 0u : rank, parts = PAIR ? 1u : share;
+    const uint32_t first = (uint32_t)((uint64_t)a.steps * part / parts), steps = (uint32_t)((uint64_t)a.steps * (part + 1) / parts) - first;
+    qesgd_wait_for_previous();
+
+    if (warp == 0 && elect_one()) {
+        uint32_t n = 0;
+        const uint32_t full_lead = PAIR ? map_shared(full, 0) : full;
+        const uint32_t bytes = (LANES + (PAIR ? S::HELD_Q : q_rows)) * 128u + SCALE_TILES * SCALE_TILE * (1u + S::MOST_Q / 128u);
+        for (uint32_t t = group; t < a.tiles && !*stop; t += groups) {
+            const uint32_t p0 = t % a.tiles_n * (PAIR ? 256u : 128u) + (PAIR ? rank * 128u : 0u), q0 = t / a.tiles_n * q_rows;
+            for (uint32_t k = first; k < first + steps; ++k, ++n) {
+                const uint32_t s = n % S::STAGES, to = base + s * S::STAGE_BYTES, bar = full_lead + 8 * s;
+                if (n >= S::STAGES && !pipe_wait(empty + 8 * s, (n / S::STAGES - 1u) & 1u, stop)) break;
+                if (!PAIR || rank == 0)
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(full + 8 * s), "r"(bytes * (PAIR ? 2u : 1u)) : "memory");
+                tma_load_2d<PAIR>(to, &map_p, k * 128u, p0, bar);
+                tma_load_2d<PAIR>(to + LANES * 128, &map_q, k * 128u, q0 + (PAIR ? rank * 128u : 0u), bar);
+                const uint32_t scales = to + (LANES + S::HELD_Q) * 128;
+                // in units of 8 bytes
+                tma_load_2d<PAIR>(scales, &map_sp, k * SCALE_TILES * (SCALE_TILE / 8), p0 / 128u, bar);
+                tma_load_2d<PAIR>(scales + S::SCALES_P, &map_sq, k * SCALE_TILES * (SCALE_TILE / 8), q0 / 128u, bar);
+                if (PAIR) tma_load_2d<PAIR>(scales + S::SCALES_P + 2048, &map_sq, k * SCALE_TILES * (SCALE_TILE / 8), q0 / 128u + 1u, bar);
+            }
+        }
+        if (*stop) drain();
+    } else if (warp == 1 && (!PAIR || rank == 0) && elect_one()) {
+        // E2M1 operands, fp32 sums; scales E8M0 (MX) or E4M3
+        const uint32_t instruction = 1u << 7 | 1u << 10 | (q_rows / 8u) << 17 | (MX ? 1u << 23 : 0u) | (PAIR ? 2u : 1u) << 27;
+        uint32_t n = 0, done_tiles = 0;
+        for (uint32_t t = group; t < a.tiles && !*stop; t += groups, ++done_tiles) {
+            const uint32_t which = done_tiles % S::TILES, turn = done_tiles / S::TILES, sums = tmem + which * S::MOST_Q;
+            if (turn >= 1 && !pipe_wait(free_ + 8 * which, (turn - 1u) & 1u, stop)) break;
+            fence_after_sync();
+            bool ok = true;
+            for (uint32_t k = 0; k < steps; ++k, ++n) {
+                const uint32_t s = n % S::STAGES, from = base + s * S::STAGE_BYTES;
+                ok = pipe_wait(full + 8 * s, (n / S::STAGES) & 1u, stop);
+                if (!ok) break;
+                fence_after_sync();
+                // the set of scales was last read by the products of two stages ago
+                if (n >= 2) {
+                    ok = pipe_wait(empty + 8 * ((n - 2) % S::STAGES), ((n - 2) / S::STAGES) & 1u, stop);
+                    if (!ok) break;
+                }
+                const uint32_t scales = from + (LANES + S::HELD_Q) * 128, sp = tmem + S::SCALE_COLUMN + n % 2u * S::SET, sq = sp + 16u;
+                // rows 0..127 and 128..255 of A lie side by side for each tile of four blocks
+#pragma unroll
+                for (uint32_t i = 0; i < SCALE_TILES; ++i) {
+                    copy_scales<PAIR>(sp + 4 * i, scales + i * SCALE_TILE);
+                    copy_scales<PAIR>(sq + (PAIR ? 8 : 4) * i, scales + S::SCALES_P + i * SCALE_TILE);
+                    if (PAIR) copy_scales<PAIR>(sq + 8 * i + 4, scales + S::SCALES_P + 2048 + i * SCALE_TILE);
+                }
+#pragma unroll
+                for (uint32_t i = 0; i < DEPTH / 64; ++i) {
+                    const uint64_t p = swizzled_matrix(from + i * 32u, 16u, 1024u), q = swizzled_matrix(from + LANES * 128 + i * 32u, 16u, 1024u);
+                    const uint32_t at = MX ? i / 2 : i, half = MX ? i % 2 * 2 : 0u;   // MX: two products share a tile of scales
+                    mma_fp4<PAIR, MX>(sums, p, q, instruction | half << 4 | half << 29, sp + 4 * at, sq + (PAIR ? 8 : 4) * at, k > 0 || i > 0);
+                }
+                mma_commit<PAIR>(empty + 8 * s);
+            }
+            if (!ok) break;
+            mma_commit<PAIR>(done + 8 * which);
+        }
+        if (*stop) drain();
+    } else if (warp >= 4) {
+        const uint32_t quarter = warp % 4u, part_of = (warp - 4u) / 4u;
+        const uint32_t free_lead = PAIR ? map_shared(free_, 0) : free_;
+        const float power_a = power_of(a.a_exponent), power_b = power_of(a.b_exponent);
+        uint32_t done_tiles = 0;
+        for (uint32_t t = group; t < a.tiles; t += groups, ++done_tiles) {
+            const uint32_t which = done_tiles % S::TILES, turn = done_tiles / S::TILES;
+            const uint32_t n = t % a.tiles_n * (PAIR ? 256u : 128u) + (PAIR ? rank * 128u : 0u) + quarter * 32u + lane, m0 = t / a.tiles_n * q_rows;
+            if (!__all_sync(0xFFFFFFFFu, pipe_wait(done + 8 * which, turn & 1u, stop))) break;
+            fence_after_sync();
+            const uint32_t from = tmem + (quarter * 32u << 16) + which * S::MOST_Q;
+            float v[S::MOST_Q / 64][32];
+#pragma unroll
+            for (uint32_t i = 0; i < S::MOST_Q / 64; ++i)
+                if ((2 * i + part_of) * 32u < q_rows) tmem_load32(from + (2 * i + part_of) * 32u, v[i]);
+            tmem_wait_load();
+            fence_before_sync();
+            __syncwarp();
+            if (lane == 0) {
+                if (PAIR) mbar_arrive_cluster(free_lead + 8 * which);
+                else asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(free_ + 8 * which) : "memory");
+            }
+            if (parts == 1) {
+#pragma unroll
+                for (uint32_t i = 0; i < S::MOST_Q / 64; ++i)
+                    if ((2 * i + part_of) * 32u < q_rows) store_column(v[i], m0 + (2 * i + part_of) * 32u, n, a, power_a, power_b);
+            } else {
+                // all copies and products of this CTA are done: its part of the sums goes where the stages were
+                float *const mine = reinterpret_cast<float *>(raw + (base - smem_u32(raw)));
+#pragma unroll
+                for (uint32_t i = 0; i < S::MOST_Q / 64; ++i)
+                    if ((2 * i + part_of) * 32u < q_rows)
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) mine[((2 * i + part_of) * 32u + k) * LANES + quarter * 32u + lane] = steps ? v[i][k] : 0.0f;
+            }
+        }
+    }
+    __syncwarp();
+    if (!PAIR && parts > 1) {
+        cluster_sync_all();
+        if (!*stop) {
+            // every CTA adds up its share of the tile's columns, in the order of the contraction
+            const uint32_t t = group, n = t % a.tiles_n * 128u + threadIdx.x % LANES;
+            const float power_a = power_of(a.a_exponent), power_b = power_of(a.b_exponent);
+            for (uint32_t col = rank + parts * (threadIdx.x / LANES); col < q_rows; col += parts * (WARPS * 32 / LANES)) {
+                float sum[1] = {0.0f};
+                for (uint32_t r = 0; r < parts; ++r) {
+                    float v;
+                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(map_shared(base + (col * LANES + threadIdx.x % LANES) * 4u, r)) : "memory");
+                    sum[0] += v;
+                }
+                store_column(sum, t / a.tiles_n * q_rows + col, n, a, power_a, power_b);
+            }
+        }
+        cluster_sync_all();   // the others may still read this CTA's part
+    }
+    __syncthreads();
+    if (threadIdx.x == 0 && *stop) atomicOr(a.status, QESGD_STATUS_TIMEOUT);
+    fence_before_sync();
+    if (PAIR) cluster_sync_all();
+    fence_after_sync();
+    if (warp == 2) tmem_dealloc<PAIR>(tmem, S::COLUMNS);
+}
+
+// rows of `bytes` bytes; a box is 128 bytes of box_rows rows, swizzled
+bool codes_map(CUtensorMap *map, const uint8_t *p, uint64_t rows, uint64_t bytes, uint32_t box_rows)
+{
+    const cuuint64_t dims[2] = {bytes, rows}, strides[1] = {bytes};
+    const cuuint32_t box[2] = {128u, box_rows}, unit[2] = {1u, 1u};
+    return qesgd_encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2u, const_cast<uint8_t *>(p), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// the tiles of scales of 128 rows as one row of 8-byte elements; a box is what a stage wants of it
+bool scales_map(CUtensorMap *map, const uint8_t *p, uint64_t rows, uint64_t K, bool mx)
+{
+    const uint64_t tiles = qesgd_div_up(K, mx ? 128 : 64);
+    const cuuint64_t dims[2] = {tiles * (SCALE_TILE / 8), qesgd_div_up(rows, 128)}, strides[1] = {tiles * SCALE_TILE};
+    const cuuint32_t box[2] = {(mx ? 2u : 4u) * (SCALE_TILE / 8), 1u}, unit[2] = {1u, 1u};
+    return qesgd_encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT64, 2u, const_cast<uint8_t *>(p), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool PAIR, bool MX>
+int launch(const Fp4MatmulArgs &f, uint32_t dtype, uint32_t q, uint32_t split, int sm_count, cudaStream_t stream)
+{
+    using S = Shape<PAIR>;
+    const auto kernel = qesgd_fp4_matmul_kernel<PAIR, MX>;
+    const uint64_t row_bytes = qesgd_div_up(f.K, 32) * 16;
+    CUtensorMap p, qm, sp, sq;
+    if (!qesgd_encode_tiled() || !codes_map(&p, f.b_codes, f.N, row_bytes, 128) || !codes_map(&qm, f.a_codes, f.M, row_bytes, PAIR ? 128u : q) ||
+        !scales_map(&sp, f.b_scales, f.N, f.K, MX) || !scales_map(&sq, f.a_scales, f.M, f.K, MX))
+        return (int)cudaErrorInvalidValue;
+    ProductArgs a = {};
+    a.M = (uint32_t)f.M;
+    a.N = (uint32_t)f.N;
+    a.steps = (uint32_t)qesgd_div_up(f.K, DEPTH);
+    a.split = split;
+    a.q = q;
+    a.tiles_n = (uint32_t)qesgd_div_up(f.N, PAIR ? 256 : 128);
+    const uint64_t tiles = a.tiles_n * qesgd_div_up(f.M, q);
+    if (tiles > 0x7FFFFFFF) return (int)cudaErrorInvalidValue;
+    a.tiles = (uint32_t)tiles;
+    a.a_exponent = f.a_exponent;
+    a.b_exponent = f.b_exponent;
+    a.c = f.c;
+    a.ldc = f.ldc;
+    a.dtype = dtype;
+    a.accumulate = f.accumulate;
+    a.status = f.status;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+    if (e == cudaSuccess && split > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return (int)e;
+    const uint32_t most = (uint32_t)sm_count / (PAIR ? 2u : 1u), share = PAIR ? 2u : split;
+    const uint32_t groups = split > 1 || a.tiles < most ? a.tiles : most;   // a shared contraction: one tile for each cluster
+    return (int)qesgd_launch_cluster(kernel, dim3(groups * share), dim3(WARPS * 32), S::SMEM, share, stream, a, p, qm, sp, sq);
 }
 
 }  // namespace
 
-int qesgd_launch_fp4_matmul(const Fp4MatmulArgs &a, uint32_t dtype, uint32_t format, int, cudaStream_t stream, int *launched)
+int qesgd_launch_fp4_matmul(const Fp4MatmulArgs &a, uint32_t dtype, uint32_t format, int sm_count, cudaStream_t stream, int *launched)
 {
     *launched = 1;
-    switch (dtype) {
-        case QESGD_F32: return (int)launch<float>(a, format, stream);
-        case QESGD_BF16: return (int)launch<__nv_bfloat16>(a, format, stream);
-        default: return (int)launch<__half>(a, format, stream);
-    }
+    const bool mx = format == QESGD_FP4_MX;
+    const uint64_t pairs = qesgd_div_up(a.M, 256) * qesgd_div_up(a.N, 256);
+    if (pairs * 2 >= (uint64_t)sm_count)
+        return mx ? launch<true, true>(a, dtype, 256, 1, sm_count, stream) : launch<true, false>(a, dtype, 256, 1, sm_count, stream);
+    const uint32_t q = a.M <= 32 ? 32 : a.M <= 64 ? 64 : 128;
+    const uint64_t tiles = qesgd_div_up(a.M, q) * qesgd_div_up(a.N, 128), steps = qesgd_div_up(a.K, DEPTH);
+    uint32_t split = 1;
+    while (split < 16 && tiles * split * 2 <= (uint64_t)sm_count && steps >= split * 2) split *= 2;
+    return mx ? launch<false, true>(a, dtype, q, split, sm_count, stream) : launch<false, false>(a, dtype, q, split, sm_count, stream);
 }

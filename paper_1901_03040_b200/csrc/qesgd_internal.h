@@ -187,6 +187,7 @@ struct Fp4MatmulArgs {
     uint64_t M, N, K, ldc;
     void *c;
     uint32_t accumulate;
+    uint32_t *status;
 };
 struct OrthoArgs {
     const void *x;

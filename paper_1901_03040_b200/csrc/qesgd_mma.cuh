@@ -91,6 +91,18 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map
                      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
                      : "memory");
 }
+template <bool PAIR>
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, uint32_t x, uint32_t y, uint32_t bar)
+{
+    if (PAIR)
+        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+                     "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
+                     : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+                     "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
+                     : "memory");
+}
 __device__ __forceinline__ void prefetch_map(const CUtensorMap *map)
 {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
@@ -152,6 +164,30 @@ __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint
         asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b),
                      "r"(instruction), "r"((uint32_t)add)
                      : "memory");
+}
+// E2M1 operands with a scale for each 32 elements (powers of two: 2 of them for a product's contraction of 64) or each 16
+// (E4M3: 4), scales in tensor memory
+template <bool PAIR, bool MX>
+__device__ __forceinline__ void mma_fp4(uint32_t d, uint64_t a, uint64_t b, uint32_t instruction, uint32_t scales_a, uint32_t scales_b, bool add)
+{
+#define QESGD_MMA_FP4(GROUP, KIND)                                                                                                              \
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %6, 0;\ntcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d), \
+                 "l"(a), "l"(b), "r"(instruction), "r"(scales_a), "r"(scales_b), "r"((uint32_t)add)                                               \
+                 : "memory")
+    if (PAIR && MX) QESGD_MMA_FP4("2", "mxf4.block_scale.scale_vec::2X");
+    else if (PAIR) QESGD_MMA_FP4("2", "mxf4nvf4.block_scale.scale_vec::4X");
+    else if (MX) QESGD_MMA_FP4("1", "mxf4.block_scale.scale_vec::2X");
+    else QESGD_MMA_FP4("1", "mxf4nvf4.block_scale.scale_vec::4X");
+#undef QESGD_MMA_FP4
+}
+// A tile of scales (128 rows by 4 blocks, 512 bytes: 32 lines of 16) from shared memory into 4 columns of tensor memory,
+// once for each of its four quarters; with PAIR in both CTAs, each from its own shared memory.  In order with the products.
+template <bool PAIR>
+__device__ __forceinline__ void copy_scales(uint32_t to, uint32_t from)
+{
+    const uint64_t lines = (uint64_t)((from & 0x3FFFFu) >> 4) | (uint64_t)(128 >> 4) << 32 | 1ull << 46;
+    if (PAIR) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(lines) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(lines) : "memory");
 }
 // One arrival on the barrier (with PAIR: on that of both CTAs) when all products so far are done.
 template <bool PAIR>

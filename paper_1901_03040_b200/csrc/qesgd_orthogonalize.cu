@@ -329,11 +329,10 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
         const uint32_t quarter = warp % 4u;
         const uint32_t free_lead = PAIR ? map_shared(free_, 0) : free_;
         uint32_t done_tiles = 0;
-        for (uint32_t t = group; t < all && !*stop; t += groups, ++done_tiles) {
+        for (uint32_t t = group; t < all; t += groups, ++done_tiles) {
             const Tile x = tile_of<MODE>(t, a);
             const uint32_t half = done_tiles & 1u;
-            if (!pipe_wait(done + 8 * half, (done_tiles / 2) & 1u, stop)) break;
-            __syncwarp();
+            if (!__all_sync(FULL, pipe_wait(done + 8 * half, (done_tiles / 2) & 1u, stop))) break;
             fence_after_sync();
             const uint32_t row = x.i * S::SIDE + rank * 128u + quarter * 32u + lane;
             for (uint32_t c = 0; c < S::SIDE; c += 32) {

@@ -245,6 +245,41 @@ def test_product_of_exact_sums(fmt, M, N, K):
     assert G.ctx().qesgd_status() == 0
 
 
+@pytest.mark.parametrize("M,N,K", [(2100, 2400, 300), (2304, 2500, 3000), (9000, 520, 65)])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_product_of_many_tiles(fmt, M, N, K):
+    """Enough tiles that pairs of SMs share them: exact sums, as above."""
+    a, ca, sa = _operand(M, K, fmt, 5, True)
+    b, cb, sb = _operand(N, K, fmt, 6, True)
+    want = torch.from_numpy(a @ b.T)
+    for dtype, pad, acc in ((qesgd.F32, 1, 1), (qesgd.BF16, 0, 0)):
+        c = torch.randint(-8, 9, (M, N + pad), generator=torch.Generator().manual_seed(N)).to(DTYPE[dtype]).cuda()
+        before = c.clone()
+        G.ctx().qesgd_fp4_matmul(ca, sa, None, cb, sb, None, M, N, K, fmt, c, dtype, N + pad, acc)
+        torch.cuda.synchronize()
+        full = want + (before[:, :N].cpu().double() if acc else 0.0)
+        assert torch.equal(c[:, :N].cpu(), full.to(DTYPE[dtype])), (dtype, pad, acc)
+        assert torch.equal(c[:, N:], before[:, N:])
+    assert G.ctx().qesgd_status() == 0
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 2500, 20000), (64, 1000, 65536), (40, 130, 40000), (150, 700, 30001)])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_product_of_a_long_contraction(fmt, M, N, K):
+    """Values up to 1.5 and scales of one: sums are multiples of 1/4 below 2.25 * 65536 < 2^18, exact in any order."""
+    g = np.random.default_rng(K)
+    held = []
+    for rows in (M, N):
+        codes = g.integers(0, 4, (rows, K), dtype=np.uint8) + 8 * g.integers(0, 2, (rows, K), dtype=np.uint8)
+        byte = np.full((rows, -(-K // ref.BLOCK[fmt])), 127 if fmt == qesgd.FP4_MX else 0x38, dtype=np.uint8)
+        held.append((ref.values(codes, byte, fmt), G.dev(ref.pack(codes)), G.dev(ref.tiles(byte))))
+    (a, ca, sa), (b, cb, sb) = held
+    c = torch.empty((M, N), device="cuda")
+    G.ctx().qesgd_fp4_matmul(ca, sa, None, cb, sb, None, M, N, K, fmt, c, qesgd.F32, N, 0)
+    assert torch.equal(c.cpu().double(), torch.from_numpy(a @ b.T))
+    assert G.ctx().qesgd_status() == 0
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 200, 3000), (33, 333, 1111), (300, 400, 2000)])
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_product_of_any_scales(fmt, M, N, K):
