@@ -5,7 +5,9 @@
 // whatever C's alignment, and a single token fills the lanes with the weight's rows.
 //
 // A stage is a contraction of 256: 128 bytes of codes of each row, and the tiles of scales as they lie in memory (128 rows by 4
-// blocks, 512 bytes), which go on to tensor memory in the same order.  What lies outside the matrices arrives as zeros.
+// blocks, 512 bytes), which go on to tensor memory in the same order.  Every stage has columns of its own for its scales, so
+// that the thread that issues products need not wait for earlier ones before it copies scales (with two sets in turn, and
+// that wait, 8192^3 took 224 us instead of 202).  What lies outside the matrices arrives as zeros.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -30,8 +32,9 @@ struct Shape {
     static constexpr uint32_t STAGE_BYTES = LANES * 128 + HELD_Q * 128 + SCALES_P + SCALES_Q;
     static constexpr uint32_t SMEM = STAGES * STAGE_BYTES + 1024 + 256;
     static constexpr uint32_t COLUMNS = 512;
-    static constexpr uint32_t SCALE_COLUMN = TILES * MOST_Q;  // two sets of scales behind the tiles
+    static constexpr uint32_t SCALE_COLUMN = TILES * MOST_Q;  // a set of scales for each stage behind the tiles
     static constexpr uint32_t SET = 16 + MOST_Q / 128 * 16;
+    static_assert(SCALE_COLUMN + STAGES * SET <= COLUMNS, "tensor memory");
 };
 
 struct ProductArgs {
@@ -170,12 +173,7 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const _
                 ok = pipe_wait(full + 8 * s, (n / S::STAGES) & 1u, stop);
                 if (!ok) break;
                 fence_after_sync();
-                // the set of scales was last read by the products of two stages ago
-                if (n >= 2) {
-                    ok = pipe_wait(empty + 8 * ((n - 2) % S::STAGES), ((n - 2) / S::STAGES) & 1u, stop);
-                    if (!ok) break;
-                }
-                const uint32_t scales = from + (LANES + S::HELD_Q) * 128, sp = tmem + S::SCALE_COLUMN + n % 2u * S::SET, sq = sp + 16u;
+                const uint32_t scales = from + (LANES + S::HELD_Q) * 128, sp = tmem + S::SCALE_COLUMN + s * S::SET, sq = sp + 16u;
                 // rows 0..127 and 128..255 of A lie side by side for each tile of four blocks
 #pragma unroll
                 for (uint32_t i = 0; i < SCALE_TILES; ++i) {
