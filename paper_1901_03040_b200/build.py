@@ -68,7 +68,8 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     headers = [os.path.join(CSRC, "qesgd_internal.h"), os.path.join(CSRC, "qesgd_lr_device.cuh"),
                os.path.join(CSRC, "qesgd_lr_tile.h"),
                os.path.join(CSRC, "qesgd_orthogonalize.h"),
-               os.path.join(CSRC, "qesgd_device.cuh"), os.path.join(CSRC, "qesgd_mma.cuh"), os.path.join(ROOT, "include", "qesgd.h"),
+               os.path.join(CSRC, "qesgd_device.cuh"), os.path.join(CSRC, "qesgd_mma.cuh"),
+               os.path.join(CSRC, "qesgd_matrix.cuh"), os.path.join(ROOT, "include", "qesgd.h"),
                os.path.abspath(__file__)]
     nvcc = _nvcc()
     objs = []

@@ -8,9 +8,7 @@
 // blocks, 512 bytes), which go on to tensor memory in the same order.  Every stage has columns of its own for its scales, so
 // that the thread that issues products need not wait for earlier ones before it copies scales (with two sets in turn, and
 // that wait, 8192^3 took 224 us instead of 202).  What lies outside the matrices arrives as zeros.
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
+#include "qesgd_matrix.cuh"
 #include "qesgd_mma.cuh"
 
 namespace {
@@ -47,18 +45,6 @@ struct ProductArgs {
     uint32_t dtype, accumulate;
     uint32_t *status;
 };
-
-__device__ __forceinline__ float to_float(float v) { return v; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
-template <typename T>
-__device__ __forceinline__ T from_float(float v);
-template <>
-__device__ __forceinline__ float from_float<float>(float v) { return v; }
-template <>
-__device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
-template <>
-__device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 
 // Column n of `count` rows of C from row m on.
 template <typename T, int COUNT>

@@ -1,7 +1,5 @@
 // Newton-Schulz orthogonalisation of a batch of matrices (definition in include/qesgd.h).
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
+#include "qesgd_matrix.cuh"
 #include "qesgd_mma.cuh"
 #include "qesgd_orthogonalize.h"
 
@@ -10,68 +8,116 @@ namespace {
 constexpr int THREADS = 256;
 constexpr uint32_t FULL = 0xFFFFFFFFu;
 
-__device__ __forceinline__ float to_float(float v) { return v; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
-
-// Sum of the squares of a part of a matrix, in 64 bits: no 32-bit value's square is out of range, and the sum is the
-// same in every run.
-template <typename T>
-__global__ __launch_bounds__(THREADS) void qesgd_ortho_norm_kernel(const T *x, uint64_t rows, uint64_t cols, uint64_t ldx, uint64_t stride,
-                                                                   double *parts)
+// Sum over a block; every thread calls it, thread 0 has the sum.  The order of the additions is fixed.
+__device__ __forceinline__ double block_sum(double sum)
 {
     __shared__ double sums[THREADS / 32];
-    qesgd_wait_for_previous();
-    const T *const m = x + blockIdx.y * stride;
-    const uint64_t per = (rows * cols + gridDim.x - 1) / gridDim.x;
-    const uint64_t last = min(rows * cols, per * (blockIdx.x + 1));
-    double sum = 0.0;
-    for (uint64_t i = per * blockIdx.x + threadIdx.x; i < last; i += THREADS) {
-        const double v = to_float(m[i / cols * ldx + i % cols]);
-        sum = fma(v, v, sum);
-    }
     for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(FULL, sum, o);
     if (threadIdx.x % 32 == 0) sums[threadIdx.x / 32] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0)
         for (int i = 1; i < THREADS / 32; ++i) sum += sums[i];
-        parts[blockIdx.y * gridDim.x + blockIdx.x] = sum;
-    }
+    return sum;
 }
 
-__device__ __forceinline__ __half to_half(float v) { return __float2half_rn(fminf(fmaxf(v, -65504.0f), 65504.0f)); }
-
-// X = G / ||G||, with fewer rows than columns, in two terms.
+// Sum of the squares of a part of a matrix, in 64 bits: no 32-bit value's square is out of range.
 template <typename T>
-__global__ __launch_bounds__(THREADS) void qesgd_ortho_start_kernel(const T *x, uint64_t rows, uint64_t cols, uint64_t ldx, uint64_t stride,
+__global__ __launch_bounds__(THREADS) void qesgd_ortho_norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ldx, uint64_t stride, bool vec,
+                                                                   double *parts)
+{
+    qesgd_wait_for_previous();
+    const T *const m = x + blockIdx.y * stride;
+    const uint32_t octets = (cols + 7) / 8, all = octets * rows;
+    double sum = 0.0;
+    for (uint32_t n = blockIdx.x * THREADS + threadIdx.x; n < all; n += gridDim.x * THREADS) {
+        float v[8];
+        load_octet(m + n / octets * ldx, n % octets * 8, cols, vec, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum = fma((double)v[j], (double)v[j], sum);
+    }
+    sum = block_sum(sum);
+    if (threadIdx.x == 0) parts[blockIdx.y * gridDim.x + blockIdx.x] = sum;
+}
+
+__device__ __forceinline__ __half2 to_halves(float a, float b)
+{
+    const __half2 most = __float2half2_rn(65504.0f);
+    return __hmax2(__hmin2(__floats2half2_rn(a, b), most), __hneg2(most));
+}
+__device__ __forceinline__ uint32_t half_pair(float a, float b)
+{
+    const __half2 h = to_halves(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ void store_terms(const float (&f)[8], __half *hi, __half *lo)
+{
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        h[k] = half_pair(f[2 * k], f[2 * k + 1]);
+        const float2 kept = __half22float2(*reinterpret_cast<const __half2 *>(&h[k]));
+        l[k] = half_pair((f[2 * k] - kept.x) * ORTHO_LO_SCALE, (f[2 * k + 1] - kept.y) * ORTHO_LO_SCALE);
+    }
+    *reinterpret_cast<uint4 *>(hi) = make_uint4(h[0], h[1], h[2], h[3]);
+    *reinterpret_cast<uint4 *>(lo) = make_uint4(l[0], l[1], l[2], l[3]);
+}
+
+// X = G / ||G|| in two terms, turned where G has more rows than columns.  Zeros behind the last column, up to the next octet.
+template <typename T, bool TURNED>
+__global__ __launch_bounds__(THREADS) void qesgd_ortho_start_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ldx, uint64_t stride, bool vec,
                                                                     const double *parts, uint32_t nparts, OrthoView v, uint32_t *status)
 {
     __shared__ double inverse;
+    __shared__ float held[TURNED ? 64 * 65 : 1];
     qesgd_wait_for_previous();
+    double sum = 0.0;
+    for (uint32_t i = threadIdx.x; i < nparts; i += THREADS) sum += parts[blockIdx.y * nparts + i];
+    sum = block_sum(sum);
     if (threadIdx.x == 0) {
-        double sum = 0.0;
-        for (uint32_t i = 0; i < nparts; ++i) sum += parts[blockIdx.y * nparts + i];
         const bool fine = sum <= 1.7976931348623157e308;
         if (!fine && blockIdx.x == 0) atomicOr(status, QESGD_STATUS_NONFINITE);
-        inverse = fine && sum > 0.0 ? 1.0 / sqrt(sum) : 0.0;
+        inverse = fine && sum > 0.0 ? (double)ORTHO_X_SCALE / sqrt(sum) : 0.0;
     }
     __syncthreads();
     const double inv = inverse;
     const T *const m = x + blockIdx.y * stride;
     __half *const hi = v.hi + blockIdx.y * v.x_stride, *const lo = v.lo + blockIdx.y * v.x_stride;
-    for (uint64_t i = (uint64_t)blockIdx.x * THREADS + threadIdx.x; i < rows * cols; i += (uint64_t)gridDim.x * THREADS) {
-        const uint64_t r = i / cols, c = i % cols;
-        const float f = inv == 0.0 ? 0.0f : (float)((double)to_float(m[r * ldx + c]) * inv) * ORTHO_X_SCALE;
-        const uint64_t at = rows <= cols ? r * v.ld + c : c * v.ld + r;
-        hi[at] = to_half(f);
-        lo[at] = to_half((f - __half2float(hi[at])) * ORTHO_LO_SCALE);
+    if (!TURNED) {
+        const uint32_t octets = (cols + 7) / 8, all = octets * rows;
+        for (uint32_t n = blockIdx.x * THREADS + threadIdx.x; n < all; n += gridDim.x * THREADS) {
+            const uint32_t r = n / octets, c = n % octets * 8;
+            float f[8];
+            load_octet(m + r * ldx, c, cols, vec, f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = inv == 0.0 ? 0.0f : (float)((double)f[j] * inv);
+            store_terms(f, hi + r * v.ld + c, lo + r * v.ld + c);
+        }
+        return;
+    }
+    const uint32_t across = (cols + 63) / 64, tiles = (rows + 63) / 64 * across;
+    for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+        const uint32_t r0 = t / across * 64, c0 = t % across * 64;
+        for (uint32_t i = threadIdx.x; i < 64 * 64; i += THREADS) {
+            const uint32_t r = r0 + i / 64, c = c0 + i % 64;
+            const float g = r < rows && c < cols ? to_float(m[r * ldx + c]) : 0.0f;
+            held[i / 64 * 65 + i % 64] = inv == 0.0 ? 0.0f : (float)((double)g * inv);
+        }
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < 64 * 8; i += THREADS) {
+            const uint32_t c = c0 + i / 8, r = r0 + i % 8 * 8;
+            if (c < cols && r < v.ld) {
+                float f[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] = held[(i % 8 * 8 + j) * 65 + i / 8];
+                store_terms(f, hi + c * v.ld + r, lo + c * v.ld + r);
+            }
+        }
+        __syncthreads();
     }
 }
 
 // ------------------------------------------------------------- products ----
-// The three products of a step, C = P Q with fp32 sums in tensor memory, by persistent CTAs (or pairs of them) of
-// 8 warps: one fills a ring of stages by tiled copies, one thread issues the products, four warps take finished tiles
-// out of tensor memory, where the next tile is summed meanwhile.
+// The three products of a step, C = P Q with fp32 sums in tensor memory, by persistent CTAs (or pairs of them):
 //   GRAM    A = X X^T: both operands are rows of X.  What is off the diagonal goes to F (fp16), the diagonal to d (fp32).
 //   POLY    B = b A + c A A = b (D + F) + c (F F + D F + F D + D D): the product is F F, both operands rows of F (F = F^T).
 //   UPDATE  X' = a X + B X: rows of B's part off the diagonal, and X with the contraction across its rows.
@@ -79,25 +125,36 @@ __global__ __launch_bounds__(THREADS) void qesgd_ortho_start_kernel(const T *x, 
 // diagonal, and rounding that to fp16 moves all singular values of a row alike (20 x 2000: 2.4e-3 off instead of 1.0e-3,
 // before the result's own rounding).  A and B are symmetric: tiles below the diagonal are not computed, the ones above
 // are stored twice.
+//
+// A CTA's warps: 0 fills a ring of stages with operands by tiled copies; one thread of 1 issues the products; 4 to 7 take
+// finished tiles out of tensor memory, where the next tile is summed meanwhile, 64 columns at a time.  What a tile's end
+// reads (X in two terms, or F) and what it writes pass through a second ring of 128 x 64 boxes: 2 has them filled by tiled
+// copies, the four warps replace each element by its result, 3 has them stored by tiled copies.  (With loads and stores by
+// the four warps, a row for each lane, the update of 12 x 512 x 2048 took 63 us, three times what its products take: 32
+// rows' segments in one instruction are 32 passes through the load-store unit.)
 enum Product { GRAM, POLY, UPDATE };
 
-constexpr int WARPS = 8;
+constexpr int TAKERS = 16;                    // warps that take tiles out: four for each quarter of tensor memory
+constexpr int WARPS = 4 + TAKERS;
 constexpr int DEPTH = 64;                     // contraction of a stage: 128 bytes of fp16
-constexpr uint32_t OPERAND_BYTES = 128 * 128; // 128 rows (or columns) of a stage
+constexpr uint32_t OPERAND_BYTES = 128 * 128; // 128 rows (or columns) of a stage; also a box of the second ring
+constexpr uint32_t BOX_COLS = 64;
 
 struct ProductArgs {
     uint32_t rows, cols, depth, batch;
     uint32_t tiles_m, tiles_n, tiles;         // tiles of one matrix
-    __half *f;                                // GRAM: out, POLY: in
-    __half *b;                                // POLY: out
+    __half *mirror;                           // GRAM: F, POLY: B, for the elements below the diagonal
     float *d, *db;                            // diagonals of A and of B
-    const __half *hi, *lo;                    // UPDATE: X; lo may be null
-    __half *hi_out, *lo_out;                  // UPDATE: X', lo_out may be null
+    uint32_t lo_in, lo_out;                   // UPDATE: whether X and X' have a second term
     __nv_bfloat16 *out;                       // UPDATE: the result, of the last step; else null
-    uint64_t ld_x, x_stride, ld_a, a_stride, d_stride, ldo, out_stride;
-    uint32_t turned, out_vec;
+    uint64_t ld_a, a_stride, d_stride, ldo, out_stride;
+    uint32_t turned, out_tiled;                // out_tiled: by tiled copies
     float ca, cb, cc;
     uint32_t *status;
+};
+// P and Q; what the end of a tile reads (F, or X and its second term) and writes
+struct ProductMaps {
+    CUtensorMap p, q, in, in_lo, out, out_lo;
 };
 
 struct Tile {
@@ -120,152 +177,195 @@ __device__ __forceinline__ Tile tile_of(uint32_t t, const ProductArgs &a)
     return x;
 }
 
-__device__ __forceinline__ uint32_t half_pair(float a, float b)
+__device__ __forceinline__ uint4 load_shared(uint32_t addr)
 {
-    const __half2 h = __halves2half2(to_half(a), to_half(b));
-    return *reinterpret_cast<const uint32_t *>(&h);
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+    return v;
 }
-// 32 values of a row from column c on; rows are `ld` long, a multiple of 8, and may be written up to there
-__device__ __forceinline__ void store_halves(__half *row, uint32_t c, uint64_t ld, const float (&v)[32])
+__device__ __forceinline__ void store_shared(uint32_t addr, uint4 v)
+{
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w));
+}
+// Octet `o` (16 bytes) of row r of a box, as the tiled copies lay it: swizzled over 8 rows.
+__device__ __forceinline__ uint32_t box_octet(uint32_t box, uint32_t r, uint32_t o) { return box + r * 128u + ((o ^ (r & 7u)) << 4); }
+template <int N>
+__device__ __forceinline__ void halves(const uint4 (&w)[N], float (&v)[8 * N])
 {
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
-        if (c + 8u * g < ld)
-            *reinterpret_cast<uint4 *>(row + c + 8 * g) = make_uint4(half_pair(v[8 * g], v[8 * g + 1]), half_pair(v[8 * g + 2], v[8 * g + 3]),
-                                                                     half_pair(v[8 * g + 4], v[8 * g + 5]), half_pair(v[8 * g + 6], v[8 * g + 7]));
+    for (int i = 0; i < N; ++i) {
+        const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&u[k]));
+            v[8 * i + 2 * k] = f.x;
+            v[8 * i + 2 * k + 1] = f.y;
+        }
+    }
 }
 
-// One row's 32 sums from column c on.
+constexpr int TAKEN = 64 / (TAKERS / 4);   // columns of a box that a warp takes
+constexpr int OCTETS = TAKEN / 8;
+
+// TAKEN neighbouring sums of row `row` (row r of the CTA's boxes) from column c on (octet o of the box) -> what is kept of
+// them, in the box at `box` (and a second term in the box behind it).  `linear`: the row's element of D (POLY), a and the
+// row's element of B's diagonal (UPDATE); `across`: D from column c on, in shared memory.
 template <int MODE>
-__device__ __forceinline__ void finish(float (&v)[32], uint32_t batch, uint32_t row, uint32_t c, bool mirror, const ProductArgs &a)
+__device__ __forceinline__ void finish(float (&v)[TAKEN], uint32_t batch, uint32_t row, uint32_t c, uint32_t box, uint32_t r, uint32_t o, float linear,
+                                       uint32_t across, bool mirror, const ProductArgs &a)
 {
     constexpr float XS = ORTHO_X_SCALE, AS = ORTHO_A_SCALE, BS = ORTHO_B_SCALE;
-    if (row >= a.rows || c >= a.cols) return;
+    const bool diagonal = MODE != UPDATE && row - c < (uint32_t)TAKEN;
+    float in[TAKEN];
+    if (MODE != GRAM) {
+        uint4 w[OCTETS];
+#pragma unroll
+        for (int i = 0; i < OCTETS; ++i) w[i] = load_shared(box_octet(box, r, o + i));
+        halves(w, in);
+    }
     if (MODE == GRAM) {
 #pragma unroll
-        for (int k = 0; k < 32; ++k) {
-            if (c + k == row) {
-                a.d[batch * a.d_stride + row] = v[k] * (1.0f / (XS * XS));
+        for (int k = 0; k < TAKEN; ++k) {
+            if (diagonal && c + k == row) {
+                if (row < a.rows) a.d[batch * a.d_stride + row] = v[k] * (1.0f / (XS * XS));
                 v[k] = 0.0f;
             }
             v[k] *= AS / (XS * XS);
         }
     }
     if (MODE == POLY) {
-        const float *const d = a.d + batch * a.d_stride;
-        const float di = __ldcg(d + row);
-        const __half *const f = a.f + batch * a.a_stride + row * a.ld_a;
+        const float s2 = a.cc * BS / (AS * AS), s1 = a.cc * BS / AS, s0 = a.cb * BS / AS + s1 * linear;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            if (c + 8u * g >= a.ld_a) break;
-            const uint4 w = __ldcg(reinterpret_cast<const uint4 *>(f + c) + g);
-            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+        for (int i = 0; i < TAKEN / 4; ++i) {
+            const uint4 w = load_shared(across + i * 16);
+            const float d[4] = {__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)};
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float2 p = __half22float2(*reinterpret_cast<const __half2 *>(&u[k / 2]));
-                const float fk = (k % 2 ? p.y : p.x) * (1.0f / AS), s = v[8 * g + k] * (1.0f / (AS * AS));
-                const uint32_t col = c + 8 * g + k;
-                if (col == row) a.db[batch * a.d_stride + row] = a.cb * di + a.cc * (s + di * di);
-                v[8 * g + k] = col == row ? 0.0f : BS * (a.cc * (s + (di + __ldcg(d + col)) * fk) + a.cb * fk);
-            }
-        }
-    }
-    if (MODE == GRAM || MODE == POLY) {
-        __half *const m = (MODE == GRAM ? a.f : a.b) + batch * a.a_stride;
-        store_halves(m + row * a.ld_a, c, a.ld_a, v);
-        if (mirror)
-#pragma unroll
-            for (int k = 0; k < 32; ++k)
-                if (c + k < a.cols) m[(c + k) * a.ld_a + row] = to_half(v[k]);
-        return;
-    }
-    const float linear = (a.ca + __ldcg(a.db + batch * a.d_stride + row)) * (1.0f / XS);
-    const uint64_t at = batch * a.x_stride + row * a.ld_x + c;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-        if (c + 8u * g >= a.ld_x) break;
-        const uint4 w = __ldcg(reinterpret_cast<const uint4 *>(a.hi + at) + g);
-        const uint4 z = a.lo ? __ldcg(reinterpret_cast<const uint4 *>(a.lo + at) + g) : make_uint4(0u, 0u, 0u, 0u);
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w}, l[4] = {z.x, z.y, z.z, z.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float2 p = __half22float2(*reinterpret_cast<const __half2 *>(&u[k])), q = __half22float2(*reinterpret_cast<const __half2 *>(&l[k]));
-            float &v0 = v[8 * g + 2 * k], &v1 = v[8 * g + 2 * k + 1];
-            v0 = linear * (p.x + q.x * (1.0f / ORTHO_LO_SCALE)) + v0 * (1.0f / (BS * XS));
-            v1 = linear * (p.y + q.y * (1.0f / ORTHO_LO_SCALE)) + v1 * (1.0f / (BS * XS));
-        }
-    }
-    if (a.out) {
-        __nv_bfloat16 *const o = a.out + batch * a.out_stride;
-        if (a.turned) {
-#pragma unroll
-            for (int k = 0; k < 32; ++k)
-                if (c + k < a.cols) o[(c + k) * a.ldo + row] = __float2bfloat16_rn(v[k]);
-        } else {
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                __nv_bfloat16 h[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) h[k] = __float2bfloat16_rn(v[8 * g + k]);
-                const uint32_t first = c + 8 * g;
-                if (a.out_vec && first + 8 <= a.cols) {
-                    *reinterpret_cast<uint4 *>(o + row * a.ldo + first) = *reinterpret_cast<const uint4 *>(h);
+            for (int j = 0; j < 4; ++j) {
+                const int k = 4 * i + j;
+                if (diagonal && c + k == row) {
+                    if (row < a.rows) a.db[batch * a.d_stride + row] = a.cb * linear + a.cc * (v[k] * (1.0f / (AS * AS)) + linear * linear);
+                    v[k] = 0.0f;
                 } else {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        if (first + k < a.cols) o[row * a.ldo + first + k] = h[k];
+                    v[k] = s2 * v[k] + (s0 + s1 * d[j]) * in[k];
                 }
             }
         }
-        return;
     }
-    float rest[32];
+    if (MODE == UPDATE) {
+        if (a.lo_in) {
+            uint4 w[OCTETS];
+            float rest[TAKEN];
 #pragma unroll
-    for (int k = 0; k < 32; ++k) {
-        v[k] *= XS;
-        rest[k] = (v[k] - __half2float(to_half(v[k]))) * ORTHO_LO_SCALE;
+            for (int i = 0; i < OCTETS; ++i) w[i] = load_shared(box_octet(box + OPERAND_BYTES, r, o + i));
+            halves(w, rest);
+#pragma unroll
+            for (int k = 0; k < TAKEN; ++k) in[k] += rest[k] * (1.0f / ORTHO_LO_SCALE);
+        }
+#pragma unroll
+        for (int k = 0; k < TAKEN; ++k) v[k] = linear * in[k] + v[k] * (1.0f / BS);   // times XS, as X is kept
+        if (a.out) {
+            __nv_bfloat162 h[TAKEN / 2];
+#pragma unroll
+            for (int k = 0; k < TAKEN / 2; ++k) h[k] = __floats2bfloat162_rn(v[2 * k] * (1.0f / XS), v[2 * k + 1] * (1.0f / XS));
+            if (a.turned) {
+                __nv_bfloat16 *to = a.out + batch * a.out_stride + c * a.ldo + row;
+                if (row < a.rows)
+#pragma unroll
+                    for (int k = 0; k < TAKEN; ++k, to += a.ldo)
+                        if (c + k < a.cols) *to = k % 2 ? h[k / 2].y : h[k / 2].x;
+            } else {
+                const uint32_t *const w = reinterpret_cast<const uint32_t *>(h);
+#pragma unroll
+                for (int i = 0; i < OCTETS; ++i) store_shared(box_octet(box, r, o + i), make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+            }
+            return;
+        }
     }
-    store_halves(a.hi_out + batch * a.x_stride + row * a.ld_x, c, a.ld_x, v);
-    if (a.lo_out) store_halves(a.lo_out + batch * a.x_stride + row * a.ld_x, c, a.ld_x, rest);
+    __half2 h[TAKEN / 2];
+#pragma unroll
+    for (int k = 0; k < TAKEN / 2; ++k) h[k] = to_halves(v[2 * k], v[2 * k + 1]);
+    const uint32_t *const w = reinterpret_cast<const uint32_t *>(h);
+#pragma unroll
+    for (int i = 0; i < OCTETS; ++i) store_shared(box_octet(box, r, o + i), make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+    if (MODE == UPDATE && a.lo_out) {
+        __half2 l[TAKEN / 2];
+#pragma unroll
+        for (int k = 0; k < TAKEN / 2; ++k) {
+            const float2 f = __half22float2(h[k]);
+            l[k] = to_halves((v[2 * k] - f.x) * ORTHO_LO_SCALE, (v[2 * k + 1] - f.y) * ORTHO_LO_SCALE);
+        }
+        const uint32_t *const z = reinterpret_cast<const uint32_t *>(l);
+#pragma unroll
+        for (int i = 0; i < OCTETS; ++i)
+            store_shared(box_octet(box + OPERAND_BYTES, r, o + i), make_uint4(z[4 * i], z[4 * i + 1], z[4 * i + 2], z[4 * i + 3]));
+    }
+    if (MODE != UPDATE && mirror && row < a.rows) {
+        __half *to = a.mirror + batch * a.a_stride + c * a.ld_a + row;
+#pragma unroll
+        for (int k = 0; k < TAKEN; ++k, to += a.ld_a)
+            if (c + k < a.cols) *to = k % 2 ? __high2half(h[k / 2]) : __low2half(h[k / 2]);
+    }
 }
 
-template <bool PAIR>
-struct Shape {
-    static constexpr int SIDE = PAIR ? 256 : 128;            // a tile is square
-    static constexpr int STAGES = 6;
-    static constexpr uint32_t STAGE_BYTES = 2 * OPERAND_BYTES;   // of one CTA: 128 rows of either operand
-    static constexpr uint32_t COLUMNS = 2 * SIDE;            // of tensor memory: two tiles
-    static constexpr uint32_t SMEM = STAGES * STAGE_BYTES + 1024 + 256;
-};
+// 128 rows from a box of results to rows of `out` that no tiled copy takes, by all threads that take tiles out.
+__device__ __forceinline__ void store_rows(uint32_t batch, uint32_t row0, uint32_t c, uint32_t box, uint32_t thread, const ProductArgs &a)
+{
+    for (uint32_t i = thread; i < 128 * BOX_COLS; i += TAKERS * 32) {
+        const uint32_t r = i / BOX_COLS, col = i % BOX_COLS;
+        uint16_t h;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(box_octet(box, r, col / 8u) + col % 8u * 2u));
+        if (row0 + r < a.rows && c + col < a.cols)
+            a.out[batch * a.out_stride + (row0 + r) * a.ldo + c + col] = *reinterpret_cast<const __nv_bfloat16 *>(&h);
+    }
+}
 
 template <int MODE, bool PAIR>
-__global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(const __grid_constant__ ProductArgs a, const __grid_constant__ CUtensorMap map_p,
-                                                                            const __grid_constant__ CUtensorMap map_q)
+struct Shape {
+    static constexpr uint32_t SIDE = PAIR ? 256 : 128;       // a tile is square
+    static constexpr int STAGES = MODE == UPDATE ? 4 : 5;
+    static constexpr int SLOTS = 3;                          // of the second ring
+    static constexpr uint32_t STAGE_BYTES = 2 * OPERAND_BYTES;   // of one CTA: 128 rows of either operand
+    static constexpr uint32_t SLOT_BYTES = (MODE == UPDATE ? 2 : 1) * OPERAND_BYTES;
+    static constexpr uint32_t COLUMNS = 2 * SIDE;            // of tensor memory: two tiles
+    static constexpr uint32_t SMEM = STAGES * STAGE_BYTES + SLOTS * SLOT_BYTES + 1024 + 256 + SIDE * 4;
+};
+
+__device__ __forceinline__ void takers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(TAKERS * 32) : "memory"); }
+
+template <int MODE, bool PAIR>
+__global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(const __grid_constant__ ProductArgs a, const __grid_constant__ ProductMaps maps)
 {
-    using S = Shape<PAIR>;
+    using S = Shape<MODE, PAIR>;
+    constexpr uint32_t BOXES = S::SIDE / BOX_COLS;                   // of a tile, for each CTA
     extern __shared__ uint8_t raw[];
-    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
-    // barriers behind the stages: full[STAGES], empty[STAGES], done[2], free[2]; then the base of the tensor memory
-    const uint32_t bars = base + S::STAGES * S::STAGE_BYTES;
-    const uint32_t full = bars, empty = bars + 8 * S::STAGES, done = empty + 8 * S::STAGES, free_ = done + 16, slot = free_ + 16;
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u, ring = base + S::STAGES * S::STAGE_BYTES;
+    const uint32_t bars = ring + S::SLOTS * S::SLOT_BYTES;
+    const uint32_t full = bars, empty = full + 8 * S::STAGES, done = empty + 8 * S::STAGES, free_ = done + 16;
+    const uint32_t filled = free_ + 16, worked = filled + 8 * S::SLOTS, stored = worked + 8 * S::SLOTS, slot = stored + 8 * S::SLOTS;
+    const uint32_t across = bars + 256;                              // D along the columns of a tile (POLY)
     volatile uint32_t *const stop = reinterpret_cast<volatile uint32_t *>(raw + (slot + 8 - smem_u32(raw)));
     const uint32_t warp = threadIdx.x / 32u, lane = threadIdx.x % 32u;
     const uint32_t rank = PAIR ? cluster_rank() : 0u;
     const uint32_t group = PAIR ? blockIdx.x / 2u : blockIdx.x, groups = PAIR ? gridDim.x / 2u : gridDim.x;
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::STAGES; ++s) {
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(full + 8 * s), "r"(1u) : "memory");
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(empty + 8 * s), "r"(1u) : "memory");
+            mbar_init_at(full + 8 * s, 1u);
+            mbar_init_at(empty + 8 * s, 1u);
         }
         for (int s = 0; s < 2; ++s) {
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(done + 8 * s), "r"(1u) : "memory");
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(free_ + 8 * s), "r"(PAIR ? 8u : 4u) : "memory");
+            mbar_init_at(done + 8 * s, 1u);
+            mbar_init_at(free_ + 8 * s, PAIR ? 2u * TAKERS : TAKERS);
+        }
+        for (int s = 0; s < S::SLOTS; ++s) {
+            mbar_init_at(filled + 8 * s, 1u);
+            mbar_init_at(worked + 8 * s, TAKERS);
+            mbar_init_at(stored + 8 * s, 1u);
         }
         *stop = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        prefetch_map(&map_p);
-        prefetch_map(&map_q);
+        fence_async_shared();
+        prefetch_map(&maps.p);
+        prefetch_map(&maps.q);
     }
     if (PAIR) cluster_sync_all();   // both CTAs of the pair are there
     if (warp == 2) tmem_alloc<PAIR>(slot, S::COLUMNS);
@@ -286,21 +386,20 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
             for (uint32_t k = 0; k < steps; ++k, ++n) {
                 const uint32_t s = n % S::STAGES, to = base + s * S::STAGE_BYTES;
                 if (n >= S::STAGES && !pipe_wait(empty + 8 * s, (n / S::STAGES - 1u) & 1u, stop)) break;
-                if (rank == 0)
-                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(full + 8 * s), "r"(S::STAGE_BYTES * (PAIR ? 2u : 1u)) : "memory");
-                tma_load_3d<PAIR>(to, &map_p, k * DEPTH, row, x.batch, full_lead + 8 * s);
+                if (rank == 0) mbar_expect_at(full + 8 * s, S::STAGE_BYTES * (PAIR ? 2u : 1u));
+                tma_load_3d<PAIR>(to, &maps.p, k * DEPTH, row, x.batch, full_lead + 8 * s);
                 if (MODE == UPDATE) {
-                    tma_load_3d<PAIR>(to + OPERAND_BYTES, &map_q, col, k * DEPTH, x.batch, full_lead + 8 * s);
-                    tma_load_3d<PAIR>(to + OPERAND_BYTES + OPERAND_BYTES / 2, &map_q, col + 64u, k * DEPTH, x.batch, full_lead + 8 * s);
+                    tma_load_3d<PAIR>(to + OPERAND_BYTES, &maps.q, col, k * DEPTH, x.batch, full_lead + 8 * s);
+                    tma_load_3d<PAIR>(to + OPERAND_BYTES + OPERAND_BYTES / 2, &maps.q, col + 64u, k * DEPTH, x.batch, full_lead + 8 * s);
                 } else {
-                    tma_load_3d<PAIR>(to + OPERAND_BYTES, &map_q, k * DEPTH, col, x.batch, full_lead + 8 * s);
+                    tma_load_3d<PAIR>(to + OPERAND_BYTES, &maps.q, k * DEPTH, col, x.batch, full_lead + 8 * s);
                 }
             }
         }
         if (*stop) drain();
     } else if (warp == 1 && rank == 0 && elect_one()) {
         // fp16 operands, fp32 sums, SIDE x SIDE; Q of UPDATE has its contraction across the rows
-        constexpr uint32_t INSTRUCTION = 1u << 4 | (MODE == UPDATE ? 1u << 16 : 0u) | (uint32_t)(S::SIDE / 8) << 17 | (uint32_t)(S::SIDE / 16) << 24;
+        constexpr uint32_t INSTRUCTION = 1u << 4 | (MODE == UPDATE ? 1u << 16 : 0u) | (S::SIDE / 8) << 17 | (S::SIDE / 16) << 24;
         uint32_t n = 0, done_tiles = 0;
         for (uint32_t t = group; t < all && !*stop; t += groups, ++done_tiles) {
             const uint32_t half = done_tiles & 1u, sums = tmem + half * S::SIDE;
@@ -325,30 +424,90 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
             mma_commit<PAIR>(done + 8 * half);
         }
         if (*stop) drain();
+    } else if (warp == 2 && elect_one()) {
+        uint32_t n = 0;
+        for (uint32_t t = group; t < all && !*stop; t += groups) {
+            const Tile x = tile_of<MODE>(t, a);
+            for (uint32_t b = 0; b < BOXES; ++b, ++n) {
+                const uint32_t s = n % S::SLOTS, to = ring + s * S::SLOT_BYTES;
+                if (n >= S::SLOTS && !pipe_wait(stored + 8 * s, (n / S::SLOTS - 1u) & 1u, stop)) break;
+                if (MODE == GRAM) {
+                    mbar_arrive_at(filled + 8 * s);
+                    continue;
+                }
+                const uint32_t col = x.j * S::SIDE + b * BOX_COLS, row = x.i * S::SIDE + rank * 128u;
+                const bool lo = MODE == UPDATE && a.lo_in;
+                mbar_expect_at(filled + 8 * s, lo ? 2 * OPERAND_BYTES : OPERAND_BYTES);
+                tma_load_3d<false>(to, &maps.in, col, row, x.batch, filled + 8 * s);
+                if (lo) tma_load_3d<false>(to + OPERAND_BYTES, &maps.in_lo, col, row, x.batch, filled + 8 * s);
+            }
+        }
+        if (*stop) drain();
+    } else if (warp == 3 && elect_one()) {
+        uint32_t n = 0;
+        const bool store = MODE != UPDATE || !a.out || a.out_tiled;
+        for (uint32_t t = group; t < all && !*stop; t += groups) {
+            const Tile x = tile_of<MODE>(t, a);
+            for (uint32_t b = 0; b < BOXES; ++b, ++n) {
+                const uint32_t s = n % S::SLOTS, from = ring + s * S::SLOT_BYTES;
+                if (!pipe_wait(worked + 8 * s, (n / S::SLOTS) & 1u, stop)) break;
+                const uint32_t col = x.j * S::SIDE + b * BOX_COLS, row = x.i * S::SIDE + rank * 128u;
+                if (store && col < a.cols && row < a.rows) {
+                    tma_store_3d(&maps.out, col, row, x.batch, from);
+                    if (MODE == UPDATE && a.lo_out) tma_store_3d(&maps.out_lo, col, row, x.batch, from + OPERAND_BYTES);
+                }
+                store_commit();
+                store_wait_read<0>();
+                mbar_arrive_at(stored + 8 * s);
+            }
+        }
+        store_wait<0>();
+        if (*stop) drain();
     } else if (warp >= 4) {
-        const uint32_t quarter = warp % 4u;
+        const uint32_t quarter = warp % 4u, r = quarter * 32u + lane, part = (warp - 4u) / 4u, thread = threadIdx.x - 128u;
         const uint32_t free_lead = PAIR ? map_shared(free_, 0) : free_;
-        uint32_t done_tiles = 0;
+        uint32_t n = 0, done_tiles = 0;
+        // after a wait that ran out the loops are gone through without work: the barriers of these warps stay in step
+        bool ok = true;
         for (uint32_t t = group; t < all; t += groups, ++done_tiles) {
             const Tile x = tile_of<MODE>(t, a);
-            const uint32_t half = done_tiles & 1u;
-            if (!__all_sync(FULL, pipe_wait(done + 8 * half, (done_tiles / 2) & 1u, stop))) break;
+            const uint32_t half = done_tiles & 1u, row0 = x.i * S::SIDE + rank * 128u, row = row0 + r;
+            float linear = 0.0f;
+            if (MODE != GRAM && row < a.rows) linear = __ldcg((MODE == POLY ? a.d : a.db) + x.batch * a.d_stride + row) + (MODE == UPDATE ? a.ca : 0.0f);
+            if (MODE == POLY) {
+                takers_sync();   // the last tile's have been read
+                if (thread < S::SIDE) {
+                    const uint32_t c = x.j * S::SIDE + thread;
+                    const float d = c < a.cols ? __ldcg(a.d + x.batch * a.d_stride + c) : 0.0f;
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(across + thread * 4u), "f"(d));
+                }
+                takers_sync();
+            }
+            ok = __all_sync(FULL, ok && pipe_wait(done + 8 * half, (done_tiles / 2) & 1u, stop));
             fence_after_sync();
-            const uint32_t row = x.i * S::SIDE + rank * 128u + quarter * 32u + lane;
-            for (uint32_t c = 0; c < S::SIDE; c += 32) {
-                float v[32];
+            for (uint32_t b = 0; b < BOXES; ++b, ++n) {
+                const uint32_t s = n % S::SLOTS, box = ring + s * S::SLOT_BYTES, first = b * BOX_COLS + part * TAKEN;
+                float v[TAKEN];
                 __syncwarp();
-                tmem_load32(tmem + (quarter * 32u << 16) + half * S::SIDE + c, v);
+                tmem_load16(tmem + (quarter * 32u << 16) + half * S::SIDE + first, v);
+                ok = __all_sync(FULL, ok && pipe_wait(filled + 8 * s, (n / S::SLOTS) & 1u, stop));
                 tmem_wait_load();
-                if (c + 32 == S::SIDE) {   // the last of the tile is in registers
+                if (b + 1 == BOXES) {   // the last of the tile is in registers
                     fence_before_sync();
                     __syncwarp();
                     if (lane == 0) {
                         if (PAIR) mbar_arrive_cluster(free_lead + 8 * half);
-                        else asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(free_ + 8 * half) : "memory");
+                        else mbar_arrive_at(free_ + 8 * half);
                     }
                 }
-                finish<MODE>(v, x.batch, row, x.j * S::SIDE + c, MODE != UPDATE && x.i != x.j, a);
+                if (ok) finish<MODE>(v, x.batch, row, x.j * S::SIDE + first, box, r, part * OCTETS, linear, across + first * 4u, x.i != x.j, a);
+                if (MODE == UPDATE && a.out && !a.turned && !a.out_tiled) {
+                    takers_sync();
+                    if (ok) store_rows(x.batch, row0, x.j * S::SIDE + b * BOX_COLS, box, thread, a);
+                }
+                fence_async_shared();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_at(worked + 8 * s);
             }
         }
     }
@@ -365,28 +524,32 @@ template <typename T>
 cudaError_t start(const OrthoArgs &a, const OrthoLayout &l, cudaStream_t stream)
 {
     const T *const x = static_cast<const T *>(a.x);
-    cudaError_t e = qesgd_launch(qesgd_ortho_norm_kernel<T>, dim3(l.parts, (unsigned)a.batch), dim3(THREADS), stream, x, a.rows, a.cols, a.ldx,
-                                 a.x_stride, reinterpret_cast<double *>(a.workspace));
+    const bool vec = qesgd_aligned(x, 16) && a.ldx * sizeof(T) % 16 == 0 && a.x_stride * sizeof(T) % 16 == 0;
+    const dim3 grid(l.parts, (unsigned)a.batch);
+    const uint32_t rows = (uint32_t)a.rows, cols = (uint32_t)a.cols;
+    double *const parts = reinterpret_cast<double *>(a.workspace);
+    cudaError_t e = qesgd_launch(qesgd_ortho_norm_kernel<T>, grid, dim3(THREADS), stream, x, rows, cols, a.ldx, a.x_stride, vec, parts);
     if (e != cudaSuccess) return e;
     const OrthoView v = {reinterpret_cast<__half *>(a.workspace + l.off_hi[0]), reinterpret_cast<__half *>(a.workspace + l.off_lo[0]), l.ld_x, l.x_stride};
-    return qesgd_launch(qesgd_ortho_start_kernel<T>, dim3(l.parts, (unsigned)a.batch), dim3(THREADS), stream, x, a.rows, a.cols, a.ldx,
-                        a.x_stride, reinterpret_cast<const double *>(a.workspace), l.parts, v, a.status);
+    return qesgd_launch(rows > cols ? qesgd_ortho_start_kernel<T, true> : qesgd_ortho_start_kernel<T, false>, grid, dim3(THREADS), stream, x, rows, cols,
+                        a.ldx, a.x_stride, vec, (const double *)parts, l.parts, v, a.status);
 }
 
-// fp16 matrices [batch][rows][ld] of `cols` columns; a box is 64 columns of `box_rows` rows, 128-byte rows swizzled.
-bool half_map(CUtensorMap *map, const void *p, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t batch, uint64_t stride, uint32_t box_rows)
+// 16-bit matrices [batch][rows][ld] of `cols` columns; a box is 64 columns of `box_rows` rows, 128-byte rows swizzled.
+bool half_map(CUtensorMap *map, const void *p, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t batch, uint64_t stride, uint32_t box_rows,
+              CUtensorMapDataType type = CU_TENSOR_MAP_DATA_TYPE_FLOAT16)
 {
     const QesgdEncodeTiledFn encode = qesgd_encode_tiled();
     const cuuint64_t dims[3] = {cols, rows, batch}, strides[2] = {ld * 2, stride * 2};
     const cuuint32_t box[3] = {64u, box_rows, 1u}, unit[3] = {1u, 1u, 1u};
-    return encode && encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3u, const_cast<void *>(p), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    return encode && encode(map, type, 3u, const_cast<void *>(p), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int MODE, bool PAIR>
-cudaError_t launch_product(ProductArgs a, const CUtensorMap &p, const CUtensorMap &q, int sm_count, cudaStream_t stream)
+cudaError_t launch_product(ProductArgs a, const ProductMaps &maps, int sm_count, cudaStream_t stream)
 {
-    using S = Shape<PAIR>;
+    using S = Shape<MODE, PAIR>;
     const auto kernel = qesgd_ortho_product_kernel<MODE, PAIR>;
     a.tiles_m = (a.rows + S::SIDE - 1) / S::SIDE;
     a.tiles_n = (a.cols + S::SIDE - 1) / S::SIDE;
@@ -394,15 +557,15 @@ cudaError_t launch_product(ProductArgs a, const CUtensorMap &p, const CUtensorMa
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
     if (e != cudaSuccess) return e;
     const uint32_t all = a.tiles * a.batch, most = (uint32_t)sm_count / (PAIR ? 2u : 1u);
-    return qesgd_launch_cluster(kernel, dim3((all < most ? all : most) * (PAIR ? 2u : 1u)), dim3(WARPS * 32), S::SMEM, PAIR ? 2u : 1u, stream, a, p, q);
+    return qesgd_launch_cluster(kernel, dim3((all < most ? all : most) * (PAIR ? 2u : 1u)), dim3(WARPS * 32), S::SMEM, PAIR ? 2u : 1u, stream, a, maps);
 }
 template <int MODE>
-cudaError_t launch_product(const ProductArgs &a, const CUtensorMap &p, const CUtensorMap &q, int sm_count, cudaStream_t stream)
+cudaError_t launch_product(const ProductArgs &a, const ProductMaps &maps, int sm_count, cudaStream_t stream)
 {
     // pairs where they fill most of the SMs
     const uint64_t m = (a.rows + 255) / 256, n = (a.cols + 255) / 256;
     const uint64_t pairs = (MODE == UPDATE ? m * n : m * (m + 1) / 2) * a.batch;
-    return pairs * 2 >= (uint64_t)sm_count ? launch_product<MODE, true>(a, p, q, sm_count, stream) : launch_product<MODE, false>(a, p, q, sm_count, stream);
+    return pairs * 2 >= (uint64_t)sm_count ? launch_product<MODE, true>(a, maps, sm_count, stream) : launch_product<MODE, false>(a, maps, sm_count, stream);
 }
 
 }  // namespace
@@ -411,10 +574,11 @@ int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t st
 {
     const OrthoLayout l = qesgd_ortho_layout(a.rows, a.cols, a.batch);
     const auto at = [&](uint64_t off) { return reinterpret_cast<__half *>(a.workspace + off); };
-    CUtensorMap rows[2], across[2], f, b;   // X by rows, X across them, F, B
+    CUtensorMap hi[2], lo[2], across[2], f, b;   // X by rows and its second term, X across its rows, F, B
     bool ok = half_map(&f, at(l.off_a), l.m, l.m, l.ld_a, a.batch, l.a_stride, 128) && half_map(&b, at(l.off_b), l.m, l.m, l.ld_a, a.batch, l.a_stride, 128);
     for (int i = 0; i < 2; ++i)
-        ok = ok && half_map(&rows[i], at(l.off_hi[i]), l.m, l.n, l.ld_x, a.batch, l.x_stride, 128) &&
+        ok = ok && half_map(&hi[i], at(l.off_hi[i]), l.m, l.n, l.ld_x, a.batch, l.x_stride, 128) &&
+             half_map(&lo[i], at(l.off_lo[i]), l.m, l.n, l.ld_x, a.batch, l.x_stride, 128) &&
              half_map(&across[i], at(l.off_hi[i]), l.m, l.n, l.ld_x, a.batch, l.x_stride, DEPTH);
     if (!ok) return (int)cudaErrorInvalidValue;
     cudaError_t e = a.dtype == QESGD_F32 ? start<float>(a, l, stream) : a.dtype == QESGD_BF16 ? start<__nv_bfloat16>(a, l, stream) : start<__half>(a, l, stream);
@@ -424,12 +588,8 @@ int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t st
         const uint32_t now = step % 2, next = 1 - now;
         ProductArgs p = {};
         p.batch = (uint32_t)a.batch;
-        p.f = at(l.off_a);
-        p.b = at(l.off_b);
         p.d = reinterpret_cast<float *>(a.workspace + l.off_d);
         p.db = p.d + a.batch * l.d_stride;
-        p.ld_x = l.ld_x;
-        p.x_stride = l.x_stride;
         p.ld_a = l.ld_a;
         p.a_stride = l.a_stride;
         p.d_stride = l.d_stride;
@@ -439,26 +599,29 @@ int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t st
         p.status = a.status;
         p.rows = p.cols = (uint32_t)l.m;
         p.depth = (uint32_t)l.n;
-        e = launch_product<GRAM>(p, rows[now], rows[now], sm_count, stream);
+        p.mirror = at(l.off_a);
+        e = launch_product<GRAM>(p, {hi[now], hi[now], f, f, f, f}, sm_count, stream);
         if (e != cudaSuccess) return (int)e;
         *launched += 1;
         p.depth = (uint32_t)l.m;
-        e = launch_product<POLY>(p, f, f, sm_count, stream);
+        p.mirror = at(l.off_b);
+        e = launch_product<POLY>(p, {f, f, f, f, b, b}, sm_count, stream);
         if (e != cudaSuccess) return (int)e;
         *launched += 1;
         p.cols = (uint32_t)l.n;
-        p.hi = at(l.off_hi[now]);
-        p.lo = step < ORTHO_LO_STEPS ? at(l.off_lo[now]) : nullptr;
-        p.hi_out = at(l.off_hi[next]);
-        p.lo_out = step + 1 < ORTHO_LO_STEPS ? at(l.off_lo[next]) : nullptr;
+        p.lo_in = step < ORTHO_LO_STEPS;
+        p.lo_out = step + 1 < ORTHO_LO_STEPS;
         if (step + 1 == a.steps) {
             p.out = static_cast<__nv_bfloat16 *>(a.out);
             p.ldo = a.ldo;
             p.out_stride = a.out_stride;
             p.turned = a.rows > a.cols;
-            p.out_vec = qesgd_aligned(a.out, 16) && a.ldo % 8 == 0 && a.out_stride % 8 == 0;
+            // a batch of one matrix has no stride of its own
+            const uint64_t stride = a.batch > 1 ? a.out_stride : (a.rows * a.ldo + 7) / 8 * 8;
+            p.out_tiled = !p.turned && qesgd_aligned(a.out, 16) && a.ldo % 8 == 0 && stride % 8 == 0 &&
+                          half_map(&hi[next], a.out, l.m, l.n, a.ldo, a.batch, stride, 128, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16);
         }
-        e = launch_product<UPDATE>(p, b, across[now], sm_count, stream);
+        e = launch_product<UPDATE>(p, {b, across[now], hi[now], lo[now], hi[next], lo[next]}, sm_count, stream);
         if (e != cudaSuccess) return (int)e;
         *launched += 1;
     }
