@@ -148,6 +148,7 @@ struct ProductArgs {
     uint32_t lo_in, lo_out;                   // UPDATE: whether X and X' have a second term
     __nv_bfloat16 *out;                       // UPDATE: the result, of the last step; else null
     uint64_t ld_a, a_stride, d_stride, ldo, out_stride;
+    uint32_t split;                           // CTAs of a cluster that share a tile's contraction, one tile for each cluster
     uint32_t turned, out_tiled;                // out_tiled: by tiled copies
     float ca, cb, cc;
     uint32_t *status;
@@ -224,17 +225,17 @@ __device__ __forceinline__ void finish(float (&v)[TAKEN], uint32_t batch, uint32
         halves(w, in);
     }
     if (MODE == GRAM) {
+        float own = 0.0f;
 #pragma unroll
         for (int k = 0; k < TAKEN; ++k) {
-            if (diagonal && c + k == row) {
-                if (row < a.rows) a.d[batch * a.d_stride + row] = v[k] * (1.0f / (XS * XS));
-                v[k] = 0.0f;
-            }
-            v[k] *= AS / (XS * XS);
+            own = c + k == row ? v[k] : own;
+            v[k] = c + k == row ? 0.0f : v[k] * (AS / (XS * XS));
         }
+        if (diagonal && row < a.rows) a.d[batch * a.d_stride + row] = own * (1.0f / (XS * XS));
     }
     if (MODE == POLY) {
         const float s2 = a.cc * BS / (AS * AS), s1 = a.cc * BS / AS, s0 = a.cb * BS / AS + s1 * linear;
+        float own = 0.0f;
 #pragma unroll
         for (int i = 0; i < TAKEN / 4; ++i) {
             const uint4 w = load_shared(across + i * 16);
@@ -242,14 +243,11 @@ __device__ __forceinline__ void finish(float (&v)[TAKEN], uint32_t batch, uint32
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int k = 4 * i + j;
-                if (diagonal && c + k == row) {
-                    if (row < a.rows) a.db[batch * a.d_stride + row] = a.cb * linear + a.cc * (v[k] * (1.0f / (AS * AS)) + linear * linear);
-                    v[k] = 0.0f;
-                } else {
-                    v[k] = s2 * v[k] + (s0 + s1 * d[j]) * in[k];
-                }
+                own = c + k == row ? v[k] : own;
+                v[k] = c + k == row ? 0.0f : s2 * v[k] + (s0 + s1 * d[j]) * in[k];
             }
         }
+        if (diagonal && row < a.rows) a.db[batch * a.d_stride + row] = a.cb * linear + a.cc * (own * (1.0f / (AS * AS)) + linear * linear);
     }
     if (MODE == UPDATE) {
         if (a.lo_in) {
@@ -345,8 +343,12 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
     const uint32_t across = bars + 256;                              // D along the columns of a tile (POLY)
     volatile uint32_t *const stop = reinterpret_cast<volatile uint32_t *>(raw + (slot + 8 - smem_u32(raw)));
     const uint32_t warp = threadIdx.x / 32u, lane = threadIdx.x % 32u;
-    const uint32_t rank = PAIR ? cluster_rank() : 0u;
-    const uint32_t group = PAIR ? blockIdx.x / 2u : blockIdx.x, groups = PAIR ? gridDim.x / 2u : gridDim.x;
+    const uint32_t rank = PAIR || a.split > 1 ? cluster_rank() : 0u;
+    // CTAs of a cluster: a pair, or those that share a contraction, of which the first two each finish one box
+    const uint32_t share = PAIR ? 2u : a.split, parts = PAIR ? 1u : a.split, part_k = PAIR ? 0u : rank;
+    const uint32_t group = blockIdx.x / share, groups = gridDim.x / share;
+    const uint32_t own_rows = PAIR ? rank * 128u : 0u;
+    const uint32_t box_first = parts > 1 ? rank : 0u, box_end = parts > 1 ? min(rank + 1u, BOXES) : BOXES;
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::STAGES; ++s) {
             mbar_init_at(full + 8 * s, 1u);
@@ -374,30 +376,34 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
     if (PAIR) cluster_sync_all();
     fence_after_sync();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(raw + (slot - smem_u32(raw)));
-    const uint32_t all = a.tiles * a.batch, steps = (a.depth + DEPTH - 1) / DEPTH;
+    const uint32_t all = a.tiles * a.batch, every = (a.depth + DEPTH - 1) / DEPTH;
+    const uint32_t step0 = every * part_k / parts, steps = every * (part_k + 1) / parts - step0;
     qesgd_wait_for_previous();
 
+    // the warp that stores has nothing that the others of a cluster wait for
+    if (parts > 1 && warp == 3) cluster_arrive();
     if (warp == 0 && elect_one()) {
         uint32_t n = 0;
         const uint32_t full_lead = PAIR ? map_shared(full, 0) : full;
         for (uint32_t t = group; t < all && !*stop; t += groups) {
             const Tile x = tile_of<MODE>(t, a);
-            const uint32_t row = x.i * S::SIDE + rank * 128u, col = x.j * S::SIDE + rank * 128u;
+            const uint32_t row = x.i * S::SIDE + own_rows, col = x.j * S::SIDE + own_rows;
             for (uint32_t k = 0; k < steps; ++k, ++n) {
                 const uint32_t s = n % S::STAGES, to = base + s * S::STAGE_BYTES;
                 if (n >= S::STAGES && !pipe_wait(empty + 8 * s, (n / S::STAGES - 1u) & 1u, stop)) break;
-                if (rank == 0) mbar_expect_at(full + 8 * s, S::STAGE_BYTES * (PAIR ? 2u : 1u));
-                tma_load_3d<PAIR>(to, &maps.p, k * DEPTH, row, x.batch, full_lead + 8 * s);
+                const uint32_t at = (step0 + k) * DEPTH;
+                if (!PAIR || rank == 0) mbar_expect_at(full + 8 * s, S::STAGE_BYTES * (PAIR ? 2u : 1u));
+                tma_load_3d<PAIR>(to, &maps.p, at, row, x.batch, full_lead + 8 * s);
                 if (MODE == UPDATE) {
-                    tma_load_3d<PAIR>(to + OPERAND_BYTES, &maps.q, col, k * DEPTH, x.batch, full_lead + 8 * s);
-                    tma_load_3d<PAIR>(to + OPERAND_BYTES + OPERAND_BYTES / 2, &maps.q, col + 64u, k * DEPTH, x.batch, full_lead + 8 * s);
+                    tma_load_3d<PAIR>(to + OPERAND_BYTES, &maps.q, col, at, x.batch, full_lead + 8 * s);
+                    tma_load_3d<PAIR>(to + OPERAND_BYTES + OPERAND_BYTES / 2, &maps.q, col + 64u, at, x.batch, full_lead + 8 * s);
                 } else {
-                    tma_load_3d<PAIR>(to + OPERAND_BYTES, &maps.q, k * DEPTH, col, x.batch, full_lead + 8 * s);
+                    tma_load_3d<PAIR>(to + OPERAND_BYTES, &maps.q, at, col, x.batch, full_lead + 8 * s);
                 }
             }
         }
         if (*stop) drain();
-    } else if (warp == 1 && rank == 0 && elect_one()) {
+    } else if (warp == 1 && (!PAIR || rank == 0) && elect_one()) {
         // fp16 operands, fp32 sums, SIDE x SIDE; Q of UPDATE has its contraction across the rows
         constexpr uint32_t INSTRUCTION = 1u << 4 | (MODE == UPDATE ? 1u << 16 : 0u) | (S::SIDE / 8) << 17 | (S::SIDE / 16) << 24;
         uint32_t n = 0, done_tiles = 0;
@@ -428,14 +434,14 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
         uint32_t n = 0;
         for (uint32_t t = group; t < all && !*stop; t += groups) {
             const Tile x = tile_of<MODE>(t, a);
-            for (uint32_t b = 0; b < BOXES; ++b, ++n) {
+            for (uint32_t b = box_first; b < box_end; ++b, ++n) {
                 const uint32_t s = n % S::SLOTS, to = ring + s * S::SLOT_BYTES;
                 if (n >= S::SLOTS && !pipe_wait(stored + 8 * s, (n / S::SLOTS - 1u) & 1u, stop)) break;
                 if (MODE == GRAM) {
                     mbar_arrive_at(filled + 8 * s);
                     continue;
                 }
-                const uint32_t col = x.j * S::SIDE + b * BOX_COLS, row = x.i * S::SIDE + rank * 128u;
+                const uint32_t col = x.j * S::SIDE + b * BOX_COLS, row = x.i * S::SIDE + own_rows;
                 const bool lo = MODE == UPDATE && a.lo_in;
                 mbar_expect_at(filled + 8 * s, lo ? 2 * OPERAND_BYTES : OPERAND_BYTES);
                 tma_load_3d<false>(to, &maps.in, col, row, x.batch, filled + 8 * s);
@@ -448,10 +454,10 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
         const bool store = MODE != UPDATE || !a.out || a.out_tiled;
         for (uint32_t t = group; t < all && !*stop; t += groups) {
             const Tile x = tile_of<MODE>(t, a);
-            for (uint32_t b = 0; b < BOXES; ++b, ++n) {
+            for (uint32_t b = box_first; b < box_end; ++b, ++n) {
                 const uint32_t s = n % S::SLOTS, from = ring + s * S::SLOT_BYTES;
                 if (!pipe_wait(worked + 8 * s, (n / S::SLOTS) & 1u, stop)) break;
-                const uint32_t col = x.j * S::SIDE + b * BOX_COLS, row = x.i * S::SIDE + rank * 128u;
+                const uint32_t col = x.j * S::SIDE + b * BOX_COLS, row = x.i * S::SIDE + own_rows;
                 if (store && col < a.cols && row < a.rows) {
                     tma_store_3d(&maps.out, col, row, x.batch, from);
                     if (MODE == UPDATE && a.lo_out) tma_store_3d(&maps.out_lo, col, row, x.batch, from + OPERAND_BYTES);
@@ -471,7 +477,7 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
         bool ok = true;
         for (uint32_t t = group; t < all; t += groups, ++done_tiles) {
             const Tile x = tile_of<MODE>(t, a);
-            const uint32_t half = done_tiles & 1u, row0 = x.i * S::SIDE + rank * 128u, row = row0 + r;
+            const uint32_t half = done_tiles & 1u, row0 = x.i * S::SIDE + own_rows, row = row0 + r;
             float linear = 0.0f;
             if (MODE != GRAM && row < a.rows) linear = __ldcg((MODE == POLY ? a.d : a.db) + x.batch * a.d_stride + row) + (MODE == UPDATE ? a.ca : 0.0f);
             if (MODE == POLY) {
@@ -485,14 +491,51 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
             }
             ok = __all_sync(FULL, ok && pipe_wait(done + 8 * half, (done_tiles / 2) & 1u, stop));
             fence_after_sync();
-            for (uint32_t b = 0; b < BOXES; ++b, ++n) {
+            if (parts > 1) {
+                // all products of this CTA are done: the sums that others finish go where the stages were, by four columns
+                for (uint32_t b = 0; b < BOXES; ++b) {
+                    if (b == rank) continue;
+                    float v[TAKEN];
+                    __syncwarp();
+                    tmem_load16(tmem + (quarter * 32u << 16) + b * BOX_COLS + part * TAKEN, v);
+                    tmem_wait_load();
+#pragma unroll
+                    for (int i = 0; i < TAKEN / 4; ++i)
+                        store_shared(base + (((b * BOX_COLS + part * TAKEN) / 4 + i) * 128u + r) * 16u,
+                                     make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])));
+                }
+                __syncwarp();
+                cluster_arrive();
+                cluster_wait();
+            }
+            for (uint32_t b = box_first; b < box_end; ++b, ++n) {
                 const uint32_t s = n % S::SLOTS, box = ring + s * S::SLOT_BYTES, first = b * BOX_COLS + part * TAKEN;
                 float v[TAKEN];
                 __syncwarp();
                 tmem_load16(tmem + (quarter * 32u << 16) + half * S::SIDE + first, v);
                 ok = __all_sync(FULL, ok && pipe_wait(filled + 8 * s, (n / S::SLOTS) & 1u, stop));
                 tmem_wait_load();
-                if (b + 1 == BOXES) {   // the last of the tile is in registers
+                if (parts > 1) {
+                    float mine[TAKEN];
+#pragma unroll
+                    for (int k = 0; k < TAKEN; ++k) {
+                        mine[k] = v[k];
+                        v[k] = 0.0f;
+                    }
+                    for (uint32_t p = 0; p < parts; ++p) {   // in the order of the contraction
+                        const uint32_t from = map_shared(base + (first / 4u * 128u + r) * 16u, p);
+#pragma unroll
+                        for (int i = 0; i < TAKEN / 4; ++i) {
+                            float4 f = make_float4(mine[4 * i], mine[4 * i + 1], mine[4 * i + 2], mine[4 * i + 3]);
+                            if (p != rank)
+                                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w) : "r"(from + i * 2048u));
+                            v[4 * i] += f.x;
+                            v[4 * i + 1] += f.y;
+                            v[4 * i + 2] += f.z;
+                            v[4 * i + 3] += f.w;
+                        }
+                    }
+                } else if (b + 1 == BOXES) {   // the last of the tile is in registers
                     fence_before_sync();
                     __syncwarp();
                     if (lane == 0) {
@@ -512,6 +555,11 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
         }
     }
     __syncwarp();
+    if (parts > 1) {
+        if (warp < 3) cluster_arrive();
+        if (warp < 4) cluster_wait();
+        cluster_sync_all();   // the others have read this CTA's sums
+    }
     __syncthreads();
     if (threadIdx.x == 0 && *stop) atomicOr(a.status, QESGD_STATUS_TIMEOUT);
     fence_before_sync();
@@ -547,25 +595,44 @@ bool half_map(CUtensorMap *map, const void *p, uint64_t rows, uint64_t cols, uin
 }
 
 template <int MODE, bool PAIR>
-cudaError_t launch_product(ProductArgs a, const ProductMaps &maps, int sm_count, cudaStream_t stream)
+cudaError_t launch_product(ProductArgs a, const ProductMaps &maps, uint32_t split, int sm_count, cudaStream_t stream)
 {
     using S = Shape<MODE, PAIR>;
     const auto kernel = qesgd_ortho_product_kernel<MODE, PAIR>;
     a.tiles_m = (a.rows + S::SIDE - 1) / S::SIDE;
     a.tiles_n = (a.cols + S::SIDE - 1) / S::SIDE;
     a.tiles = MODE == UPDATE ? a.tiles_m * a.tiles_n : a.tiles_m * (a.tiles_m + 1) / 2;
+    a.split = split;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
     if (e != cudaSuccess) return e;
-    const uint32_t all = a.tiles * a.batch, most = (uint32_t)sm_count / (PAIR ? 2u : 1u);
-    return qesgd_launch_cluster(kernel, dim3((all < most ? all : most) * (PAIR ? 2u : 1u)), dim3(WARPS * 32), S::SMEM, PAIR ? 2u : 1u, stream, a, maps);
+    const uint32_t share = PAIR ? 2u : split, all = a.tiles * a.batch, most = (uint32_t)sm_count / share;
+    return qesgd_launch_cluster(kernel, dim3((split > 1 || all < most ? all : most) * share), dim3(WARPS * 32), S::SMEM, share, stream, a, maps);
 }
+// Pairs or single CTAs, and how many CTAs share a contraction: by modelled time.
 template <int MODE>
 cudaError_t launch_product(const ProductArgs &a, const ProductMaps &maps, int sm_count, cudaStream_t stream)
 {
-    // pairs where they fill most of the SMs
-    const uint64_t m = (a.rows + 255) / 256, n = (a.cols + 255) / 256;
-    const uint64_t pairs = (MODE == UPDATE ? m * n : m * (m + 1) / 2) * a.batch;
-    return pairs * 2 >= (uint64_t)sm_count ? launch_product<MODE, true>(a, maps, sm_count, stream) : launch_product<MODE, false>(a, maps, sm_count, stream);
+    const auto tiles = [&](uint64_t side) {
+        const uint64_t m = (a.rows + side - 1) / side, n = (a.cols + side - 1) / side;
+        return (MODE == UPDATE ? m * n : m * (m + 1) / 2) * a.batch;
+    };
+    const double steps = (a.depth + DEPTH - 1) / DEPTH, sms = sm_count;
+    const double singles = (double)tiles(128), pairs = (double)tiles(256);
+    // clocks: a stage of one CTA takes 450 (few CTAs) to 650 (all SMs) to arrive, one of a pair 512 to 690
+    const auto stage = [&](double ctas, double few, double many) { return few + (many - few) * (ctas < sms ? ctas / sms : 1.0); };
+    const auto waves = [&](double n, double most) { return (double)(uint64_t)((n + most - 1) / most); };
+    double best = waves(pairs, (double)(sm_count / 2)) * steps * stage(2 * pairs, 512, 690) + 5000;
+    uint32_t split = 0;
+    for (uint32_t s = 1; s <= 4; s *= 2) {
+        // clusters of s lie within a group of 16 to 20 SMs each: seven of eight SMs take part at best
+        if (s > 1 && (singles * s > sms * 0.875 || steps < 4 * s)) break;
+        const double t = waves(singles * s, sms) * (double)(uint64_t)((steps + s - 1) / s) * stage(singles * s, 450, 650) + 2500 + (s > 1 ? 2000 : 0);
+        if (t < best) {
+            best = t;
+            split = s;
+        }
+    }
+    return split == 0 ? launch_product<MODE, true>(a, maps, 1, sm_count, stream) : launch_product<MODE, false>(a, maps, split, sm_count, stream);
 }
 
 }  // namespace
