@@ -9,14 +9,15 @@ constexpr int THREADS = 256;
 constexpr uint32_t FULL = 0xFFFFFFFFu;
 
 // Sum over a block; every thread calls it, thread 0 has the sum.  The order of the additions is fixed.
+template <int SIZE>
 __device__ __forceinline__ double block_sum(double sum)
 {
-    __shared__ double sums[THREADS / 32];
+    __shared__ double sums[SIZE / 32];
     for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(FULL, sum, o);
     if (threadIdx.x % 32 == 0) sums[threadIdx.x / 32] = sum;
     __syncthreads();
     if (threadIdx.x == 0)
-        for (int i = 1; i < THREADS / 32; ++i) sum += sums[i];
+        for (int i = 1; i < SIZE / 32; ++i) sum += sums[i];
     return sum;
 }
 
@@ -35,7 +36,7 @@ __global__ __launch_bounds__(THREADS) void qesgd_ortho_norm_kernel(const T *x, u
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum = fma((double)v[j], (double)v[j], sum);
     }
-    sum = block_sum(sum);
+    sum = block_sum<THREADS>(sum);
     if (threadIdx.x == 0) parts[blockIdx.y * gridDim.x + blockIdx.x] = sum;
 }
 
@@ -72,7 +73,7 @@ __global__ __launch_bounds__(THREADS) void qesgd_ortho_start_kernel(const T *x, 
     qesgd_wait_for_previous();
     double sum = 0.0;
     for (uint32_t i = threadIdx.x; i < nparts; i += THREADS) sum += parts[blockIdx.y * nparts + i];
-    sum = block_sum(sum);
+    sum = block_sum<THREADS>(sum);
     if (threadIdx.x == 0) {
         const bool fine = sum <= 1.7976931348623157e308;
         if (!fine && blockIdx.x == 0) atomicOr(status, QESGD_STATUS_NONFINITE);
@@ -568,6 +569,403 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
     if (warp == 2) tmem_dealloc<PAIR>(tmem, S::COLUMNS);
 }
 
+// ---------------------------------------------------- a whole matrix at once ----
+// Matrices with up to 128 rows (of the smaller side) and 4096 columns: all steps in one kernel.  A cluster of 1 to 16 CTAs
+// has a matrix, each up to 256 of its columns: X in two terms, and F, then B in its place, stay in shared memory; all sums
+// stay in tensor memory.  A step exchanges the parts of A among the CTAs: each adds up some of its columns, in the order
+// of the CTAs, and writes F's share of them into every CTA.  The fifteen products as kernels of their own take 5 us each
+// here, most of it for starting, waiting for the first copies and storing what the next one loads.
+constexpr uint32_t WHOLE_ROWS = 128, WHOLE_COLS = 256, WHOLE_MAX_CLUSTER = 16;
+constexpr uint32_t BOX_BYTES = OPERAND_BYTES;              // 128 rows of 64 columns
+constexpr uint32_t WHOLE_EXTRA = 1152;                     // diagonals, barrier and the like
+constexpr uint32_t WHOLE_THREADS = 512;
+constexpr uint32_t WHOLE_MIN_SMEM = 120 * 1024;            // one CTA of an SM: CTAs of two clusters must not wait for one another's tensor memory
+
+struct WholeArgs {
+    const void *x;
+    uint64_t rows, cols, ldx, x_stride, ldo, out_stride;
+    uint32_t m, n, width, steps, turned, vec, out_vec;     // width: columns of a CTA
+    float ca, cb, cc;
+    __nv_bfloat16 *out;
+    uint32_t *status;
+};
+
+__device__ __forceinline__ void store_remote(uint32_t addr, uint4 v)
+{
+    asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ void store_remote(uint32_t addr, float v) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory"); }
+__device__ __forceinline__ float load_shared_float(uint32_t addr)
+{
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr));
+    return v;
+}
+
+template <typename T, bool CLUSTER>
+__global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(const __grid_constant__ WholeArgs a)
+{
+    constexpr float XS = ORTHO_X_SCALE, AS = ORTHO_A_SCALE, BS = ORTHO_B_SCALE;
+    constexpr uint32_t A_COLUMN = 0, P_COLUMN = 128, U_COLUMN = 256;   // of tensor memory: sums of GRAM, POLY, UPDATE
+    extern __shared__ uint8_t raw[];
+    const uint32_t boxes = a.width / BOX_COLS, share = CLUSTER ? (a.n + a.width - 1) / a.width : 1u;
+    const uint32_t hi = (smem_u32(raw) + 1023u) & ~1023u, lo = hi + boxes * BOX_BYTES, f = lo + boxes * BOX_BYTES;
+    const uint32_t d = f + 2 * BOX_BYTES, db = d + 512, bar = db + 512, slot = bar + 8, norm = bar + 16, parts = f + 2 * BOX_BYTES + WHOLE_EXTRA;
+    volatile uint32_t *const stop = reinterpret_cast<volatile uint32_t *>(raw + (slot + 4 - smem_u32(raw)));
+    const uint32_t warp = threadIdx.x / 32u, lane = threadIdx.x % 32u, quarter = warp % 4u, part = warp / 4u, r = quarter * 32u + lane;
+    const uint32_t rank = CLUSTER ? cluster_rank() : 0u, cluster = CLUSTER ? gridDim.x : 1u;   // gridDim.x: a power of two, `share` or more
+    const uint32_t c0 = rank * a.width;
+    if (threadIdx.x == 0) {
+        mbar_init_at(bar, 1u);
+        *stop = 0u;
+        fence_async_shared();
+    }
+    if (warp == 0) tmem_alloc<false>(slot, 512u);
+    qesgd_wait_for_previous();
+
+    // ---- X = G / ||G||: this CTA's columns, every thread eight octets at most (of a row; turned, of a column) ----
+    const T *const g = static_cast<const T *>(a.x) + blockIdx.y * a.x_stride;
+    float v[8][8];
+    double sum = 0.0;
+    const uint32_t octets = a.turned ? WHOLE_ROWS / 8 : a.width / 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t n = threadIdx.x + i * WHOLE_THREADS, line = n / octets, first = n % octets * 8;   // line: row of X, or column
+        const bool inside = n < WHOLE_ROWS * a.width / 8 && (a.turned ? c0 + line < a.n && first < a.m : line < a.m && c0 + first < a.n);
+        if (inside) {
+            if (a.turned) load_octet(g + (c0 + line) * a.ldx, first, a.m, a.vec, v[i]);
+            else load_octet(g + line * a.ldx, c0 + first, a.n, a.vec, v[i]);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (!inside) v[i][k] = 0.0f;
+            sum = fma((double)v[i][k], (double)v[i][k], sum);
+        }
+    }
+    sum = block_sum<WHOLE_THREADS>(sum);
+    if (threadIdx.x == 0) *reinterpret_cast<double *>(raw + (norm - smem_u32(raw))) = sum;
+    fence_before_sync();
+    if (CLUSTER) cluster_sync_all();
+    else __syncthreads();
+    fence_after_sync();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(raw + (slot - smem_u32(raw)));
+    sum = 0.0;
+    for (uint32_t p = 0; p < cluster; ++p) {
+        double other;
+        if (CLUSTER) asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(other) : "r"(map_shared(norm, p)) : "memory");
+        else other = *reinterpret_cast<volatile double *>(raw + (norm - smem_u32(raw)));
+        sum += other;
+    }
+    const bool fine = sum <= 1.7976931348623157e308;
+    if (!fine && threadIdx.x == 0 && rank == 0) atomicOr(a.status, QESGD_STATUS_NONFINITE);
+    const double inverse = fine && sum > 0.0 ? (double)XS / sqrt(sum) : 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t n = threadIdx.x + i * WHOLE_THREADS, line = n / octets, first = n % octets * 8;
+        if (n >= WHOLE_ROWS * a.width / 8) break;
+        uint32_t h[4], l[4];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[i][k] = inverse == 0.0 ? 0.0f : (float)((double)v[i][k] * inverse);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            h[k] = half_pair(v[i][2 * k], v[i][2 * k + 1]);
+            const float2 kept = __half22float2(*reinterpret_cast<const __half2 *>(&h[k]));
+            l[k] = half_pair((v[i][2 * k] - kept.x) * ORTHO_LO_SCALE, (v[i][2 * k + 1] - kept.y) * ORTHO_LO_SCALE);
+        }
+        if (!a.turned) {
+            const uint32_t at = first / 64u * BOX_BYTES;
+            store_shared(box_octet(hi + at, line, first / 8u % 8u), make_uint4(h[0], h[1], h[2], h[3]));
+            store_shared(box_octet(lo + at, line, first / 8u % 8u), make_uint4(l[0], l[1], l[2], l[3]));
+        } else {
+            const uint32_t at = line / 64u * BOX_BYTES, o = line / 8u % 8u, in = line % 8u * 2u;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                asm volatile("st.shared.u16 [%0], %1;" ::"r"(box_octet(hi + at, first + k, o) + in), "h"((uint16_t)(h[k / 2] >> (16 * (k % 2)))));
+                asm volatile("st.shared.u16 [%0], %1;" ::"r"(box_octet(lo + at, first + k, o) + in), "h"((uint16_t)(l[k / 2] >> (16 * (k % 2)))));
+            }
+        }
+    }
+    fence_async_shared();
+    __syncthreads();
+
+    // A finished product is waited for by everybody; a wait that ran out leaves the barriers in step, and the result unsaid.
+    uint32_t phase = 0;
+    bool ok = true;
+    const auto products_done = [&]() {
+        ok = pipe_wait(bar, phase, stop) && ok;
+        phase ^= 1u;
+        __syncwarp();
+        fence_after_sync();
+    };
+    const auto settled = [&]() {   // shared memory written for the next product, tensor memory read
+        fence_async_shared();
+        fence_before_sync();
+        __syncthreads();
+        fence_after_sync();
+    };
+    constexpr uint32_t SQUARE = 1u << 4 | (128u / 8) << 17 | (128u / 16) << 24;
+    for (uint32_t step = 0; step < a.steps; ++step) {
+        const bool last = step + 1 == a.steps, lo_in = step < ORTHO_LO_STEPS, lo_out = step + 1 < ORTHO_LO_STEPS;
+        // ---- A = X X^T ----
+        if (warp == 0 && elect_one()) {
+            for (uint32_t b = 0; b < boxes; ++b)
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) {
+                    const uint64_t x = swizzled_matrix(hi + b * BOX_BYTES + i * 32u, 16u, 1024u);
+                    mma_f16<false>(tmem + A_COLUMN, x, x, SQUARE, b > 0 || i > 0);
+                }
+            mma_commit<false>(bar);
+        }
+        __syncwarp();
+        products_done();
+#pragma unroll 1
+        for (uint32_t c = part * 32u; c < part * 32u + 32u; c += 16u) {
+            float w[16];
+            __syncwarp();
+            tmem_load16(tmem + (quarter * 32u << 16) + A_COLUMN + c, w);
+            tmem_wait_load();
+            if (CLUSTER) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    store_shared(parts + ((c / 4 + i) * 128u + r) * 16u, make_uint4(__float_as_uint(w[4 * i]), __float_as_uint(w[4 * i + 1]),
+                                                                                  __float_as_uint(w[4 * i + 2]), __float_as_uint(w[4 * i + 3])));
+            } else {
+                float own = 0.0f;
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    own = c + k == r ? w[k] : own;
+                    w[k] = c + k == r ? 0.0f : w[k] * (AS / (XS * XS));
+                }
+                if (r - c < 16u) asm volatile("st.shared.f32 [%0], %1;" ::"r"(d + r * 4u), "f"(own * (1.0f / (XS * XS))));
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    store_shared(box_octet(f + c / 64u * BOX_BYTES, r, c / 8u % 8u + i),
+                                 make_uint4(half_pair(w[8 * i], w[8 * i + 1]), half_pair(w[8 * i + 2], w[8 * i + 3]), half_pair(w[8 * i + 4], w[8 * i + 5]),
+                                            half_pair(w[8 * i + 6], w[8 * i + 7])));
+            }
+        }
+        if (CLUSTER) {
+            __syncwarp();
+            cluster_sync_all();
+            const uint32_t mine = 16u / cluster;   // octets of columns
+            const uint32_t row = threadIdx.x % 128u;
+            for (uint32_t o = rank * mine + threadIdx.x / 128u; o < (rank + 1) * mine; o += WHOLE_THREADS / 128u) {
+                float w[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+                for (uint32_t p = 0; p < share; ++p) {   // CTAs behind the last column have nothing to add
+                    const uint32_t from = map_shared(parts + (o * 2u * 128u + row) * 16u, p);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float4 q;
+                        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(q.x), "=f"(q.y), "=f"(q.z), "=f"(q.w) : "r"(from + i * 2048u) : "memory");
+                        w[4 * i] += q.x;
+                        w[4 * i + 1] += q.y;
+                        w[4 * i + 2] += q.z;
+                        w[4 * i + 3] += q.w;
+                    }
+                }
+                float own = 0.0f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    own = o * 8u + k == row ? w[k] : own;
+                    w[k] = o * 8u + k == row ? 0.0f : w[k] * (AS / (XS * XS));
+                }
+                const uint4 packed = make_uint4(half_pair(w[0], w[1]), half_pair(w[2], w[3]), half_pair(w[4], w[5]), half_pair(w[6], w[7]));
+                for (uint32_t p = 0; p < cluster; ++p) {
+                    store_remote(map_shared(box_octet(f + o / 8u * BOX_BYTES, row, o % 8u), p), packed);
+                    if (o == row / 8u) store_remote(map_shared(d + row * 4u, p), own * (1.0f / (XS * XS)));
+                }
+            }
+            __syncwarp();
+            fence_async();
+            fence_before_sync();
+            cluster_sync_all();
+            fence_async();   // what the others wrote here, for this CTA's product
+            __syncthreads();
+            fence_after_sync();
+        } else {
+            settled();
+        }
+        // ---- B = b A + c A A ----
+        if (warp == 0 && elect_one()) {
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) {
+                const uint64_t x = swizzled_matrix(f + i / 4 * BOX_BYTES + i % 4 * 32u, 16u, 1024u);
+                mma_f16<false>(tmem + P_COLUMN, x, x, SQUARE, i > 0);
+            }
+            mma_commit<false>(bar);
+        }
+        __syncwarp();
+        products_done();
+        {
+            const float dr = load_shared_float(d + r * 4u);
+            const float s2 = a.cc * BS / (AS * AS), s1 = a.cc * BS / AS, s0 = a.cb * BS / AS + s1 * dr;
+#pragma unroll 1
+            for (uint32_t c = part * 32u; c < part * 32u + 32u; c += 16u) {
+                float w[16], in[16];
+                __syncwarp();
+                tmem_load16(tmem + (quarter * 32u << 16) + P_COLUMN + c, w);
+                uint4 q[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) q[i] = load_shared(box_octet(f + c / 64u * BOX_BYTES, r, c / 8u % 8u + i));
+                halves(q, in);
+                tmem_wait_load();
+                float own = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint4 z = load_shared(d + c * 4u + i * 16u);
+                    const float dc[4] = {__uint_as_float(z.x), __uint_as_float(z.y), __uint_as_float(z.z), __uint_as_float(z.w)};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int k = 4 * i + j;
+                        own = c + k == r ? w[k] : own;
+                        w[k] = c + k == r ? 0.0f : s2 * w[k] + (s0 + s1 * dc[j]) * in[k];
+                    }
+                }
+                if (r - c < 16u) asm volatile("st.shared.f32 [%0], %1;" ::"r"(db + r * 4u), "f"(a.cb * dr + a.cc * (own * (1.0f / (AS * AS)) + dr * dr)));
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    store_shared(box_octet(f + c / 64u * BOX_BYTES, r, c / 8u % 8u + i),
+                                 make_uint4(half_pair(w[8 * i], w[8 * i + 1]), half_pair(w[8 * i + 2], w[8 * i + 3]), half_pair(w[8 * i + 4], w[8 * i + 5]),
+                                            half_pair(w[8 * i + 6], w[8 * i + 7])));
+            }
+        }
+        settled();
+        // ---- X' = a X + B X ----
+        if (warp == 0 && elect_one()) {
+            const uint32_t instruction = 1u << 4 | 1u << 16 | (a.width / 8) << 17 | (128u / 16) << 24;
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i)
+                mma_f16<false>(tmem + U_COLUMN, swizzled_matrix(f + i / 4 * BOX_BYTES + i % 4 * 32u, 16u, 1024u), swizzled_matrix(hi + i * 2048u, BOX_BYTES, 1024u),
+                               instruction, i > 0);
+            mma_commit<false>(bar);
+        }
+        __syncwarp();
+        products_done();
+        const float linear = a.ca + load_shared_float(db + r * 4u);
+#pragma unroll 1
+        for (uint32_t c = part * 16u; c < a.width; c += 64u) {
+            float w[16], in[16];
+            __syncwarp();
+            tmem_load16(tmem + (quarter * 32u << 16) + U_COLUMN + c, w);
+            const uint32_t at = c / 64u * BOX_BYTES, o = c / 8u % 8u;
+            uint4 q[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) q[i] = load_shared(box_octet(hi + at, r, o + i));
+            halves(q, in);
+            if (lo_in) {
+                float rest[16];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) q[i] = load_shared(box_octet(lo + at, r, o + i));
+                halves(q, rest);
+#pragma unroll
+                for (int k = 0; k < 16; ++k) in[k] += rest[k] * (1.0f / ORTHO_LO_SCALE);
+            }
+            tmem_wait_load();
+#pragma unroll
+            for (int k = 0; k < 16; ++k) w[k] = linear * in[k] + w[k] * (1.0f / BS);
+            uint32_t h[8];
+            if (last) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const __nv_bfloat162 p = __floats2bfloat162_rn(w[2 * k] * (1.0f / XS), w[2 * k + 1] * (1.0f / XS));
+                    h[k] = *reinterpret_cast<const uint32_t *>(&p);
+                }
+                if (a.turned) {
+                    __nv_bfloat16 *to = a.out + blockIdx.y * a.out_stride + (c0 + c) * a.ldo + r;
+                    if (r < a.m && ok)
+#pragma unroll
+                        for (int k = 0; k < 16; ++k, to += a.ldo)
+                            if (c0 + c + k < a.n) {
+                                const uint16_t e = (uint16_t)(h[k / 2] >> (16 * (k % 2)));
+                                *to = *reinterpret_cast<const __nv_bfloat16 *>(&e);
+                            }
+                    continue;
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) h[k] = half_pair(w[2 * k], w[2 * k + 1]);
+                if (lo_out) {
+                    uint32_t l[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const float2 kept = __half22float2(*reinterpret_cast<const __half2 *>(&h[k]));
+                        l[k] = half_pair((w[2 * k] - kept.x) * ORTHO_LO_SCALE, (w[2 * k + 1] - kept.y) * ORTHO_LO_SCALE);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) store_shared(box_octet(lo + at, r, o + i), make_uint4(l[4 * i], l[4 * i + 1], l[4 * i + 2], l[4 * i + 3]));
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) store_shared(box_octet(hi + at, r, o + i), make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]));
+        }
+        __syncwarp();
+        settled();
+    }
+    // ---- the result, row by row ----
+    if (!a.turned && ok) {
+        __nv_bfloat16 *const out = a.out + blockIdx.y * a.out_stride;
+        for (uint32_t n = threadIdx.x; n < a.m * (a.width / 8); n += WHOLE_THREADS) {
+            const uint32_t row = n / (a.width / 8), o = n % (a.width / 8), c = c0 + o * 8;
+            if (c >= a.n) continue;
+            const uint4 w = load_shared(box_octet(hi + o / 8 * BOX_BYTES, row, o % 8));
+            __nv_bfloat16 *const to = out + row * a.ldo + c;
+            if (a.out_vec && c + 8 <= a.n) {
+                *reinterpret_cast<uint4 *>(to) = w;
+            } else {
+                const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const uint16_t e = (uint16_t)(u[k / 2] >> (16 * (k % 2)));
+                    if (c + k < a.n) to[k] = *reinterpret_cast<const __nv_bfloat16 *>(&e);
+                }
+            }
+        }
+    }
+    __syncwarp();
+    if (threadIdx.x == 0 && *stop) {
+        drain();
+        atomicOr(a.status, QESGD_STATUS_TIMEOUT);
+    }
+    fence_before_sync();
+    __syncthreads();
+    if (warp == 0) tmem_dealloc<false>(tmem, 512u);
+}
+
+template <typename T>
+cudaError_t launch_whole(const OrthoArgs &o, cudaStream_t stream)
+{
+    WholeArgs a = {};
+    a.x = o.x;
+    a.rows = o.rows;
+    a.cols = o.cols;
+    a.ldx = o.ldx;
+    a.x_stride = o.x_stride;
+    a.ldo = o.ldo;
+    a.out_stride = o.out_stride;
+    a.m = (uint32_t)(o.rows < o.cols ? o.rows : o.cols);
+    a.n = (uint32_t)(o.rows < o.cols ? o.cols : o.rows);
+    a.turned = o.rows > o.cols;
+    a.steps = o.steps;
+    a.vec = qesgd_aligned(o.x, 16) && o.ldx * sizeof(T) % 16 == 0 && o.x_stride * sizeof(T) % 16 == 0;
+    a.out_vec = qesgd_aligned(o.out, 16) && o.ldo % 8 == 0 && o.out_stride % 8 == 0;
+    a.ca = o.a;
+    a.cb = o.b;
+    a.cc = o.c;
+    a.out = static_cast<__nv_bfloat16 *>(o.out);
+    a.status = o.status;
+    uint32_t cluster = 1;
+    while (cluster * WHOLE_COLS < a.n) cluster *= 2;
+    a.width = (a.n + cluster - 1) / cluster;
+    a.width = (a.width + BOX_COLS - 1) / BOX_COLS * BOX_COLS;
+    uint32_t smem = (2 * a.width / BOX_COLS + 2) * BOX_BYTES + WHOLE_EXTRA + 1024 + (cluster > 1 ? 128 * 128 * 4 : 0);
+    if (smem < WHOLE_MIN_SMEM) smem = WHOLE_MIN_SMEM;
+    const auto kernel = cluster > 1 ? qesgd_ortho_whole_kernel<T, true> : qesgd_ortho_whole_kernel<T, false>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e == cudaSuccess && cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+    return qesgd_launch_cluster(kernel, dim3(cluster, (unsigned)o.batch), dim3(WHOLE_THREADS), smem, cluster, stream, a);
+}
+
 template <typename T>
 cudaError_t start(const OrthoArgs &a, const OrthoLayout &l, cudaStream_t stream)
 {
@@ -639,6 +1037,10 @@ cudaError_t launch_product(const ProductArgs &a, const ProductMaps &maps, int sm
 
 int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t stream, int *launched)
 {
+    if ((a.rows < a.cols ? a.rows : a.cols) <= WHOLE_ROWS && (a.rows < a.cols ? a.cols : a.rows) <= WHOLE_COLS * WHOLE_MAX_CLUSTER) {
+        *launched = 1;
+        return (int)(a.dtype == QESGD_F32 ? launch_whole<float>(a, stream) : a.dtype == QESGD_BF16 ? launch_whole<__nv_bfloat16>(a, stream) : launch_whole<__half>(a, stream));
+    }
     const OrthoLayout l = qesgd_ortho_layout(a.rows, a.cols, a.batch);
     const auto at = [&](uint64_t off) { return reinterpret_cast<__half *>(a.workspace + off); };
     CUtensorMap hi[2], lo[2], across[2], f, b;   // X by rows and its second term, X across its rows, F, B

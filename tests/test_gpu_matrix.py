@@ -335,7 +335,7 @@ def _gradient(batch, rows, cols, dtype, seed, pad=0):
 
 
 @pytest.mark.parametrize("rows,cols", [(16, 16), (17, 31), (64, 256), (256, 64), (100, 1000), (128, 128), (129, 300), (300, 129),
-                                       (256, 512), (500, 500), (520, 1030), (1000, 130)])
+                                       (256, 512), (500, 500), (520, 1030), (1000, 130), (128, 4096), (2100, 90), (70, 520), (40, 4500), (4500, 40)])
 @pytest.mark.parametrize("dtype", list(DTYPE))
 def test_orthogonalize(dtype, rows, cols):
     for batch, pad, ldo in ((1, 0, None), (3, 1, cols + 3), (2, 8, cols + 8)):
