@@ -21,7 +21,45 @@ __device__ __forceinline__ double block_sum(double sum)
     return sum;
 }
 
-// Sum of the squares of a part of a matrix, in 64 bits: no 32-bit value's square is out of range.
+// Power of two next to the largest of eight magnitudes, as an exponent that keeps 2^-e a normal number.
+__device__ __forceinline__ int octet_exponent(const float (&v)[8])
+{
+    float top = fmaxf(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))),
+                      fmaxf(fmaxf(fabsf(v[4]), fabsf(v[5])), fmaxf(fabsf(v[6]), fabsf(v[7]))));
+    return min(max((int)(__float_as_uint(top) >> 23) - 127, -120), 120);
+}
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+// Sum of the squares of eight elements, in 64 bits.  The squares are taken in 32 bits (four times the conversions to 64 would
+// take as long as the loads) of elements scaled by a power of two: none is out of range, whatever the elements.
+__device__ __forceinline__ double octet_squares(const float (&v)[8])
+{
+    const int e = octet_exponent(v);
+    const float p = power_of_two(-e);
+    float sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum = fmaf(v[k] * p, v[k] * p, sum);
+    return (double)sum * __longlong_as_double((long long)(2 * e + 1023) << 52);
+}
+// What an element of G is multiplied by to become one of X as it is kept: three factors, of which two are powers of two that
+// together bring the norm next to 1, since the quotient may not be a 32-bit number where its product with G's elements is.
+struct Normalise {
+    float f, p, q;
+};
+__device__ __forceinline__ Normalise normalise(double squares)
+{
+    Normalise n = {0.0f, 0.0f, 0.0f};
+    if (squares > 0.0 && squares <= 1.7976931348623157e308) {
+        const double norm = sqrt(squares);
+        const int e = (int)(__double_as_longlong(norm) >> 52) - 1023, half = e / 2;   // |e| < 200
+        n.p = power_of_two(-half);
+        n.q = power_of_two(half - e);
+        n.f = (float)((double)ORTHO_X_SCALE / (norm * __longlong_as_double((long long)(1023 - e) << 52)));
+    }
+    return n;
+}
+__device__ __forceinline__ float times(float g, const Normalise &n) { return n.f == 0.0f ? 0.0f : g * n.p * n.q * n.f; }
+
+// Sum of the squares of a part of a matrix.
 template <typename T>
 __global__ __launch_bounds__(THREADS) void qesgd_ortho_norm_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ldx, uint64_t stride, bool vec,
                                                                    double *parts)
@@ -33,22 +71,34 @@ __global__ __launch_bounds__(THREADS) void qesgd_ortho_norm_kernel(const T *x, u
     for (uint32_t n = blockIdx.x * THREADS + threadIdx.x; n < all; n += gridDim.x * THREADS) {
         float v[8];
         load_octet(m + n / octets * ldx, n % octets * 8, cols, vec, v);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum = fma((double)v[j], (double)v[j], sum);
+        sum += octet_squares(v);
     }
     sum = block_sum<THREADS>(sum);
     if (threadIdx.x == 0) parts[blockIdx.y * gridDim.x + blockIdx.x] = sum;
 }
 
-__device__ __forceinline__ __half2 to_halves(float a, float b)
-{
-    const __half2 most = __float2half2_rn(65504.0f);
-    return __hmax2(__hmin2(__floats2half2_rn(a, b), most), __hneg2(most));
-}
+// Two floats as fp16, cut off at its largest number.
 __device__ __forceinline__ uint32_t half_pair(float a, float b)
 {
-    const __half2 h = to_halves(a, b);
-    return *reinterpret_cast<const uint32_t *>(&h);
+    uint32_t r;
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    return r;
+}
+__device__ __forceinline__ float2 float_pair(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2 *>(&h)); }
+// What rounding two floats to the fp16 pair h has left behind.
+__device__ __forceinline__ uint32_t rest_pair(float a, float b, uint32_t h)
+{
+    const float2 kept = float_pair(h);
+    return half_pair(a - kept.x, b - kept.y);
+}
+// a * b + c on two floats at once
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 r;
+    asm("{\n.reg .b64 a, b, c;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\nfma.rn.f32x2 a, a, b, c;\nmov.b64 {%0, %1}, a;\n}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
 }
 __device__ __forceinline__ void store_terms(const float (&f)[8], __half *hi, __half *lo)
 {
@@ -56,8 +106,7 @@ __device__ __forceinline__ void store_terms(const float (&f)[8], __half *hi, __h
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         h[k] = half_pair(f[2 * k], f[2 * k + 1]);
-        const float2 kept = __half22float2(*reinterpret_cast<const __half2 *>(&h[k]));
-        l[k] = half_pair((f[2 * k] - kept.x) * ORTHO_LO_SCALE, (f[2 * k + 1] - kept.y) * ORTHO_LO_SCALE);
+        l[k] = rest_pair(f[2 * k], f[2 * k + 1], h[k]);
     }
     *reinterpret_cast<uint4 *>(hi) = make_uint4(h[0], h[1], h[2], h[3]);
     *reinterpret_cast<uint4 *>(lo) = make_uint4(l[0], l[1], l[2], l[3]);
@@ -68,19 +117,18 @@ template <typename T, bool TURNED>
 __global__ __launch_bounds__(THREADS) void qesgd_ortho_start_kernel(const T *x, uint32_t rows, uint32_t cols, uint64_t ldx, uint64_t stride, bool vec,
                                                                     const double *parts, uint32_t nparts, OrthoView v, uint32_t *status)
 {
-    __shared__ double inverse;
+    __shared__ double squares;
     __shared__ float held[TURNED ? 64 * 65 : 1];
     qesgd_wait_for_previous();
     double sum = 0.0;
     for (uint32_t i = threadIdx.x; i < nparts; i += THREADS) sum += parts[blockIdx.y * nparts + i];
     sum = block_sum<THREADS>(sum);
     if (threadIdx.x == 0) {
-        const bool fine = sum <= 1.7976931348623157e308;
-        if (!fine && blockIdx.x == 0) atomicOr(status, QESGD_STATUS_NONFINITE);
-        inverse = fine && sum > 0.0 ? (double)ORTHO_X_SCALE / sqrt(sum) : 0.0;
+        if (!(sum <= 1.7976931348623157e308) && blockIdx.x == 0) atomicOr(status, QESGD_STATUS_NONFINITE);
+        squares = sum;
     }
     __syncthreads();
-    const double inv = inverse;
+    const Normalise scale = normalise(squares);
     const T *const m = x + blockIdx.y * stride;
     __half *const hi = v.hi + blockIdx.y * v.x_stride, *const lo = v.lo + blockIdx.y * v.x_stride;
     if (!TURNED) {
@@ -90,7 +138,7 @@ __global__ __launch_bounds__(THREADS) void qesgd_ortho_start_kernel(const T *x, 
             float f[8];
             load_octet(m + r * ldx, c, cols, vec, f);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = inv == 0.0 ? 0.0f : (float)((double)f[j] * inv);
+            for (int j = 0; j < 8; ++j) f[j] = times(f[j], scale);
             store_terms(f, hi + r * v.ld + c, lo + r * v.ld + c);
         }
         return;
@@ -101,7 +149,7 @@ __global__ __launch_bounds__(THREADS) void qesgd_ortho_start_kernel(const T *x, 
         for (uint32_t i = threadIdx.x; i < 64 * 64; i += THREADS) {
             const uint32_t r = r0 + i / 64, c = c0 + i % 64;
             const float g = r < rows && c < cols ? to_float(m[r * ldx + c]) : 0.0f;
-            held[i / 64 * 65 + i % 64] = inv == 0.0 ? 0.0f : (float)((double)g * inv);
+            held[i / 64 * 65 + i % 64] = times(g, scale);
         }
         __syncthreads();
         for (uint32_t i = threadIdx.x; i < 64 * 8; i += THREADS) {
@@ -209,6 +257,20 @@ __device__ __forceinline__ void halves(const uint4 (&w)[N], float (&v)[8 * N])
 constexpr int TAKEN = 64 / (TAKERS / 4);   // columns of a box that a warp takes
 constexpr int OCTETS = TAKEN / 8;
 
+// a X + B X as X is kept, from the sums of B X
+template <int N>
+__device__ __forceinline__ void update(float (&v)[N], const float (&in)[N], float linear)
+{
+    constexpr float S = 1.0f / ORTHO_B_SCALE;
+#pragma unroll
+    for (int k = 0; k < N; k += 2) {
+        const float2 b = fma2(make_float2(v[k], v[k + 1]), make_float2(S, S), make_float2(0.0f, 0.0f));
+        const float2 x = fma2(make_float2(in[k], in[k + 1]), make_float2(linear, linear), b);
+        v[k] = x.x;
+        v[k + 1] = x.y;
+    }
+}
+
 // TAKEN neighbouring sums of row `row` (row r of the CTA's boxes) from column c on (octet o of the box) -> what is kept of
 // them, in the box at `box` (and a second term in the box behind it).  `linear`: the row's element of D (POLY), a and the
 // row's element of B's diagonal (UPDATE); `across`: D from column c on, in shared memory.
@@ -258,10 +320,9 @@ __device__ __forceinline__ void finish(float (&v)[TAKEN], uint32_t batch, uint32
             for (int i = 0; i < OCTETS; ++i) w[i] = load_shared(box_octet(box + OPERAND_BYTES, r, o + i));
             halves(w, rest);
 #pragma unroll
-            for (int k = 0; k < TAKEN; ++k) in[k] += rest[k] * (1.0f / ORTHO_LO_SCALE);
+            for (int k = 0; k < TAKEN; ++k) in[k] += rest[k];
         }
-#pragma unroll
-        for (int k = 0; k < TAKEN; ++k) v[k] = linear * in[k] + v[k] * (1.0f / BS);   // times XS, as X is kept
+        update(v, in, linear);
         if (a.out) {
             __nv_bfloat162 h[TAKEN / 2];
 #pragma unroll
@@ -280,29 +341,24 @@ __device__ __forceinline__ void finish(float (&v)[TAKEN], uint32_t batch, uint32
             return;
         }
     }
-    __half2 h[TAKEN / 2];
+    uint32_t h[TAKEN / 2];
 #pragma unroll
-    for (int k = 0; k < TAKEN / 2; ++k) h[k] = to_halves(v[2 * k], v[2 * k + 1]);
-    const uint32_t *const w = reinterpret_cast<const uint32_t *>(h);
+    for (int k = 0; k < TAKEN / 2; ++k) h[k] = half_pair(v[2 * k], v[2 * k + 1]);
 #pragma unroll
-    for (int i = 0; i < OCTETS; ++i) store_shared(box_octet(box, r, o + i), make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+    for (int i = 0; i < OCTETS; ++i) store_shared(box_octet(box, r, o + i), make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]));
     if (MODE == UPDATE && a.lo_out) {
-        __half2 l[TAKEN / 2];
+        uint32_t l[TAKEN / 2];
 #pragma unroll
-        for (int k = 0; k < TAKEN / 2; ++k) {
-            const float2 f = __half22float2(h[k]);
-            l[k] = to_halves((v[2 * k] - f.x) * ORTHO_LO_SCALE, (v[2 * k + 1] - f.y) * ORTHO_LO_SCALE);
-        }
-        const uint32_t *const z = reinterpret_cast<const uint32_t *>(l);
+        for (int k = 0; k < TAKEN / 2; ++k) l[k] = rest_pair(v[2 * k], v[2 * k + 1], h[k]);
 #pragma unroll
         for (int i = 0; i < OCTETS; ++i)
-            store_shared(box_octet(box + OPERAND_BYTES, r, o + i), make_uint4(z[4 * i], z[4 * i + 1], z[4 * i + 2], z[4 * i + 3]));
+            store_shared(box_octet(box + OPERAND_BYTES, r, o + i), make_uint4(l[4 * i], l[4 * i + 1], l[4 * i + 2], l[4 * i + 3]));
     }
     if (MODE != UPDATE && mirror && row < a.rows) {
-        __half *to = a.mirror + batch * a.a_stride + c * a.ld_a + row;
+        unsigned short *to = reinterpret_cast<unsigned short *>(a.mirror) + batch * a.a_stride + c * a.ld_a + row;
 #pragma unroll
         for (int k = 0; k < TAKEN; ++k, to += a.ld_a)
-            if (c + k < a.cols) *to = k % 2 ? __high2half(h[k / 2]) : __low2half(h[k / 2]);
+            if (c + k < a.cols) *to = (unsigned short)(h[k / 2] >> (16 * (k % 2)));
     }
 }
 
@@ -525,15 +581,19 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
                     }
                     for (uint32_t p = 0; p < parts; ++p) {   // in the order of the contraction
                         const uint32_t from = map_shared(base + (first / 4u * 128u + r) * 16u, p);
+                        float4 f[TAKEN / 4];
+                        if (p != rank)
+#pragma unroll
+                            for (int i = 0; i < TAKEN / 4; ++i)
+                                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                             : "=f"(f[i].x), "=f"(f[i].y), "=f"(f[i].z), "=f"(f[i].w)
+                                             : "r"(from + i * 2048u));
 #pragma unroll
                         for (int i = 0; i < TAKEN / 4; ++i) {
-                            float4 f = make_float4(mine[4 * i], mine[4 * i + 1], mine[4 * i + 2], mine[4 * i + 3]);
-                            if (p != rank)
-                                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w) : "r"(from + i * 2048u));
-                            v[4 * i] += f.x;
-                            v[4 * i + 1] += f.y;
-                            v[4 * i + 2] += f.z;
-                            v[4 * i + 3] += f.w;
+                            v[4 * i] += p == rank ? mine[4 * i] : f[i].x;
+                            v[4 * i + 1] += p == rank ? mine[4 * i + 1] : f[i].y;
+                            v[4 * i + 2] += p == rank ? mine[4 * i + 2] : f[i].z;
+                            v[4 * i + 3] += p == rank ? mine[4 * i + 3] : f[i].w;
                         }
                     }
                 } else if (b + 1 == BOXES) {   // the last of the tile is in registers
@@ -636,11 +696,10 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
             if (a.turned) load_octet(g + (c0 + line) * a.ldx, first, a.m, a.vec, v[i]);
             else load_octet(g + line * a.ldx, c0 + first, a.n, a.vec, v[i]);
         }
+        if (!inside)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            if (!inside) v[i][k] = 0.0f;
-            sum = fma((double)v[i][k], (double)v[i][k], sum);
-        }
+            for (int k = 0; k < 8; ++k) v[i][k] = 0.0f;
+        sum += octet_squares(v[i]);
     }
     sum = block_sum<WHOLE_THREADS>(sum);
     if (threadIdx.x == 0) *reinterpret_cast<double *>(raw + (norm - smem_u32(raw))) = sum;
@@ -656,21 +715,19 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
         else other = *reinterpret_cast<volatile double *>(raw + (norm - smem_u32(raw)));
         sum += other;
     }
-    const bool fine = sum <= 1.7976931348623157e308;
-    if (!fine && threadIdx.x == 0 && rank == 0) atomicOr(a.status, QESGD_STATUS_NONFINITE);
-    const double inverse = fine && sum > 0.0 ? (double)XS / sqrt(sum) : 0.0;
+    if (!(sum <= 1.7976931348623157e308) && threadIdx.x == 0 && rank == 0) atomicOr(a.status, QESGD_STATUS_NONFINITE);
+    const Normalise scale = normalise(sum);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const uint32_t n = threadIdx.x + i * WHOLE_THREADS, line = n / octets, first = n % octets * 8;
         if (n >= WHOLE_ROWS * a.width / 8) break;
         uint32_t h[4], l[4];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[i][k] = inverse == 0.0 ? 0.0f : (float)((double)v[i][k] * inverse);
+        for (int k = 0; k < 8; ++k) v[i][k] = times(v[i][k], scale);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             h[k] = half_pair(v[i][2 * k], v[i][2 * k + 1]);
-            const float2 kept = __half22float2(*reinterpret_cast<const __half2 *>(&h[k]));
-            l[k] = half_pair((v[i][2 * k] - kept.x) * ORTHO_LO_SCALE, (v[i][2 * k + 1] - kept.y) * ORTHO_LO_SCALE);
+            l[k] = rest_pair(v[i][2 * k], v[i][2 * k + 1], h[k]);
         }
         if (!a.turned) {
             const uint32_t at = first / 64u * BOX_BYTES;
@@ -751,17 +808,27 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
             const uint32_t row = threadIdx.x % 128u;
             for (uint32_t o = rank * mine + threadIdx.x / 128u; o < (rank + 1) * mine; o += WHOLE_THREADS / 128u) {
                 float w[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-                for (uint32_t p = 0; p < share; ++p) {   // CTAs behind the last column have nothing to add
-                    const uint32_t from = map_shared(parts + (o * 2u * 128u + row) * 16u, p);
+                for (uint32_t p0 = 0; p0 < share; p0 += 4) {   // CTAs behind the last column have nothing to add
+                    float4 q[4][2];
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        float4 q;
-                        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(q.x), "=f"(q.y), "=f"(q.z), "=f"(q.w) : "r"(from + i * 2048u) : "memory");
-                        w[4 * i] += q.x;
-                        w[4 * i + 1] += q.y;
-                        w[4 * i + 2] += q.z;
-                        w[4 * i + 3] += q.w;
+                    for (uint32_t p = 0; p < 4; ++p) {
+                        const uint32_t from = map_shared(parts + (o * 2u * 128u + row) * 16u, min(p0 + p, share - 1u));
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                         : "=f"(q[p][i].x), "=f"(q[p][i].y), "=f"(q[p][i].z), "=f"(q[p][i].w)
+                                         : "r"(from + i * 2048u));
                     }
+#pragma unroll
+                    for (uint32_t p = 0; p < 4; ++p)
+                        if (p0 + p < share)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                w[4 * i] += q[p][i].x;
+                                w[4 * i + 1] += q[p][i].y;
+                                w[4 * i + 2] += q[p][i].z;
+                                w[4 * i + 3] += q[p][i].w;
+                            }
                 }
                 float own = 0.0f;
 #pragma unroll
@@ -858,11 +925,10 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
                 for (int i = 0; i < 2; ++i) q[i] = load_shared(box_octet(lo + at, r, o + i));
                 halves(q, rest);
 #pragma unroll
-                for (int k = 0; k < 16; ++k) in[k] += rest[k] * (1.0f / ORTHO_LO_SCALE);
+                for (int k = 0; k < 16; ++k) in[k] += rest[k];
             }
             tmem_wait_load();
-#pragma unroll
-            for (int k = 0; k < 16; ++k) w[k] = linear * in[k] + w[k] * (1.0f / BS);
+            update(w, in, linear);
             uint32_t h[8];
             if (last) {
 #pragma unroll
@@ -887,10 +953,7 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
                 if (lo_out) {
                     uint32_t l[8];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const float2 kept = __half22float2(*reinterpret_cast<const __half2 *>(&h[k]));
-                        l[k] = half_pair((w[2 * k] - kept.x) * ORTHO_LO_SCALE, (w[2 * k + 1] - kept.y) * ORTHO_LO_SCALE);
-                    }
+                    for (int k = 0; k < 8; ++k) l[k] = rest_pair(w[2 * k], w[2 * k + 1], h[k]);
 #pragma unroll
                     for (int i = 0; i < 2; ++i) store_shared(box_octet(lo + at, r, o + i), make_uint4(l[4 * i], l[4 * i + 1], l[4 * i + 2], l[4 * i + 3]));
                 }

@@ -9,11 +9,10 @@
 // start near 1 / n and end near 1 / sqrt(n), those of A near n^-1.5: unscaled they would fall below fp16's normal
 // numbers (6e-5) from n = 128 on.  In magnitude X may reach 255, A 15, B 63.
 constexpr float ORTHO_X_SCALE = 256.0f, ORTHO_A_SCALE = 4096.0f, ORTHO_B_SCALE = 1024.0f;
-// What rounding X to fp16 leaves behind, times 2^11, is kept beside X for the term a X of the first steps.  There the
+// What rounding X to fp16 leaves behind is kept beside X, in fp16 too, for the term a X of the first steps.  There the
 // rounding error of the large singular values is as large as small ones and grows with them: for singular values
 // falling as 1 / i (512 x 512) five steps end 3.3e-3 off without, 1.9e-3 with two steps of it, 1.8e-3 with three (of which
 // 1.7e-3 is the result's rounding to bf16); from the fourth on it gains nothing.
-constexpr float ORTHO_LO_SCALE = 2048.0f;
 constexpr uint32_t ORTHO_LO_STEPS = 3;
 
 struct OrthoView {
