@@ -40,24 +40,33 @@ __device__ __forceinline__ double octet_squares(const float (&v)[8])
     for (int k = 0; k < 8; ++k) sum = fmaf(v[k] * p, v[k] * p, sum);
     return (double)sum * __longlong_as_double((long long)(2 * e + 1023) << 52);
 }
-// What an element of G is multiplied by to become one of X as it is kept: three factors, of which two are powers of two that
-// together bring the norm next to 1, since the quotient may not be a 32-bit number where its product with G's elements is.
+// What an element of G is multiplied by to become one of X as it is kept: f, after p where that is not 1 (a power of two, since
+// the quotient may not be a 32-bit number where its product with G's elements is).  f = 0: a matrix of zeros, or not finite.
 struct Normalise {
-    float f, p, q;
+    float f, p;
 };
 __device__ __forceinline__ Normalise normalise(double squares)
 {
-    Normalise n = {0.0f, 0.0f, 0.0f};
+    Normalise n = {0.0f, 1.0f};
     if (squares > 0.0 && squares <= 1.7976931348623157e308) {
-        const double norm = sqrt(squares);
-        const int e = (int)(__double_as_longlong(norm) >> 52) - 1023, half = e / 2;   // |e| < 200
-        n.p = power_of_two(-half);
-        n.q = power_of_two(half - e);
-        n.f = (float)((double)ORTHO_X_SCALE / (norm * __longlong_as_double((long long)(1023 - e) << 52)));
+        double norm = sqrt(squares);
+        const int e = (int)(__double_as_longlong(norm) >> 52) - 1023;   // |e| < 200
+        if (e < -100 || e > 100) {
+            n.p = e < 0 ? 0x1p100f : 0x1p-100f;
+            norm *= (double)n.p;
+        }
+        n.f = (float)((double)ORTHO_X_SCALE / norm);
     }
     return n;
 }
-__device__ __forceinline__ float times(float g, const Normalise &n) { return n.f == 0.0f ? 0.0f : g * n.p * n.q * n.f; }
+__device__ __forceinline__ void times(float (&v)[8], const Normalise &n)
+{
+    if (n.p != 1.0f)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] *= n.p;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = n.f == 0.0f ? 0.0f : v[k] * n.f;
+}
 
 // Sum of the squares of a part of a matrix.
 template <typename T>
@@ -137,8 +146,7 @@ __global__ __launch_bounds__(THREADS) void qesgd_ortho_start_kernel(const T *x, 
             const uint32_t r = n / octets, c = n % octets * 8;
             float f[8];
             load_octet(m + r * ldx, c, cols, vec, f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = times(f[j], scale);
+            times(f, scale);
             store_terms(f, hi + r * v.ld + c, lo + r * v.ld + c);
         }
         return;
@@ -149,7 +157,7 @@ __global__ __launch_bounds__(THREADS) void qesgd_ortho_start_kernel(const T *x, 
         for (uint32_t i = threadIdx.x; i < 64 * 64; i += THREADS) {
             const uint32_t r = r0 + i / 64, c = c0 + i % 64;
             const float g = r < rows && c < cols ? to_float(m[r * ldx + c]) : 0.0f;
-            held[i / 64 * 65 + i % 64] = times(g, scale);
+            held[i / 64 * 65 + i % 64] = g;
         }
         __syncthreads();
         for (uint32_t i = threadIdx.x; i < 64 * 8; i += THREADS) {
@@ -158,6 +166,7 @@ __global__ __launch_bounds__(THREADS) void qesgd_ortho_start_kernel(const T *x, 
                 float f[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) f[j] = held[(i % 8 * 8 + j) * 65 + i / 8];
+                times(f, scale);
                 store_terms(f, hi + c * v.ld + r, lo + c * v.ld + r);
             }
         }
@@ -722,8 +731,7 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
         const uint32_t n = threadIdx.x + i * WHOLE_THREADS, line = n / octets, first = n % octets * 8;
         if (n >= WHOLE_ROWS * a.width / 8) break;
         uint32_t h[4], l[4];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[i][k] = times(v[i][k], scale);
+        times(v[i], scale);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             h[k] = half_pair(v[i][2 * k], v[i][2 * k + 1]);
@@ -760,7 +768,10 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
         __syncthreads();
         fence_after_sync();
     };
-    constexpr uint32_t SQUARE = 1u << 4 | (128u / 8) << 17 | (128u / 16) << 24;
+    // rows of X in whole products, columns of A in whole loads; what lies behind them in tensor memory is not looked at
+    const uint32_t rows = (a.m + 15u) / 16u * 16u;
+    const bool idle = quarter * 32u >= rows;
+    const uint32_t square = 1u << 4 | (rows / 8) << 17 | (128u / 16) << 24;
     for (uint32_t step = 0; step < a.steps; ++step) {
         const bool last = step + 1 == a.steps, lo_in = step < ORTHO_LO_STEPS, lo_out = step + 1 < ORTHO_LO_STEPS;
         // ---- A = X X^T ----
@@ -769,14 +780,14 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
 #pragma unroll
                 for (uint32_t i = 0; i < 4; ++i) {
                     const uint64_t x = swizzled_matrix(hi + b * BOX_BYTES + i * 32u, 16u, 1024u);
-                    mma_f16<false>(tmem + A_COLUMN, x, x, SQUARE, b > 0 || i > 0);
+                    mma_f16<false>(tmem + A_COLUMN, x, x, square, b > 0 || i > 0);
                 }
             mma_commit<false>(bar);
         }
         __syncwarp();
         products_done();
 #pragma unroll 1
-        for (uint32_t c = part * 32u; c < part * 32u + 32u; c += 16u) {
+        for (uint32_t c = part * 16u; c < rows && !idle; c += 64u) {
             float w[16];
             __syncwarp();
             tmem_load16(tmem + (quarter * 32u << 16) + A_COLUMN + c, w);
@@ -804,9 +815,9 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
         if (CLUSTER) {
             __syncwarp();
             cluster_sync_all();
-            const uint32_t mine = 16u / cluster;   // octets of columns
+            // octets of columns, dealt out to the CTAs in turn
             const uint32_t row = threadIdx.x % 128u;
-            for (uint32_t o = rank * mine + threadIdx.x / 128u; o < (rank + 1) * mine; o += WHOLE_THREADS / 128u) {
+            for (uint32_t o = rank + cluster * (threadIdx.x / 128u); o < rows / 8u && row < rows; o += cluster * (WHOLE_THREADS / 128u)) {
                 float w[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
                 for (uint32_t p0 = 0; p0 < share; p0 += 4) {   // CTAs behind the last column have nothing to add
                     float4 q[4][2];
@@ -854,10 +865,9 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
         }
         // ---- B = b A + c A A ----
         if (warp == 0 && elect_one()) {
-#pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) {
+            for (uint32_t i = 0; i < rows / 16u; ++i) {
                 const uint64_t x = swizzled_matrix(f + i / 4 * BOX_BYTES + i % 4 * 32u, 16u, 1024u);
-                mma_f16<false>(tmem + P_COLUMN, x, x, SQUARE, i > 0);
+                mma_f16<false>(tmem + P_COLUMN, x, x, square, i > 0);
             }
             mma_commit<false>(bar);
         }
@@ -867,7 +877,7 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
             const float dr = load_shared_float(d + r * 4u);
             const float s2 = a.cc * BS / (AS * AS), s1 = a.cc * BS / AS, s0 = a.cb * BS / AS + s1 * dr;
 #pragma unroll 1
-            for (uint32_t c = part * 32u; c < part * 32u + 32u; c += 16u) {
+            for (uint32_t c = part * 16u; c < rows && !idle; c += 64u) {
                 float w[16], in[16];
                 __syncwarp();
                 tmem_load16(tmem + (quarter * 32u << 16) + P_COLUMN + c, w);
@@ -900,8 +910,7 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
         // ---- X' = a X + B X ----
         if (warp == 0 && elect_one()) {
             const uint32_t instruction = 1u << 4 | 1u << 16 | (a.width / 8) << 17 | (128u / 16) << 24;
-#pragma unroll
-            for (uint32_t i = 0; i < 8; ++i)
+            for (uint32_t i = 0; i < rows / 16u; ++i)
                 mma_f16<false>(tmem + U_COLUMN, swizzled_matrix(f + i / 4 * BOX_BYTES + i % 4 * 32u, 16u, 1024u), swizzled_matrix(hi + i * 2048u, BOX_BYTES, 1024u),
                                instruction, i > 0);
             mma_commit<false>(bar);
@@ -910,7 +919,7 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
         products_done();
         const float linear = a.ca + load_shared_float(db + r * 4u);
 #pragma unroll 1
-        for (uint32_t c = part * 16u; c < a.width; c += 64u) {
+        for (uint32_t c = part * 16u; c < a.width && !idle; c += 64u) {
             float w[16], in[16];
             __syncwarp();
             tmem_load16(tmem + (quarter * 32u << 16) + U_COLUMN + c, w);
