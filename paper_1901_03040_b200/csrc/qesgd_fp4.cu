@@ -89,27 +89,27 @@ __device__ __forceinline__ Scale block_scale(uint32_t top, float to_tensor)
 }
 // x over the block's scale, correctly rounded.  NV: the quotient by the rounded reciprocal, corrected by its residual; s has
 // 4 significant bits, so a quotient lies on a rounding border or at least 2^-5 units in the last place from it, far
-// more than the correction is off.
-template <int FORMAT>
+// more than the correction is off.  SCALED: there is a tensor exponent, and x * 2^-t may leave the float range; an
+// infinite quotient is clipped to 6 either way.
+template <int FORMAT, bool SCALED>
 __device__ __forceinline__ float over_scale(float x, const Scale &s)
 {
-    const float y = __fmul_rn(x, s.mul);
-    if (FORMAT == QESGD_FP4_MX) return y;
+    if (FORMAT == QESGD_FP4_MX) return __fmul_rn(x, s.mul);
+    const float y = SCALED ? __fmul_rn(x, s.mul) : x;
     const float q = __fmul_rn(y, s.inv);
     const float r = __fmaf_rn(__fmaf_rn(-q, s.div, y), s.inv, q);
-    return fabsf(q) < 3.402823466e38f ? r : q;   // beyond the float range: clipped to 6 either way
+    return !SCALED || fabsf(q) < 3.402823466e38f ? r : q;
 }
 
 // Eight elements of one block -> their codes.
-template <int FORMAT, bool STOCHASTIC>
+template <int FORMAT, bool SCALED, bool STOCHASTIC>
 __device__ __forceinline__ uint32_t quantize_octet(const float (&v)[8], const Scale &s, const uint32_t (&draw)[4])
 {
     uint32_t w = 0u;
-    if (s.mul == 0.0f) return 0u;
     if (!STOCHASTIC) {
         float q[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] = over_scale<FORMAT>(v[j], s);
+        for (int j = 0; j < 8; ++j) q[j] = over_scale<FORMAT, SCALED>(v[j], s);
         asm("{\n"
             ".reg .b8 b0, b1, b2, b3;\n"
             "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n"
@@ -120,22 +120,26 @@ __device__ __forceinline__ uint32_t quantize_octet(const float (&v)[8], const Sc
             "}\n"
             : "=r"(w)
             : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]), "f"(q[4]), "f"(q[5]), "f"(q[6]), "f"(q[7]));
-        // a zero has no sign: the top bit of a half stays where its level is 1 at least
-        return w & (0x77777777u | ((w & 0x77777777u) + 0x77777777u));
-    }
+    } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        // the grid is linear between 0 and 2 (steps of 1/2), 2 and 4 (1), 4 and 6 (2): h counts steps, exactly
-        const float q = fminf(fabsf(over_scale<FORMAT>(v[j], s)), 6.0f);
-        const float h = __fmul_rn(q, q < 2.0f ? 2.0f : q < 4.0f ? 1.0f : 0.5f);
-        const float below = floorf(h);
-        const uint32_t u = (draw[j / 2] >> (16 * (j % 2))) & 0xFFFFu;
-        // u's value (u + 1/2) / 2^16 against the rest h - below, both times 2^17 and then exact
-        const uint32_t up = (float)(2u * u + 1u) < __fmul_rn(h - below, 131072.0f) ? 1u : 0u;
-        const uint32_t level = (uint32_t)below + (q < 2.0f ? 0u : q < 4.0f ? 2u : 4u) + up;
-        w |= (level | (v[j] < 0.0f && level ? 8u : 0u)) << (4 * j);
+        for (int j = 0; j < 8; ++j) {
+            const float x = over_scale<FORMAT, SCALED>(v[j], s);
+            const float q = FORMAT == QESGD_FP4_MX ? fabsf(x) : fminf(fabsf(x), 6.0f);   // MX: never above 6
+            // The grid's steps are 1/2 below 2, 1 below 4 and 2 above: with e = 0, 1, 2 q counts h = q 2^(1-e) steps, exactly,
+            // behind 2 e levels.  The level is h's integer part, and one more where the draw's u = (2 k + 1) / 2^17 is below the
+            // rest: the least integer not below h - u.  Rounding upwards never passes an integer, so neither h - u nor the sum
+            // that leaves that integer in the low bits of 1.5 * 2^23 needs to be exact.
+            const uint32_t eb = __float_as_uint(fmaxf(q, 1.0f)) & 0x7F800000u;
+            const uint32_t k = j % 2 ? (draw[j / 2] >> 9) & 0x7FFF80u : (draw[j / 2] << 7) & 0x7FFF80u;
+            const float minus_u = __fsub_rn(1.0f, __uint_as_float(0x3F800040u | k));
+            const float up = __fadd_ru(__fmaf_ru(q, __uint_as_float(0x7F800000u - eb), minus_u), 12582912.0f);
+            w |= ((__float_as_uint(up) + (eb >> 22) - 254u) & 7u) << (4 * j);   // eb >> 22 is 2 (127 + e)
+            w |= (__float_as_uint(v[j]) & 0x80000000u) >> (28 - 4 * j);
+        }
     }
-    return w;
+    // a zero has no sign: the top bit of a half stays where its level is 1 at least
+    w &= 0x77777777u | ((w & 0x77777777u) + 0x77777777u);
+    return s.mul == 0.0f ? 0u : w;
 }
 
 // Byte of (row, block) within the tiles that a CTA keeps in shared memory, one after another along the blocks.
@@ -144,21 +148,19 @@ __device__ __forceinline__ uint32_t scale_slot(uint32_t row, uint32_t block)
     return block / 4u * SCALE_TILE + (row % 32u) * 16u + (row / 32u) * 4u + block % 4u;
 }
 
+// The largest magnitude of the block that an octet is part of.
 template <int FORMAT>
-__device__ __forceinline__ uint32_t block_top(const float (&v)[8])
+__device__ __forceinline__ uint32_t over_block(uint32_t top)
 {
-    uint32_t top = 0u;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7FFFFFFFu);
     top = max(top, __shfl_xor_sync(FULL, top, 1));
     if (FORMAT == QESGD_FP4_MX) top = max(top, __shfl_xor_sync(FULL, top, 2));
     return top;
 }
 
 // ------------------------------------------------------- blocks along rows ----
-constexpr int ROW_COLS = 256;   // columns of a CTA's tile: a warp takes one row at a time
+constexpr int ROW_COLS = 128;   // columns of a CTA's tile: a warp takes two rows at a time
 
-template <typename T, int FORMAT, bool STOCHASTIC>
+template <typename T, int FORMAT, bool SCALED, bool STOCHASTIC>
 __global__ __launch_bounds__(THREADS) void qesgd_fp4_quantize_rows_kernel(const __grid_constant__ Fp4QuantizeArgs a)
 {
     constexpr int BLOCK = Format<FORMAT>::BLOCK;
@@ -166,49 +168,54 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_quantize_rows_kernel(const 
     constexpr int UNROLL = 4;
     __shared__ __align__(16) uint8_t scales[TILE_ROWS * BLOCKS];
     qesgd_wait_for_previous();
-    const uint32_t lane = threadIdx.x % 32u, warp = threadIdx.x / 32u;
-    const uint64_t col_tiles = (a.cols + ROW_COLS - 1) / ROW_COLS;
-    const uint64_t tiles = col_tiles * ((a.rows + TILE_ROWS - 1) / TILE_ROWS);
+    if (a.small) qesgd_let_next_start();
+    const uint32_t o = threadIdx.x % 16u, line = threadIdx.x / 16u;
+    const uint32_t col_tiles = (uint32_t)((a.cols + ROW_COLS - 1) / ROW_COLS);
+    const uint64_t tiles = (uint64_t)col_tiles * ((a.rows + TILE_ROWS - 1) / TILE_ROWS);
     const uint64_t padded = (a.cols + 31) / 32 * 32;
     const uint64_t scale_tiles = (a.cols + 4 * BLOCK - 1) / (4 * BLOCK);
-    const float to_tensor = power_of_two(-tensor_exponent(a.tensor_exponent));
+    const float to_tensor = SCALED ? power_of_two(-tensor_exponent(a.tensor_exponent)) : 1.0f;
     bool bad = false;
     for (uint64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const uint64_t row0 = tile / col_tiles * TILE_ROWS, col0 = tile % col_tiles * ROW_COLS;
+        const uint64_t row0 = tile / col_tiles * TILE_ROWS;
+        const uint32_t col0 = (uint32_t)(tile % col_tiles) * ROW_COLS;
         const uint32_t rows = (uint32_t)min((uint64_t)TILE_ROWS, a.rows - row0);
         if (rows < TILE_ROWS) {
             for (uint32_t i = threadIdx.x; i < sizeof(scales) / 4; i += THREADS) reinterpret_cast<uint32_t *>(scales)[i] = 0u;
             __syncthreads();
         }
-        const uint64_t c = col0 + lane * 8u;
-        for (uint32_t r0 = warp; r0 < rows; r0 += THREADS / 32 * UNROLL) {
-            float v[UNROLL][8];
+        const uint64_t c = col0 + o * 8u;
+        const T *const first = static_cast<const T *>(a.x) + row0 * a.ldx;
+        uint8_t *const codes = a.codes + (row0 * padded + c) / 2;
+#pragma unroll 1
+        for (uint32_t r0 = line; r0 < (rows + 1u) / 2u * 2u; r0 += THREADS / 16 * UNROLL) {   // both halves of a warp stay together
+            Octet<T> x[UNROLL];
 #pragma unroll
             for (int i = 0; i < UNROLL; ++i) {
-                const uint32_t r = r0 + i * (THREADS / 32);
-                if (r < rows) load_octet(static_cast<const T *>(a.x) + (row0 + r) * a.ldx, c, a.cols, a.vec, v[i]);
-                else
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
+                const uint32_t r = r0 + i * (THREADS / 16);
+                x[i] = r < rows ? load_octet(first + r * a.ldx, c, a.cols, a.vec) : no_octet<T>();
             }
 #pragma unroll
             for (int i = 0; i < UNROLL; ++i) {
-                const uint32_t r = r0 + i * (THREADS / 32);
-                if (r >= rows) break;
-                const uint32_t top = block_top<FORMAT>(v[i]);
+                const uint32_t r = r0 + i * (THREADS / 16);
+                const uint32_t top = over_block<FORMAT>(top_of(x[i]));
+                if (r >= rows) continue;
                 bad |= top >= 0x7F800000u;
                 const Scale s = block_scale<FORMAT>(top, to_tensor);
                 uint32_t draw[4] = {0u, 0u, 0u, 0u};
                 if (STOCHASTIC) draws_of(((row0 + r) * padded + c) / 8, a, draw);
-                const uint32_t w = quantize_octet<FORMAT, STOCHASTIC>(v[i], s, draw);
-                if (c < padded) *reinterpret_cast<uint32_t *>(a.codes + ((row0 + r) * padded + c) / 2) = w;
-                if (lane % (BLOCK / 8) == 0) scales[scale_slot(r, lane / (BLOCK / 8))] = (uint8_t)s.byte;
+                float v[8];
+                values(x[i], v);
+                const uint32_t w = quantize_octet<FORMAT, SCALED, STOCHASTIC>(v, s, draw);
+                if (c < padded) *reinterpret_cast<uint32_t *>(codes + r * (padded / 2)) = w;
+                if (o % (BLOCK / 8) == 0) scales[scale_slot(r, o / (BLOCK / 8))] = (uint8_t)s.byte;
             }
+            __syncwarp();
         }
         __syncthreads();
-        const uint64_t first = col0 / (4 * BLOCK);
-        const uint32_t have = (uint32_t)min((uint64_t)(BLOCKS / 4), scale_tiles - first);
-        uint4 *out = reinterpret_cast<uint4 *>(a.scales + (row0 / TILE_ROWS * scale_tiles + first) * SCALE_TILE);
+        const uint64_t at = col0 / (4 * BLOCK);
+        const uint32_t have = (uint32_t)min((uint64_t)(BLOCKS / 4), scale_tiles - at);
+        uint4 *out = reinterpret_cast<uint4 *>(a.scales + (row0 / TILE_ROWS * scale_tiles + at) * SCALE_TILE);
         for (uint32_t i = threadIdx.x; i < have * (SCALE_TILE / 16); i += THREADS) out[i] = reinterpret_cast<const uint4 *>(scales)[i];
         __syncthreads();
     }
@@ -218,83 +225,120 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_quantize_rows_kernel(const 
 // ------------------------------- blocks along columns, or along both axes ----
 constexpr int SIDE = 128;   // a CTA's tile: whole tiles of scales for either axis
 
-template <typename T, int FORMAT, bool STOCHASTIC>
+// The tile goes through shared memory as it is.  Then a thread takes two neighbouring columns of 32 rows: one load for both
+// where elements have 16 bits, whole blocks without an exchange, and 16 bytes of codes for each column.
+template <typename T, int FORMAT, bool SCALED, bool STOCHASTIC>
 __global__ __launch_bounds__(THREADS) void qesgd_fp4_quantize_columns_kernel(const __grid_constant__ Fp4QuantizeArgs a)
 {
     constexpr int BLOCK = Format<FORMAT>::BLOCK;
     constexpr int BLOCKS = SIDE / BLOCK;
-    constexpr int PITCH = SIDE + 4 / (int)sizeof(T);   // elements between rows in shared memory
-    extern __shared__ __align__(16) uint8_t smem[];
-    T *const held = reinterpret_cast<T *>(smem);
+    constexpr uint32_t PITCH = SIDE * sizeof(T);       // bytes of a row in shared memory
+    extern __shared__ __align__(16) uint8_t held[];
     __shared__ __align__(16) uint8_t scales[2][SIDE * BLOCKS];
     qesgd_wait_for_previous();
-    const uint64_t col_tiles = (a.cols + SIDE - 1) / SIDE;
-    const uint64_t tiles = col_tiles * ((a.rows + SIDE - 1) / SIDE);
+    if (a.small) qesgd_let_next_start();
+    const uint32_t col_tiles = (uint32_t)((a.cols + SIDE - 1) / SIDE);
+    const uint64_t tiles = (uint64_t)col_tiles * ((a.rows + SIDE - 1) / SIDE);
     const uint64_t padded = (a.cols + 31) / 32 * 32, padded_t = (a.rows + 31) / 32 * 32;
     const uint64_t scale_tiles = (a.cols + 4 * BLOCK - 1) / (4 * BLOCK), scale_tiles_t = (a.rows + 4 * BLOCK - 1) / (4 * BLOCK);
-    const float to_tensor = power_of_two(-tensor_exponent(a.tensor_exponent));
+    const float to_tensor = SCALED ? power_of_two(-tensor_exponent(a.tensor_exponent)) : 1.0f;
     bool bad = false;
     for (uint64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const uint64_t row0 = tile / col_tiles * SIDE, col0 = tile % col_tiles * SIDE;
-        // every row and column of the tile goes the whole way, as zeros past the matrix's edge: then padding bytes are zeros
-        for (uint32_t i = threadIdx.x / 16u; i < SIDE; i += THREADS / 16) {
-            const uint32_t o = threadIdx.x % 16u;
-            const uint64_t r = row0 + i, c = col0 + o * 8u;
-            float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-            if (r < a.rows) load_octet(static_cast<const T *>(a.x) + r * a.ldx, c, a.cols, a.vec, v);
+        {
+            // every row and column of the tile goes the whole way, as zeros past the matrix's edge: then padding bytes are zeros
+            constexpr int UNROLL = 4;
+            const uint32_t o = threadIdx.x % 16u, line = threadIdx.x / 16u;
+            const uint64_t c = col0 + o * 8u;
+#pragma unroll 1
+            for (uint32_t i0 = line; i0 < SIDE; i0 += THREADS / 16 * UNROLL) {
+                Octet<T> x[UNROLL];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) held[i * PITCH + o * 8u + j] = (T)v[j];
-            if (a.codes) {
-                const uint32_t top = block_top<FORMAT>(v);
-                bad |= top >= 0x7F800000u;
-                const Scale s = block_scale<FORMAT>(top, to_tensor);
-                uint32_t draw[4] = {0u, 0u, 0u, 0u};
-                if (STOCHASTIC) draws_of((r * padded + c) / 8, a, draw);
-                const uint32_t w = quantize_octet<FORMAT, STOCHASTIC>(v, s, draw);
-                if (r < a.rows && c < padded) *reinterpret_cast<uint32_t *>(a.codes + (r * padded + c) / 2) = w;
-                if (o % (BLOCK / 8) == 0) scales[0][scale_slot(i, o / (BLOCK / 8))] = (uint8_t)s.byte;
+                for (int n = 0; n < UNROLL; ++n) {
+                    const uint64_t r = row0 + i0 + n * (THREADS / 16);
+                    x[n] = r < a.rows ? load_octet(static_cast<const T *>(a.x) + r * a.ldx, c, a.cols, a.vec) : no_octet<T>();
+                }
+#pragma unroll
+                for (int n = 0; n < UNROLL; ++n) {
+                    const uint32_t i = i0 + n * (THREADS / 16);
+#pragma unroll
+                    for (int k = 0; k < Octet<T>::WORDS / 4; ++k)
+                        *reinterpret_cast<uint4 *>(held + i * PITCH + o * 8u * sizeof(T) + k * 16) = *reinterpret_cast<const uint4 *>(&x[n].w[4 * k]);
+                    if (a.codes) {
+                        const uint64_t r = row0 + i;
+                        const uint32_t top = over_block<FORMAT>(top_of(x[n]));
+                        bad |= top >= 0x7F800000u;
+                        const Scale s = block_scale<FORMAT>(top, to_tensor);
+                        uint32_t draw[4] = {0u, 0u, 0u, 0u};
+                        if (STOCHASTIC) draws_of((r * padded + c) / 8, a, draw);
+                        float v[8];
+                        values(x[n], v);
+                        const uint32_t w = quantize_octet<FORMAT, SCALED, STOCHASTIC>(v, s, draw);
+                        if (r < a.rows && c < padded) *reinterpret_cast<uint32_t *>(a.codes + (r * padded + c) / 2) = w;
+                        if (o % (BLOCK / 8) == 0) scales[0][scale_slot(i, o / (BLOCK / 8))] = (uint8_t)s.byte;
+                    }
+                }
             }
         }
         __syncthreads();
         {
-            // a thread takes half a column: 64 elements, 32 bytes of codes
-            const uint32_t k = threadIdx.x % SIDE, half = threadIdx.x / SIDE;
-            const uint64_t c = col0 + k;
-#pragma unroll 1
-            for (uint32_t b = 0; b < 64 / 32; ++b) {
-                const uint32_t i0 = half * 64u + b * 32u;
-                uint32_t words[4];
+            const uint32_t k = threadIdx.x % (SIDE / 2) * 2u, i0 = threadIdx.x / (SIDE / 2) * 32u;
+            uint32_t words[2][4];
 #pragma unroll
-                for (int g = 0; g < 32 / BLOCK; ++g) {
-                    float v[BLOCK / 8][8];
-                    uint32_t top = 0u;
+            for (int g = 0; g < 32 / BLOCK; ++g) {
+                float v[2][BLOCK];
+                uint32_t top[2] = {0u, 0u}, both = 0u;
 #pragma unroll
-                    for (int o = 0; o < BLOCK / 8; ++o)
+                for (int j = 0; j < BLOCK; ++j) {
+                    const uint8_t *const p = held + (i0 + g * BLOCK + j) * PITCH + k * sizeof(T);
+                    if constexpr (sizeof(T) == 4) {
+                        const uint2 w = *reinterpret_cast<const uint2 *>(p);
+                        v[0][j] = __uint_as_float(w.x);
+                        v[1][j] = __uint_as_float(w.y);
+                        top[0] = max(top[0], w.x & 0x7FFFFFFFu);
+                        top[1] = max(top[1], w.y & 0x7FFFFFFFu);
+                    } else {
+                        const uint32_t w = *reinterpret_cast<const uint32_t *>(p);
+                        const float2 f = pair_of(w, T());
+                        v[0][j] = f.x;
+                        v[1][j] = f.y;
+                        both = __vmaxu2(both, w & 0x7FFF7FFFu);
+                    }
+                }
+                if constexpr (sizeof(T) == 2) {
+                    top[0] = top16<T>(both & 0xFFFFu);
+                    top[1] = top16<T>(both >> 16);
+                }
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            v[o][j] = to_float(held[(i0 + g * BLOCK + o * 8 + j) * PITCH + k]);
-                            top = max(top, __float_as_uint(v[o][j]) & 0x7FFFFFFFu);
-                        }
-                    bad |= top >= 0x7F800000u;
-                    const Scale s = block_scale<FORMAT>(top, to_tensor);
+                for (int n = 0; n < 2; ++n) {
+                    const uint64_t c = col0 + k + n;
+                    bad |= top[n] >= 0x7F800000u;
+                    const Scale s = block_scale<FORMAT>(top[n], to_tensor);
 #pragma unroll
                     for (int o = 0; o < BLOCK / 8; ++o) {
                         uint32_t draw[4] = {0u, 0u, 0u, 0u};
                         if (STOCHASTIC) draws_of((c * padded_t + row0 + i0 + g * BLOCK + o * 8) / 8, a, draw);
-                        words[g * (BLOCK / 8) + o] = quantize_octet<FORMAT, STOCHASTIC>(v[o], s, draw);
+                        float e[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) e[j] = v[n][o * 8 + j];
+                        words[n][g * (BLOCK / 8) + o] = quantize_octet<FORMAT, SCALED, STOCHASTIC>(e, s, draw);
                     }
-                    scales[1][scale_slot(k, (i0 + g * BLOCK) / BLOCK)] = (uint8_t)s.byte;
+                    scales[1][scale_slot(k + n, (i0 + g * BLOCK) / BLOCK)] = (uint8_t)s.byte;
                 }
+            }
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const uint64_t c = col0 + k + n;
                 if (c < a.cols && row0 + i0 < padded_t)
-                    *reinterpret_cast<uint4 *>(a.codes_t + (c * padded_t + row0 + i0) / 2) = make_uint4(words[0], words[1], words[2], words[3]);
+                    *reinterpret_cast<uint4 *>(a.codes_t + (c * padded_t + row0 + i0) / 2) = make_uint4(words[n][0], words[n][1], words[n][2], words[n][3]);
             }
         }
         __syncthreads();
         for (int side = a.codes ? 0 : 1; side < 2; ++side) {
             const uint64_t all = side ? scale_tiles_t : scale_tiles;
-            const uint64_t first = (side ? row0 : col0) / (4 * BLOCK), at = (side ? col0 : row0) / TILE_ROWS;
-            const uint32_t have = (uint32_t)min((uint64_t)(BLOCKS / 4), all - first);
-            uint4 *out = reinterpret_cast<uint4 *>((side ? a.scales_t : a.scales) + (at * all + first) * SCALE_TILE);
+            const uint64_t at = (side ? row0 : col0) / (4 * BLOCK), line = (side ? col0 : row0) / TILE_ROWS;
+            const uint32_t have = (uint32_t)min((uint64_t)(BLOCKS / 4), all - at);
+            uint4 *out = reinterpret_cast<uint4 *>((side ? a.scales_t : a.scales) + (line * all + at) * SCALE_TILE);
             for (uint32_t i = threadIdx.x; i < have * (SCALE_TILE / 16); i += THREADS) out[i] = reinterpret_cast<const uint4 *>(scales[side])[i];
         }
         __syncthreads();
@@ -324,35 +368,74 @@ __device__ __forceinline__ float scale_value(uint32_t byte)
     return __fmul_rn(__uint_as_float((byte & 0x7Fu) << 20), 0x1p120f);
 }
 
-template <typename T, int FORMAT>
+// A warp takes 256 columns of a row at a time: an octet for each lane where rows of `out` lie on 16 bytes, else neighbouring
+// elements in neighbouring lanes, so that stores of single elements fill whole sectors too.
+constexpr int BACK_ROWS = 32, BACK_COLS = 256;
+
+template <typename T, int FORMAT, bool VEC>
 __global__ __launch_bounds__(THREADS) void qesgd_fp4_dequantize_kernel(const __grid_constant__ Fp4DequantizeArgs a)
 {
     constexpr int BLOCK = Format<FORMAT>::BLOCK;
+    constexpr int UNROLL = 4;
     qesgd_wait_for_previous();
-    const uint64_t padded = (a.cols + 31) / 32 * 32;
-    const uint64_t scale_tiles = (a.cols + 4 * BLOCK - 1) / (4 * BLOCK);
-    const uint64_t octets = (a.cols + 7) / 8, all = octets * a.rows;
+    const uint32_t lane = threadIdx.x % 32u, warp = threadIdx.x / 32u;
+    const uint64_t padded = (a.cols + 31) / 32 * 32, scale_tiles = (a.cols + 4 * BLOCK - 1) / (4 * BLOCK);
+    const uint32_t col_tiles = (uint32_t)((a.cols + BACK_COLS - 1) / BACK_COLS);
+    const uint64_t tiles = (uint64_t)col_tiles * ((a.rows + BACK_ROWS - 1) / BACK_ROWS);
     const float tensor = power_of_two(tensor_exponent(a.tensor_exponent));
-    for (uint64_t n = (uint64_t)blockIdx.x * THREADS + threadIdx.x; n < all; n += (uint64_t)gridDim.x * THREADS) {
-        const uint64_t r = n / octets, c = n % octets * 8;
-        const uint64_t block = c / BLOCK;
-        const uint32_t byte = a.scales[(r / 128 * scale_tiles + block / 4) * SCALE_TILE + r % 32 * 16 + r / 32 % 4 * 4 + block % 4];
-        const float scale = scale_value<FORMAT>(byte);
-        const uint32_t w = *reinterpret_cast<const uint32_t *>(a.codes + (r * padded + c) / 2);
-        T v[8];
+    for (uint64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const uint64_t row0 = tile / col_tiles * BACK_ROWS;
+        const uint32_t col0 = (uint32_t)(tile % col_tiles) * BACK_COLS;
+        // within a tile of scales: rows differ by 16 bytes, BACK_ROWS of them by less than one quarter
+        const uint8_t *const scales = a.scales + row0 / 128 * scale_tiles * SCALE_TILE + row0 / 32 % 4 * 4;
+        static_assert(BACK_ROWS == 32, "a row of scales for each of the rows");
+        const uint32_t rows = (uint32_t)min((uint64_t)BACK_ROWS, a.rows - row0);
+        if (VEC) {
+            const uint64_t c = col0 + lane * 8u, block = c / BLOCK;
+            if (c >= a.cols) continue;
+            const uint8_t *const at = scales + block / 4 * SCALE_TILE + block % 4;
+            uint32_t w[UNROLL], byte[UNROLL];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float2 p = values_of((w >> (8 * j)) & 0xFFu);
-            v[2 * j] = from_float<T>(__fmul_rn(__fmul_rn(p.x, scale), tensor));
-            v[2 * j + 1] = from_float<T>(__fmul_rn(__fmul_rn(p.y, scale), tensor));
-        }
-        T *const out = static_cast<T *>(a.out) + r * a.ldo + c;
-        if (a.vec && c + 8 <= a.cols) {
+            for (int i = 0; i < UNROLL; ++i) {
+                const uint32_t r = warp + i * (THREADS / 32);
+                byte[i] = r < rows ? at[r * 16u] : 0u;
+                w[i] = r < rows ? *reinterpret_cast<const uint32_t *>(a.codes + ((row0 + r) * padded + c) / 2) : 0u;
+            }
 #pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(out)[i] = reinterpret_cast<const uint4 *>(v)[i];
+            for (int i = 0; i < UNROLL; ++i) {
+                const uint32_t r = warp + i * (THREADS / 32);
+                if (r >= rows) break;
+                const float scale = scale_value<FORMAT>(byte[i]);
+                __align__(16) T v[8];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float2 p = values_of((w[i] >> (8 * j)) & 0xFFu);
+                    v[2 * j] = from_float<T>(__fmul_rn(__fmul_rn(p.x, scale), tensor));
+                    v[2 * j + 1] = from_float<T>(__fmul_rn(__fmul_rn(p.y, scale), tensor));
+                }
+                T *const out = static_cast<T *>(a.out) + (row0 + r) * a.ldo + c;
+                if (c + 8 <= a.cols) {
+#pragma unroll
+                    for (int n = 0; n < (int)sizeof(T) / 2; ++n) reinterpret_cast<uint4 *>(out)[n] = reinterpret_cast<const uint4 *>(v)[n];
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (c + j < a.cols) out[j] = v[j];
+                }
+            }
         } else {
-            for (int j = 0; j < 8; ++j)
-                if (c + j < a.cols) out[j] = v[j];
+            for (uint32_t r = warp; r < rows; r += THREADS / 32) {
+                const uint8_t *const codes = a.codes + (row0 + r) * (padded / 2);
+                T *const out = static_cast<T *>(a.out) + (row0 + r) * a.ldo;
+#pragma unroll
+                for (uint32_t i = 0; i < BACK_COLS / 32; ++i) {
+                    const uint64_t c = col0 + i * 32u + lane, block = c / BLOCK;
+                    if (c >= a.cols) break;
+                    const float2 p = values_of(codes[c / 2]);
+                    const float scale = scale_value<FORMAT>(scales[block / 4 * SCALE_TILE + r * 16u + block % 4]);
+                    out[c] = from_float<T>(__fmul_rn(__fmul_rn(c % 2 ? p.y : p.x, scale), tensor));
+                }
+            }
         }
     }
 }
@@ -366,12 +449,16 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_tensor_exponent_kernel(cons
 {
     __shared__ uint32_t tops[THREADS / 32];
     qesgd_wait_for_previous();
-    const uint64_t octets = (cols + 7) / 8, all = octets * rows;
+    // a warp takes 256 columns of a row at a time
+    const uint32_t lane = threadIdx.x % 32u;
+    const uint32_t spans = (uint32_t)((cols + 255) / 256);
+    const uint64_t all = (uint64_t)spans * rows, warps = (uint64_t)gridDim.x * (THREADS / 32);
     uint32_t top = 0u;
     bool bad = false;
-    for (uint64_t n = (uint64_t)blockIdx.x * THREADS + threadIdx.x; n < all; n += (uint64_t)gridDim.x * THREADS) {
+    for (uint64_t n = (uint64_t)blockIdx.x * (THREADS / 32) + threadIdx.x / 32u; n < all; n += warps) {
+        const uint64_t c = n % spans * 256u + lane * 8u;
         float v[8];
-        load_octet(x + n / octets * ldx, n % octets * 8, cols, vec, v);
+        values(load_octet(x + n / spans * ldx, c, cols, vec), v);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const uint32_t m = __float_as_uint(v[j]) & 0x7FFFFFFFu;
@@ -391,41 +478,48 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_tensor_exponent_kernel(cons
     if (bad) atomicOr(status, QESGD_STATUS_NONFINITE);
 }
 
-template <typename T, int FORMAT, bool STOCHASTIC>
-cudaError_t launch_quantize(const Fp4QuantizeArgs &a, cudaStream_t stream)
+template <typename T, int FORMAT, bool SCALED, bool STOCHASTIC>
+cudaError_t launch_quantize(Fp4QuantizeArgs a, cudaStream_t stream)
 {
-    const uint64_t row_tiles = qesgd_div_up(a.rows, TILE_ROWS);
-    if (!a.codes_t) {
-        const uint64_t tiles = row_tiles * qesgd_div_up(a.cols, ROW_COLS);
-        return qesgd_launch(qesgd_fp4_quantize_rows_kernel<T, FORMAT, STOCHASTIC>, dim3((unsigned)(tiles < 0x7FFFFFFF ? tiles : 0x7FFFFFFF)), dim3(THREADS), stream, a);
-    }
-    const auto kernel = qesgd_fp4_quantize_columns_kernel<T, FORMAT, STOCHASTIC>;
-    const uint64_t tiles = row_tiles * qesgd_div_up(a.cols, SIDE);
-    const int smem = SIDE * (SIDE + 4 / (int)sizeof(T)) * (int)sizeof(T);
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != cudaSuccess) return e;
-    return qesgd_launch_smem(kernel, dim3((unsigned)(tiles < 0x7FFFFFFF ? tiles : 0x7FFFFFFF)), dim3(THREADS), smem, stream, a);
+    static_assert(ROW_COLS == SIDE, "tiles");
+    const uint64_t tiles = qesgd_div_up(a.rows, TILE_ROWS) * qesgd_div_up(a.cols, SIDE);
+    const dim3 grid((unsigned)(tiles < 0x7FFFFFFF ? tiles : 0x7FFFFFFF));
+    a.small = tiles <= 128;
+    if (!a.codes_t) return qesgd_launch(qesgd_fp4_quantize_rows_kernel<T, FORMAT, SCALED, STOCHASTIC>, grid, dim3(THREADS), stream, a);
+    const auto kernel = qesgd_fp4_quantize_columns_kernel<T, FORMAT, SCALED, STOCHASTIC>;
+    const int smem = SIDE * SIDE * (int)sizeof(T);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    return e != cudaSuccess ? e : qesgd_launch_smem(kernel, grid, dim3(THREADS), smem, stream, a);
+}
+template <typename T, bool STOCHASTIC>
+cudaError_t launch_quantize(const Fp4QuantizeArgs &a, uint32_t format, cudaStream_t stream)
+{
+    if (format == QESGD_FP4_MX) return launch_quantize<T, QESGD_FP4_MX, false, STOCHASTIC>(a, stream);
+    return a.tensor_exponent ? launch_quantize<T, QESGD_FP4_NV, true, STOCHASTIC>(a, stream) : launch_quantize<T, QESGD_FP4_NV, false, STOCHASTIC>(a, stream);
 }
 template <typename T>
 cudaError_t launch_quantize(const Fp4QuantizeArgs &a, uint32_t format, bool stochastic, cudaStream_t stream)
 {
-    if (format == QESGD_FP4_MX)
-        return stochastic ? launch_quantize<T, QESGD_FP4_MX, true>(a, stream) : launch_quantize<T, QESGD_FP4_MX, false>(a, stream);
-    return stochastic ? launch_quantize<T, QESGD_FP4_NV, true>(a, stream) : launch_quantize<T, QESGD_FP4_NV, false>(a, stream);
+    return stochastic ? launch_quantize<T, true>(a, format, stream) : launch_quantize<T, false>(a, format, stream);
+}
+template <typename T, int FORMAT>
+cudaError_t launch_dequantize(const Fp4DequantizeArgs &a, cudaStream_t stream)
+{
+    const uint64_t tiles = qesgd_div_up(a.cols, BACK_COLS) * qesgd_div_up(a.rows, BACK_ROWS);
+    const dim3 grid((unsigned)(tiles < 0x7FFFFFFF ? tiles : 0x7FFFFFFF));
+    return a.vec ? qesgd_launch(qesgd_fp4_dequantize_kernel<T, FORMAT, true>, grid, dim3(THREADS), stream, a)
+                 : qesgd_launch(qesgd_fp4_dequantize_kernel<T, FORMAT, false>, grid, dim3(THREADS), stream, a);
 }
 template <typename T>
 cudaError_t launch_dequantize(const Fp4DequantizeArgs &a, uint32_t format, cudaStream_t stream)
 {
-    const uint64_t ctas = qesgd_div_up(qesgd_div_up(a.cols, 8) * a.rows, THREADS);
-    const dim3 grid((unsigned)(ctas < 0x7FFFFFFF ? ctas : 0x7FFFFFFF));
-    if (format == QESGD_FP4_MX) return qesgd_launch(qesgd_fp4_dequantize_kernel<T, QESGD_FP4_MX>, grid, dim3(THREADS), stream, a);
-    return qesgd_launch(qesgd_fp4_dequantize_kernel<T, QESGD_FP4_NV>, grid, dim3(THREADS), stream, a);
+    return format == QESGD_FP4_MX ? launch_dequantize<T, QESGD_FP4_MX>(a, stream) : launch_dequantize<T, QESGD_FP4_NV>(a, stream);
 }
 template <typename T>
 cudaError_t launch_exponent(const void *x, uint64_t rows, uint64_t cols, uint64_t ldx, bool vec, int32_t *out, uint32_t *status,
                             int sm_count, cudaStream_t stream)
 {
-    const uint64_t ctas = qesgd_div_up(qesgd_div_up(cols, 8) * rows, THREADS), most = (uint64_t)sm_count * 8;
+    const uint64_t ctas = qesgd_div_up(qesgd_div_up(cols, 256) * rows, THREADS / 32 * 4), most = (uint64_t)sm_count * 8;
     return qesgd_launch(qesgd_fp4_tensor_exponent_kernel<T>, dim3((unsigned)(ctas < most ? ctas : most)), dim3(THREADS), stream,
                         static_cast<const T *>(x), rows, cols, ldx, vec, out, status);
 }

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(THREADS) void qesgd_ortho_norm_kernel(const T *x, u
     double sum = 0.0;
     for (uint32_t n = blockIdx.x * THREADS + threadIdx.x; n < all; n += gridDim.x * THREADS) {
         float v[8];
-        load_octet(m + n / octets * ldx, n % octets * 8, cols, vec, v);
+        values(load_octet(m + n / octets * ldx, n % octets * 8, cols, vec), v);
         sum += octet_squares(v);
     }
     sum = block_sum<THREADS>(sum);
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(THREADS) void qesgd_ortho_start_kernel(const T *x, 
         for (uint32_t n = blockIdx.x * THREADS + threadIdx.x; n < all; n += gridDim.x * THREADS) {
             const uint32_t r = n / octets, c = n % octets * 8;
             float f[8];
-            load_octet(m + r * ldx, c, cols, vec, f);
+            values(load_octet(m + r * ldx, c, cols, vec), f);
             times(f, scale);
             store_terms(f, hi + r * v.ld + c, lo + r * v.ld + c);
         }
@@ -702,8 +702,8 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
         const uint32_t n = threadIdx.x + i * WHOLE_THREADS, line = n / octets, first = n % octets * 8;   // line: row of X, or column
         const bool inside = n < WHOLE_ROWS * a.width / 8 && (a.turned ? c0 + line < a.n && first < a.m : line < a.m && c0 + first < a.n);
         if (inside) {
-            if (a.turned) load_octet(g + (c0 + line) * a.ldx, first, a.m, a.vec, v[i]);
-            else load_octet(g + line * a.ldx, c0 + first, a.n, a.vec, v[i]);
+            if (a.turned) values(load_octet(g + (c0 + line) * a.ldx, first, a.m, a.vec), v[i]);
+            else values(load_octet(g + line * a.ldx, c0 + first, a.n, a.vec), v[i]);
         }
         if (!inside)
 #pragma unroll
