@@ -121,21 +121,23 @@ __device__ __forceinline__ uint32_t quantize_octet(const float (&v)[8], const Sc
             : "=r"(w)
             : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]), "f"(q[4]), "f"(q[5]), "f"(q[6]), "f"(q[7]));
     } else {
+        // Behind q2 = max(q + 1, 2 q) (the first below 1, the second above) the grid is that of floats with one bit of mantissa,
+        // from 1.0 on: the level is what bits 22 and up of q2 count, and one more where the bits below, R / 2^22 of a step, are
+        // more than the draw's u = (2 k + 1) / 2^17: where R + 2^22 - 1 - 32 (2 k + 1) carries.  Both are integers, and q + 1,
+        // rounded upwards, compares with them as the exact sum does.  Times 64 the level stands in the top four bits (and a
+        // bit of the exponent with it), from which funnel shifts collect the word; 254 counts up to 1.0.
+        uint32_t signs = 0u;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float x = over_scale<FORMAT, SCALED>(v[j], s);
-            const float q = FORMAT == QESGD_FP4_MX ? fabsf(x) : fminf(fabsf(x), 6.0f);   // MX: never above 6
-            // The grid's steps are 1/2 below 2, 1 below 4 and 2 above: with e = 0, 1, 2 q counts h = q 2^(1-e) steps, exactly,
-            // behind 2 e levels.  The level is h's integer part, and one more where the draw's u = (2 k + 1) / 2^17 is below the
-            // rest: the least integer not below h - u.  Rounding upwards never passes an integer, so neither h - u nor the sum
-            // that leaves that integer in the low bits of 1.5 * 2^23 needs to be exact.
-            const uint32_t eb = __float_as_uint(fmaxf(q, 1.0f)) & 0x7F800000u;
-            const uint32_t k = j % 2 ? (draw[j / 2] >> 9) & 0x7FFF80u : (draw[j / 2] << 7) & 0x7FFF80u;
-            const float minus_u = __fsub_rn(1.0f, __uint_as_float(0x3F800040u | k));
-            const float up = __fadd_ru(__fmaf_ru(q, __uint_as_float(0x7F800000u - eb), minus_u), 12582912.0f);
-            w |= ((__float_as_uint(up) + (eb >> 22) - 254u) & 7u) << (4 * j);   // eb >> 22 is 2 (127 + e)
-            w |= (__float_as_uint(v[j]) & 0x80000000u) >> (28 - 4 * j);
+        for (int j = 7; j >= 0; --j) {
+            const float x = fabsf(over_scale<FORMAT, SCALED>(v[j], s));
+            const float q = FORMAT == QESGD_FP4_MX ? x : fminf(x, 6.0f);   // MX: never above 6
+            const float q2 = fmaxf(__fadd_ru(q, 1.0f), __fadd_rn(q, q));
+            const uint32_t k = j % 2 ? draw[j / 2] >> 16 : draw[j / 2] & 0xFFFFu;
+            const uint32_t t = __float_as_uint(q2) * 64u + ((((1u << 22) - 33u) - (254u << 22)) * 64u - k * 4096u);
+            w = __funnelshift_l(t, w, 4);
+            signs = __funnelshift_l(__float_as_uint(v[j]), signs, 4);
         }
+        w = (w & 0x77777777u) | (signs & 0x88888888u);
     }
     // a zero has no sign: the top bit of a half stays where its level is 1 at least
     w &= 0x77777777u | ((w & 0x77777777u) + 0x77777777u);
@@ -382,7 +384,9 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_dequantize_kernel(const __g
     const uint64_t padded = (a.cols + 31) / 32 * 32, scale_tiles = (a.cols + 4 * BLOCK - 1) / (4 * BLOCK);
     const uint32_t col_tiles = (uint32_t)((a.cols + BACK_COLS - 1) / BACK_COLS);
     const uint64_t tiles = (uint64_t)col_tiles * ((a.rows + BACK_ROWS - 1) / BACK_ROWS);
-    const float tensor = power_of_two(tensor_exponent(a.tensor_exponent));
+    // far exponents take two factors: their product with a scale may not be a 32-bit number
+    const int t = tensor_exponent(a.tensor_exponent);
+    const float near = t >= -100 && t <= 100 ? power_of_two(t) : 1.0f, far = t >= -100 && t <= 100 ? 1.0f : power_of_two(t);
     for (uint64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const uint64_t row0 = tile / col_tiles * BACK_ROWS;
         const uint32_t col0 = (uint32_t)(tile % col_tiles) * BACK_COLS;
@@ -393,27 +397,33 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_dequantize_kernel(const __g
         if (VEC) {
             const uint64_t c = col0 + lane * 8u, block = c / BLOCK;
             if (c >= a.cols) continue;
-            const uint8_t *const at = scales + block / 4 * SCALE_TILE + block % 4;
+            const uint8_t *const at = scales + block / 4 * SCALE_TILE + block % 4 + warp * 16u;
+            const uint8_t *const codes = a.codes + ((row0 + warp) * padded + c) / 2;
+            T *out = static_cast<T *>(a.out) + (row0 + warp) * a.ldo + c;
             uint32_t w[UNROLL], byte[UNROLL];
 #pragma unroll
             for (int i = 0; i < UNROLL; ++i) {
-                const uint32_t r = warp + i * (THREADS / 32);
-                byte[i] = r < rows ? at[r * 16u] : 0u;
-                w[i] = r < rows ? *reinterpret_cast<const uint32_t *>(a.codes + ((row0 + r) * padded + c) / 2) : 0u;
+                const bool inside = warp + i * (THREADS / 32) < rows;
+                byte[i] = inside ? at[i * (THREADS / 32) * 16] : 0u;
+                w[i] = inside ? *reinterpret_cast<const uint32_t *>(codes + i * (THREADS / 64) * padded) : 0u;
             }
 #pragma unroll
-            for (int i = 0; i < UNROLL; ++i) {
-                const uint32_t r = warp + i * (THREADS / 32);
-                if (r >= rows) break;
-                const float scale = scale_value<FORMAT>(byte[i]);
-                __align__(16) T v[8];
+            for (int i = 0; i < UNROLL; ++i, out += (THREADS / 32) * a.ldo) {
+                if (warp + i * (THREADS / 32) >= rows) break;
+                const float scale = __fmul_rn(scale_value<FORMAT>(byte[i]), near);
+                float f[8];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float2 p = values_of((w[i] >> (8 * j)) & 0xFFu);
-                    v[2 * j] = from_float<T>(__fmul_rn(__fmul_rn(p.x, scale), tensor));
-                    v[2 * j + 1] = from_float<T>(__fmul_rn(__fmul_rn(p.y, scale), tensor));
+                    f[2 * j] = __fmul_rn(p.x, scale);
+                    f[2 * j + 1] = __fmul_rn(p.y, scale);
                 }
-                T *const out = static_cast<T *>(a.out) + (row0 + r) * a.ldo + c;
+                if (far != 1.0f)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) f[j] = __fmul_rn(f[j], far);
+                __align__(16) T v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = from_float<T>(f[j]);
                 if (c + 8 <= a.cols) {
 #pragma unroll
                     for (int n = 0; n < (int)sizeof(T) / 2; ++n) reinterpret_cast<uint4 *>(out)[n] = reinterpret_cast<const uint4 *>(v)[n];
@@ -427,13 +437,20 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_dequantize_kernel(const __g
             for (uint32_t r = warp; r < rows; r += THREADS / 32) {
                 const uint8_t *const codes = a.codes + (row0 + r) * (padded / 2);
                 T *const out = static_cast<T *>(a.out) + (row0 + r) * a.ldo;
+                uint32_t held[BACK_COLS / 32], byte[BACK_COLS / 32];
 #pragma unroll
                 for (uint32_t i = 0; i < BACK_COLS / 32; ++i) {
                     const uint64_t c = col0 + i * 32u + lane, block = c / BLOCK;
+                    held[i] = c < a.cols ? codes[c / 2] : 0u;
+                    byte[i] = c < a.cols ? scales[block / 4 * SCALE_TILE + r * 16u + block % 4] : 0u;
+                }
+#pragma unroll
+                for (uint32_t i = 0; i < BACK_COLS / 32; ++i) {
+                    const uint64_t c = col0 + i * 32u + lane;
                     if (c >= a.cols) break;
-                    const float2 p = values_of(codes[c / 2]);
-                    const float scale = scale_value<FORMAT>(scales[block / 4 * SCALE_TILE + r * 16u + block % 4]);
-                    out[c] = from_float<T>(__fmul_rn(__fmul_rn(c % 2 ? p.y : p.x, scale), tensor));
+                    const float2 p = values_of(held[i]);
+                    const float scale = __fmul_rn(scale_value<FORMAT>(byte[i]), near);
+                    out[c] = from_float<T>(__fmul_rn(__fmul_rn(c % 2 ? p.y : p.x, scale), far));
                 }
             }
         }

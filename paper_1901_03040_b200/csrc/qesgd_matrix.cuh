@@ -101,16 +101,23 @@ __device__ __forceinline__ void values(const Octet<T> &o, float (&v)[8])
         }
     }
 }
+// The largest magnitude of three numbers, NaN where one of them is.
+__device__ __forceinline__ float max_magnitude(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 // Bits of the largest magnitude, as a 32-bit float: 0x7F800000 or more where an element is not finite.  16-bit magnitudes
 // are compared as they lie, by twos.
 template <typename T>
 __device__ __forceinline__ uint32_t top_of(const Octet<T> &o)
 {
     if constexpr (sizeof(T) == 4) {
-        uint32_t t = 0u;
+        float t = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) t = max(t, o.w[j] & 0x7FFFFFFFu);
-        return t;
+        for (int j = 0; j < 8; j += 2) t = max_magnitude(t, __uint_as_float(o.w[j]), __uint_as_float(o.w[j + 1]));
+        return __float_as_uint(t);
     } else {
         uint32_t t = 0u;
 #pragma unroll
