@@ -55,37 +55,42 @@ __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((u
 // (and, NV, divided by).
 struct Scale {
     uint32_t byte;
-    float mul;    // 2^-e (MX), 2^-t (NV); 0 where the block holds nothing but zeros or something not finite
+    float mul;    // 2^-e (MX), 2^-t (NV)
     float div;    // s (NV)
-    float inv;    // fl32(1 / s) (NV)
+    float inv;    // fl32(1 / s) (NV), 0 for s = 0
+    bool bad;     // something in the block is not finite
 };
-template <int FORMAT>
-__device__ __forceinline__ Scale block_scale(uint32_t top, float to_tensor)
+__device__ __forceinline__ float e4m3(uint32_t code, float factor) { return __fmul_rn(__uint_as_float(code << 20), factor); }   // factor: a power of two or 6 of them, times 2^120
+// inverse: fl32(1 / s) of every E4M3 number, in shared memory (__frcp_rn of each block's takes ten instructions)
+template <int FORMAT, bool SCALED>
+__device__ __forceinline__ Scale block_scale(uint32_t top, float to_tensor, const float *inverse)
 {
     Scale s;
-    const bool none = top == 0u || top >= 0x7F800000u;
+    s.bad = top >= 0x7F800000u;
     if (FORMAT == QESGD_FP4_MX) {
-        // top = 1.f * 2^(E - 127) is at most 6 * 2^e = 1.5 * 2^(e + 2) from e = E - 129 on, one later where 1.f > 1.5
-        const int byte = (int)(top >> 23) - 2 + ((top & 0x7FFFFFu) > 0x400000u ? 1 : 0);
-        s.byte = none ? 0u : (uint32_t)max(byte, 0);
-        s.mul = none ? 0.0f : __uint_as_float((254u - s.byte) << 23);
+        // top = 1.f * 2^(E - 127) is at most 6 * 2^e = 1.5 * 2^(e + 2) from e = E - 129 on, one later where 1.f > 1.5: where the
+        // mantissa carries
+        s.byte = s.bad ? 0u : (uint32_t)max((int)((top + 0x3FFFFFu) >> 23) - 2, 0);
+        s.mul = __uint_as_float((254u - s.byte) << 23);
         s.div = s.inv = 1.0f;
     } else {
-        // The bits of an E4M3 number are bits 20..26 of the float 2^-120 times it, subnormals included.  A first guess from
-        // a rounded product, right to within one number; then the smallest s with v <= 6 s, 6 s being exact.
-        const float v = __fmul_rn(__uint_as_float(none ? 0u : top), to_tensor);
-        const float g = __fmul_rn(__fmul_rn(fminf(v, 2688.0f), 0.16666667f), 0x1p-120f);
-        uint32_t code = min((__float_as_uint(g) + 0xFFFFFu) >> 20, 126u);
-        const float up = __fmul_rn(__uint_as_float(code << 20), 0x1p120f);
-        if (__fmul_rn(6.0f, up) < v) code = min(code + 1u, 126u);
-        else if (code > 0u && __fmul_rn(6.0f, __fmul_rn(__uint_as_float((code - 1u) << 20), 0x1p120f)) >= v) code -= 1u;
-        code = none ? 0u : max(code, 1u);
+        // The bits of an E4M3 number are bits 20..26 of the float 2^-120 times it, subnormals included.  A quotient by 6 that is
+        // rounded down, and then up to such bits, is right or one number short; 6 s is exact.
+        float v = __uint_as_float(s.bad ? 0u : top);
+        if (SCALED) v = __fmul_rn(v, to_tensor);
+        uint32_t code = min((__float_as_uint(__fmul_rd(v, 0x1.555554p-123f)) + 0xFFFFFu) >> 20, 126u);
+        code = min(code + (e4m3(code, 6.0f * 0x1p120f) < v ? 1u : 0u), 126u);
+        if (SCALED) code = max(code, s.bad || top == 0u ? 0u : 1u);   // top * 2^-t may be 0
         s.byte = code;
-        s.div = __fmul_rn(__uint_as_float(max(code, 1u) << 20), 0x1p120f);
-        s.inv = __frcp_rn(s.div);
-        s.mul = none ? 0.0f : to_tensor;
+        s.div = e4m3(code, 0x1p120f);
+        s.inv = inverse[code];
+        s.mul = to_tensor;
     }
     return s;
+}
+__device__ __forceinline__ void fill_inverse(float *inverse)
+{
+    if (threadIdx.x < 128) inverse[threadIdx.x] = threadIdx.x ? __frcp_rn(e4m3(threadIdx.x, 0x1p120f)) : 0.0f;
 }
 // x over the block's scale, correctly rounded.  NV: the quotient by the rounded reciprocal, corrected by its residual; s has
 // 4 significant bits, so a quotient lies on a rounding border or at least 2^-5 units in the last place from it, far
@@ -141,7 +146,7 @@ __device__ __forceinline__ uint32_t quantize_octet(const float (&v)[8], const Sc
     }
     // a zero has no sign: the top bit of a half stays where its level is 1 at least
     w &= 0x77777777u | ((w & 0x77777777u) + 0x77777777u);
-    return s.mul == 0.0f ? 0u : w;
+    return s.bad ? 0u : w;
 }
 
 // Byte of (row, block) within the tiles that a CTA keeps in shared memory, one after another along the blocks.
@@ -150,75 +155,89 @@ __device__ __forceinline__ uint32_t scale_slot(uint32_t row, uint32_t block)
     return block / 4u * SCALE_TILE + (row % 32u) * 16u + (row / 32u) * 4u + block % 4u;
 }
 
-// The largest magnitude of the block that an octet is part of.
+// The largest magnitude of a block, of which a lane has one whole (NV) or its neighbour the other half (MX).
 template <int FORMAT>
 __device__ __forceinline__ uint32_t over_block(uint32_t top)
 {
-    top = max(top, __shfl_xor_sync(FULL, top, 1));
-    if (FORMAT == QESGD_FP4_MX) top = max(top, __shfl_xor_sync(FULL, top, 2));
-    return top;
+    return FORMAT == QESGD_FP4_MX ? max(top, __shfl_xor_sync(FULL, top, 1)) : top;
+}
+// Two octets of a row -> two words of codes, and their block's scale.
+template <typename T, int FORMAT, bool SCALED, bool STOCHASTIC>
+__device__ __forceinline__ uint2 quantize_span(const Octet<T> (&x)[2], uint64_t n, float to_tensor, const float *inverse, const Fp4QuantizeArgs &a, Scale &s)
+{
+    s = block_scale<FORMAT, SCALED>(over_block<FORMAT>(max(top_of(x[0]), top_of(x[1]))), to_tensor, inverse);
+    uint32_t w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        uint32_t draw[4] = {0u, 0u, 0u, 0u};
+        if (STOCHASTIC) draws_of(n + i, a, draw);
+        float v[8];
+        values(x[i], v);
+        w[i] = quantize_octet<FORMAT, SCALED, STOCHASTIC>(v, s, draw);
+    }
+    return make_uint2(w[0], w[1]);
 }
 
 // ------------------------------------------------------- blocks along rows ----
-constexpr int ROW_COLS = 128;   // columns of a CTA's tile: a warp takes two rows at a time
+// A CTA's tile: 64 rows, half of a tile of scales, by 256 columns, 16 for each lane, two rows for a warp at a time.
+constexpr int ROW_COLS = 256, HALF_ROWS = TILE_ROWS / 2;
 
 template <typename T, int FORMAT, bool SCALED, bool STOCHASTIC>
 __global__ __launch_bounds__(THREADS) void qesgd_fp4_quantize_rows_kernel(const __grid_constant__ Fp4QuantizeArgs a)
 {
     constexpr int BLOCK = Format<FORMAT>::BLOCK;
-    constexpr int BLOCKS = ROW_COLS / BLOCK;
-    constexpr int UNROLL = 4;
-    __shared__ __align__(16) uint8_t scales[TILE_ROWS * BLOCKS];
+    constexpr int TILES = ROW_COLS / BLOCK / 4;        // of scales
+    constexpr int UNROLL = sizeof(T) == 4 ? 1 : 2;
+    __shared__ __align__(16) uint8_t scales[TILES * SCALE_TILE];   // rows 0 to 63 in the first 8 of every 16 bytes
+    __shared__ float inverse[128];
+    if (FORMAT == QESGD_FP4_NV) fill_inverse(inverse);
     qesgd_wait_for_previous();
     if (a.small) qesgd_let_next_start();
     const uint32_t o = threadIdx.x % 16u, line = threadIdx.x / 16u;
     const uint32_t col_tiles = (uint32_t)((a.cols + ROW_COLS - 1) / ROW_COLS);
-    const uint64_t tiles = (uint64_t)col_tiles * ((a.rows + TILE_ROWS - 1) / TILE_ROWS);
+    const uint64_t tiles = (uint64_t)col_tiles * ((a.rows + TILE_ROWS - 1) / TILE_ROWS * 2);
     const uint64_t padded = (a.cols + 31) / 32 * 32;
     const uint64_t scale_tiles = (a.cols + 4 * BLOCK - 1) / (4 * BLOCK);
     const float to_tensor = SCALED ? power_of_two(-tensor_exponent(a.tensor_exponent)) : 1.0f;
     bool bad = false;
     for (uint64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const uint64_t row0 = tile / col_tiles * TILE_ROWS;
+        const uint64_t row0 = tile / col_tiles * HALF_ROWS;
         const uint32_t col0 = (uint32_t)(tile % col_tiles) * ROW_COLS;
-        const uint32_t rows = (uint32_t)min((uint64_t)TILE_ROWS, a.rows - row0);
-        if (rows < TILE_ROWS) {
+        const uint32_t rows = row0 < a.rows ? (uint32_t)min((uint64_t)HALF_ROWS, a.rows - row0) : 0u;
+        if (rows < HALF_ROWS)
             for (uint32_t i = threadIdx.x; i < sizeof(scales) / 4; i += THREADS) reinterpret_cast<uint32_t *>(scales)[i] = 0u;
-            __syncthreads();
-        }
-        const uint64_t c = col0 + o * 8u;
-        const T *const first = static_cast<const T *>(a.x) + row0 * a.ldx;
-        uint8_t *const codes = a.codes + (row0 * padded + c) / 2;
+        __syncthreads();
+        const uint64_t c = col0 + o * 16u;
+        const T *from = static_cast<const T *>(a.x) + (row0 + line) * a.ldx;
+        uint64_t n = ((row0 + line) * padded + c) / 8;
 #pragma unroll 1
         for (uint32_t r0 = line; r0 < (rows + 1u) / 2u * 2u; r0 += THREADS / 16 * UNROLL) {   // both halves of a warp stay together
-            Octet<T> x[UNROLL];
+            Octet<T> x[UNROLL][2];
 #pragma unroll
-            for (int i = 0; i < UNROLL; ++i) {
-                const uint32_t r = r0 + i * (THREADS / 16);
-                x[i] = r < rows ? load_octet(first + r * a.ldx, c, a.cols, a.vec) : no_octet<T>();
-            }
+            for (int i = 0; i < UNROLL; ++i)
 #pragma unroll
-            for (int i = 0; i < UNROLL; ++i) {
+                for (int k = 0; k < 2; ++k)
+                    x[i][k] = r0 + i * (THREADS / 16) < rows ? load_octet(from + i * (THREADS / 16) * a.ldx, c + 8 * k, a.cols, a.vec) : no_octet<T>();
+            from += UNROLL * (THREADS / 16) * a.ldx;
+#pragma unroll
+            for (int i = 0; i < UNROLL; ++i, n += (THREADS / 16) * (padded / 8)) {
                 const uint32_t r = r0 + i * (THREADS / 16);
-                const uint32_t top = over_block<FORMAT>(top_of(x[i]));
+                Scale s;
+                const uint2 w = quantize_span<T, FORMAT, SCALED, STOCHASTIC>(x[i], n, to_tensor, inverse, a, s);
                 if (r >= rows) continue;
-                bad |= top >= 0x7F800000u;
-                const Scale s = block_scale<FORMAT>(top, to_tensor);
-                uint32_t draw[4] = {0u, 0u, 0u, 0u};
-                if (STOCHASTIC) draws_of(((row0 + r) * padded + c) / 8, a, draw);
-                float v[8];
-                values(x[i], v);
-                const uint32_t w = quantize_octet<FORMAT, SCALED, STOCHASTIC>(v, s, draw);
-                if (c < padded) *reinterpret_cast<uint32_t *>(codes + r * (padded / 2)) = w;
-                if (o % (BLOCK / 8) == 0) scales[scale_slot(r, o / (BLOCK / 8))] = (uint8_t)s.byte;
+                bad |= s.bad;
+                if (c < padded) *reinterpret_cast<uint2 *>(a.codes + n * 4) = w;
+                const uint32_t block = o * 16u / BLOCK;
+                if (o * 16u % BLOCK == 0u) scales[block / 4u * SCALE_TILE + r % 32u * 16u + r / 32u * 4u + block % 4u] = (uint8_t)s.byte;
             }
             __syncwarp();
         }
         __syncthreads();
         const uint64_t at = col0 / (4 * BLOCK);
-        const uint32_t have = (uint32_t)min((uint64_t)(BLOCKS / 4), scale_tiles - at);
-        uint4 *out = reinterpret_cast<uint4 *>(a.scales + (row0 / TILE_ROWS * scale_tiles + at) * SCALE_TILE);
-        for (uint32_t i = threadIdx.x; i < have * (SCALE_TILE / 16); i += THREADS) out[i] = reinterpret_cast<const uint4 *>(scales)[i];
+        const uint32_t have = (uint32_t)min((uint64_t)TILES, scale_tiles - at);
+        uint8_t *const out = a.scales + (row0 / TILE_ROWS * scale_tiles + at) * SCALE_TILE + row0 / HALF_ROWS % 2 * 8;
+        for (uint32_t i = threadIdx.x; i < have * (SCALE_TILE / 16); i += THREADS)
+            *reinterpret_cast<uint2 *>(out + i * 16u) = *reinterpret_cast<const uint2 *>(scales + i * 16u);
         __syncthreads();
     }
     if (bad) atomicOr(a.status, QESGD_STATUS_NONFINITE);
@@ -227,6 +246,16 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_quantize_rows_kernel(const 
 // ------------------------------- blocks along columns, or along both axes ----
 constexpr int SIDE = 128;   // a CTA's tile: whole tiles of scales for either axis
 
+// Where element (r, c) of the tile lies in shared memory: rows one after another, the 16-byte lines of each turned by one
+// more for every eight of them, so that eight lanes meet eight different banks when they store two or four lines apart
+// and when they load neighbouring ones.
+template <typename T>
+__device__ __forceinline__ uint32_t held_at(uint32_t r, uint32_t c)
+{
+    const uint32_t at = c * sizeof(T), line = at / 16u;
+    return r * (SIDE * sizeof(T)) + (line & ~7u) * 16u + ((line + line / 8u) & 7u) * 16u + at % 16u;
+}
+
 // The tile goes through shared memory as it is.  Then a thread takes two neighbouring columns of 32 rows: one load for both
 // where elements have 16 bits, whole blocks without an exchange, and 16 bytes of codes for each column.
 template <typename T, int FORMAT, bool SCALED, bool STOCHASTIC>
@@ -234,9 +263,11 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_quantize_columns_kernel(con
 {
     constexpr int BLOCK = Format<FORMAT>::BLOCK;
     constexpr int BLOCKS = SIDE / BLOCK;
-    constexpr uint32_t PITCH = SIDE * sizeof(T);       // bytes of a row in shared memory
     extern __shared__ __align__(16) uint8_t held[];
     __shared__ __align__(16) uint8_t scales[2][SIDE * BLOCKS];
+    __shared__ float inverse[128];
+    if (FORMAT == QESGD_FP4_NV) fill_inverse(inverse);
+    __syncthreads();
     qesgd_wait_for_previous();
     if (a.small) qesgd_let_next_start();
     const uint32_t col_tiles = (uint32_t)((a.cols + SIDE - 1) / SIDE);
@@ -249,35 +280,34 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_quantize_columns_kernel(con
         const uint64_t row0 = tile / col_tiles * SIDE, col0 = tile % col_tiles * SIDE;
         {
             // every row and column of the tile goes the whole way, as zeros past the matrix's edge: then padding bytes are zeros
-            constexpr int UNROLL = 4;
-            const uint32_t o = threadIdx.x % 16u, line = threadIdx.x / 16u;
-            const uint64_t c = col0 + o * 8u;
+            constexpr int UNROLL = sizeof(T) == 4 ? 1 : 2;
+            const uint32_t o = threadIdx.x % 8u, line = threadIdx.x / 8u;
+            const uint64_t c = col0 + o * 16u;
+            const T *from = static_cast<const T *>(a.x) + (row0 + line) * a.ldx;
+            uint64_t n = ((row0 + line) * padded + c) / 8;
 #pragma unroll 1
-            for (uint32_t i0 = line; i0 < SIDE; i0 += THREADS / 16 * UNROLL) {
-                Octet<T> x[UNROLL];
+            for (uint32_t i0 = line; i0 < SIDE; i0 += THREADS / 8 * UNROLL) {
+                Octet<T> x[UNROLL][2];
 #pragma unroll
-                for (int n = 0; n < UNROLL; ++n) {
-                    const uint64_t r = row0 + i0 + n * (THREADS / 16);
-                    x[n] = r < a.rows ? load_octet(static_cast<const T *>(a.x) + r * a.ldx, c, a.cols, a.vec) : no_octet<T>();
-                }
+                for (int i = 0; i < UNROLL; ++i)
 #pragma unroll
-                for (int n = 0; n < UNROLL; ++n) {
-                    const uint32_t i = i0 + n * (THREADS / 16);
+                    for (int k = 0; k < 2; ++k)
+                        x[i][k] = row0 + i0 + i * (THREADS / 8) < a.rows ? load_octet(from + i * (THREADS / 8) * a.ldx, c + 8 * k, a.cols, a.vec) : no_octet<T>();
+                from += UNROLL * (THREADS / 8) * a.ldx;
 #pragma unroll
-                    for (int k = 0; k < Octet<T>::WORDS / 4; ++k)
-                        *reinterpret_cast<uint4 *>(held + i * PITCH + o * 8u * sizeof(T) + k * 16) = *reinterpret_cast<const uint4 *>(&x[n].w[4 * k]);
+                for (int i = 0; i < UNROLL; ++i, n += (THREADS / 8) * (padded / 8)) {
+                    const uint32_t r = i0 + i * (THREADS / 8);
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+#pragma unroll
+                        for (int q = 0; q < Octet<T>::WORDS / 4; ++q)
+                            *reinterpret_cast<uint4 *>(held + held_at<T>(r, o * 16u + k * 8u + q * (16 / sizeof(T)))) = *reinterpret_cast<const uint4 *>(&x[i][k].w[4 * q]);
                     if (a.codes) {
-                        const uint64_t r = row0 + i;
-                        const uint32_t top = over_block<FORMAT>(top_of(x[n]));
-                        bad |= top >= 0x7F800000u;
-                        const Scale s = block_scale<FORMAT>(top, to_tensor);
-                        uint32_t draw[4] = {0u, 0u, 0u, 0u};
-                        if (STOCHASTIC) draws_of((r * padded + c) / 8, a, draw);
-                        float v[8];
-                        values(x[n], v);
-                        const uint32_t w = quantize_octet<FORMAT, SCALED, STOCHASTIC>(v, s, draw);
-                        if (r < a.rows && c < padded) *reinterpret_cast<uint32_t *>(a.codes + (r * padded + c) / 2) = w;
-                        if (o % (BLOCK / 8) == 0) scales[0][scale_slot(i, o / (BLOCK / 8))] = (uint8_t)s.byte;
+                        Scale s;
+                        const uint2 w = quantize_span<T, FORMAT, SCALED, STOCHASTIC>(x[i], n, to_tensor, inverse, a, s);
+                        bad |= s.bad;
+                        if (row0 + r < a.rows && c < padded) *reinterpret_cast<uint2 *>(a.codes + n * 4) = w;
+                        if (o * 16u % BLOCK == 0u) scales[0][scale_slot(r, o * 16u / BLOCK)] = (uint8_t)s.byte;
                     }
                 }
             }
@@ -292,7 +322,7 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_quantize_columns_kernel(con
                 uint32_t top[2] = {0u, 0u}, both = 0u;
 #pragma unroll
                 for (int j = 0; j < BLOCK; ++j) {
-                    const uint8_t *const p = held + (i0 + g * BLOCK + j) * PITCH + k * sizeof(T);
+                    const uint8_t *const p = held + held_at<T>(i0 + g * BLOCK + j, k);
                     if constexpr (sizeof(T) == 4) {
                         const uint2 w = *reinterpret_cast<const uint2 *>(p);
                         v[0][j] = __uint_as_float(w.x);
@@ -314,8 +344,8 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_quantize_columns_kernel(con
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
                     const uint64_t c = col0 + k + n;
-                    bad |= top[n] >= 0x7F800000u;
-                    const Scale s = block_scale<FORMAT>(top[n], to_tensor);
+                    const Scale s = block_scale<FORMAT, SCALED>(top[n], to_tensor, inverse);
+                    bad |= s.bad;
 #pragma unroll
                     for (int o = 0; o < BLOCK / 8; ++o) {
                         uint32_t draw[4] = {0u, 0u, 0u, 0u};
@@ -498,8 +528,7 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_tensor_exponent_kernel(cons
 template <typename T, int FORMAT, bool SCALED, bool STOCHASTIC>
 cudaError_t launch_quantize(Fp4QuantizeArgs a, cudaStream_t stream)
 {
-    static_assert(ROW_COLS == SIDE, "tiles");
-    const uint64_t tiles = qesgd_div_up(a.rows, TILE_ROWS) * qesgd_div_up(a.cols, SIDE);
+    const uint64_t tiles = qesgd_div_up(a.rows, TILE_ROWS) * (a.codes_t ? qesgd_div_up(a.cols, SIDE) : 2 * qesgd_div_up(a.cols, ROW_COLS));
     const dim3 grid((unsigned)(tiles < 0x7FFFFFFF ? tiles : 0x7FFFFFFF));
     a.small = tiles <= 128;
     if (!a.codes_t) return qesgd_launch(qesgd_fp4_quantize_rows_kernel<T, FORMAT, SCALED, STOCHASTIC>, grid, dim3(THREADS), stream, a);
