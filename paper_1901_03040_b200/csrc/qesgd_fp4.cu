@@ -534,7 +534,8 @@ cudaError_t launch_quantize(Fp4QuantizeArgs a, cudaStream_t stream)
     if (!a.codes_t) return qesgd_launch(qesgd_fp4_quantize_rows_kernel<T, FORMAT, SCALED, STOCHASTIC>, grid, dim3(THREADS), stream, a);
     const auto kernel = qesgd_fp4_quantize_columns_kernel<T, FORMAT, SCALED, STOCHASTIC>;
     const int smem = SIDE * SIDE * (int)sizeof(T);
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    static std::atomic<uint64_t> told{0};
+    const cudaError_t e = qesgd_prepare(told, (const void *)kernel, smem, false);
     return e != cudaSuccess ? e : qesgd_launch_smem(kernel, grid, dim3(THREADS), smem, stream, a);
 }
 template <typename T, bool STOCHASTIC>

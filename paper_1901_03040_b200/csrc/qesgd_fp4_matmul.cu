@@ -13,7 +13,8 @@
 
 namespace {
 
-constexpr int WARPS = 12;                 // copies, products, 2 without work, 8 that take tiles out
+constexpr int TAKERS = 16;                // warps that take tiles out: four for each quarter of tensor memory
+constexpr int WARPS = 4 + TAKERS;         // before them: copies, products, tensor memory, one without work
 constexpr uint32_t DEPTH = 256;           // contraction of a stage
 constexpr uint32_t LANES = 128;           // rows of B of a CTA
 constexpr uint32_t SCALE_TILE = 512;
@@ -42,35 +43,41 @@ struct ProductArgs {
     const int32_t *a_exponent, *b_exponent;
     void *c;
     uint64_t ldc;
-    uint32_t dtype, accumulate;
+    uint32_t dtype;
     uint32_t *status;
 };
 
-// Column n of `count` rows of C from row m on.
+// Column n of COUNT rows of C from row m on: what is there, and what comes there.
 template <typename T, int COUNT>
-__device__ __forceinline__ void store_column(const float (&v)[COUNT], T *c, uint32_t m, uint32_t M, uint64_t ldc, bool accumulate, float power_a, float power_b)
+__device__ __forceinline__ void load_column(float (&old)[COUNT], const T *c, uint32_t m, const ProductArgs &a)
 {
-    constexpr int GROUP = COUNT < 8 ? COUNT : 8;   // loads of C in flight
 #pragma unroll
-    for (int g = 0; g < COUNT; g += GROUP) {
-        float old[GROUP];
-#pragma unroll
-        for (int k = 0; k < GROUP; ++k) old[k] = accumulate && m + g + k < M ? to_float(c[(g + k) * ldc]) : 0.0f;
-#pragma unroll
-        for (int k = 0; k < GROUP; ++k) {
-            const float p = v[g + k] * power_a * power_b;
-            if (m + g + k < M) c[(g + k) * ldc] = from_float<T>(accumulate ? old[k] + p : p);
-        }
-    }
+    for (int k = 0; k < COUNT; ++k, c += a.ldc) old[k] = m + k < a.M ? to_float(*c) : 0.0f;
 }
 template <int COUNT>
-__device__ __forceinline__ void store_column(const float (&v)[COUNT], uint32_t m, uint32_t n, const ProductArgs &a, float power_a, float power_b)
+__device__ __forceinline__ void load_column(float (&old)[COUNT], uint32_t m, uint32_t n, const ProductArgs &a)
 {
     if (n >= a.N || m >= a.M) return;
     const uint64_t at = m * a.ldc + n;
-    if (a.dtype == QESGD_F32) store_column(v, static_cast<float *>(a.c) + at, m, a.M, a.ldc, a.accumulate, power_a, power_b);
-    else if (a.dtype == QESGD_BF16) store_column(v, static_cast<__nv_bfloat16 *>(a.c) + at, m, a.M, a.ldc, a.accumulate, power_a, power_b);
-    else store_column(v, static_cast<__half *>(a.c) + at, m, a.M, a.ldc, a.accumulate, power_a, power_b);
+    if (a.dtype == QESGD_F32) load_column(old, static_cast<const float *>(a.c) + at, m, a);
+    else if (a.dtype == QESGD_BF16) load_column(old, static_cast<const __nv_bfloat16 *>(a.c) + at, m, a);
+    else load_column(old, static_cast<const __half *>(a.c) + at, m, a);
+}
+template <typename T, int COUNT>
+__device__ __forceinline__ void store_column(const float (&v)[COUNT], T *c, uint32_t m, const ProductArgs &a)
+{
+#pragma unroll
+    for (int k = 0; k < COUNT; ++k, c += a.ldc)
+        if (m + k < a.M) *c = from_float<T>(v[k]);
+}
+template <int COUNT>
+__device__ __forceinline__ void store_column(const float (&v)[COUNT], uint32_t m, uint32_t n, const ProductArgs &a)
+{
+    if (n >= a.N || m >= a.M) return;
+    const uint64_t at = m * a.ldc + n;
+    if (a.dtype == QESGD_F32) store_column(v, static_cast<float *>(a.c) + at, m, a);
+    else if (a.dtype == QESGD_BF16) store_column(v, static_cast<__nv_bfloat16 *>(a.c) + at, m, a);
+    else store_column(v, static_cast<__half *>(a.c) + at, m, a);
 }
 __device__ __forceinline__ float power_of(const int32_t *exponent)
 {
@@ -78,7 +85,7 @@ __device__ __forceinline__ float power_of(const int32_t *exponent)
     return __uint_as_float((uint32_t)(t + 127) << 23);
 }
 
-template <bool PAIR, bool MX>
+template <bool PAIR, bool MX, bool ACCUMULATE>
 __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const __grid_constant__ ProductArgs a, const __grid_constant__ CUtensorMap map_p,
                                                                          const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_sp,
                                                                          const __grid_constant__ CUtensorMap map_sq)
@@ -102,7 +109,7 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const _
         }
         for (int s = 0; s < 2; ++s) {
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(done + 8 * s), "r"(1u) : "memory");
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(free_ + 8 * s), "r"(PAIR ? 16u : 8u) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(free_ + 8 * s), "r"(PAIR ? 2u * TAKERS : (uint32_t)TAKERS) : "memory");
         }
         *stop = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -119,20 +126,25 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const _
     if (PAIR) cluster_sync_all();
     fence_after_sync();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(raw + (slot - smem_u32(raw)));
-    // this CTA's part of the contraction (of a pair: all of it)
+    // this CTA's part of the contraction (of a pair: all of it).  Those who share one leave two stages to what they send
+    // one another: each sums up every parts-th row of A, and receives the others' parts of it.
     const uint32_t part = PAIR ? 0u : rank, parts = PAIR ? 1u : share;
+    const uint32_t stages = parts > 1 ? S::STAGES - 2u : S::STAGES, received = base + stages * S::STAGE_BYTES;
+    const uint32_t every = (q_rows + parts - 1u) / parts;            // rows of A that a CTA sums up, at most
+    bool joined = PAIR || parts == 1;                                // has this warp seen that all of the cluster are there?
+    if (!joined) cluster_arrive();
     const uint32_t first = (uint32_t)((uint64_t)a.steps * part / parts), steps = (uint32_t)((uint64_t)a.steps * (part + 1) / parts) - first;
     qesgd_wait_for_previous();
 
     if (warp == 0 && elect_one()) {
-        uint32_t n = 0;
+        uint32_t s = 0, turn = 0;   // the stage, and how often all of them have been gone through
         const uint32_t full_lead = PAIR ? map_shared(full, 0) : full;
         const uint32_t bytes = (LANES + (PAIR ? S::HELD_Q : q_rows)) * 128u + SCALE_TILES * SCALE_TILE * (1u + S::MOST_Q / 128u);
         for (uint32_t t = group; t < a.tiles && !*stop; t += groups) {
             const uint32_t p0 = t % a.tiles_n * (PAIR ? 256u : 128u) + (PAIR ? rank * 128u : 0u), q0 = t / a.tiles_n * q_rows;
-            for (uint32_t k = first; k < first + steps; ++k, ++n) {
-                const uint32_t s = n % S::STAGES, to = base + s * S::STAGE_BYTES, bar = full_lead + 8 * s;
-                if (n >= S::STAGES && !pipe_wait(empty + 8 * s, (n / S::STAGES - 1u) & 1u, stop)) break;
+            for (uint32_t k = first; k < first + steps; ++k) {
+                const uint32_t to = base + s * S::STAGE_BYTES, bar = full_lead + 8 * s;
+                if (turn > 0 && !pipe_wait(empty + 8 * s, (turn - 1u) & 1u, stop)) break;
                 if (!PAIR || rank == 0)
                     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(full + 8 * s), "r"(bytes * (PAIR ? 2u : 1u)) : "memory");
                 tma_load_2d<PAIR>(to, &map_p, k * 128u, p0, bar);
@@ -142,21 +154,25 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const _
                 tma_load_2d<PAIR>(scales, &map_sp, k * SCALE_TILES * (SCALE_TILE / 8), p0 / 128u, bar);
                 tma_load_2d<PAIR>(scales + S::SCALES_P, &map_sq, k * SCALE_TILES * (SCALE_TILE / 8), q0 / 128u, bar);
                 if (PAIR) tma_load_2d<PAIR>(scales + S::SCALES_P + 2048, &map_sq, k * SCALE_TILES * (SCALE_TILE / 8), q0 / 128u + 1u, bar);
+                if (++s == stages) {
+                    s = 0;
+                    ++turn;
+                }
             }
         }
         if (*stop) drain();
     } else if (warp == 1 && (!PAIR || rank == 0) && elect_one()) {
         // E2M1 operands, fp32 sums; scales E8M0 (MX) or E4M3
         const uint32_t instruction = 1u << 7 | 1u << 10 | (q_rows / 8u) << 17 | (MX ? 1u << 23 : 0u) | (PAIR ? 2u : 1u) << 27;
-        uint32_t n = 0, done_tiles = 0;
+        uint32_t s = 0, phase = 0, done_tiles = 0;
         for (uint32_t t = group; t < a.tiles && !*stop; t += groups, ++done_tiles) {
             const uint32_t which = done_tiles % S::TILES, turn = done_tiles / S::TILES, sums = tmem + which * S::MOST_Q;
             if (turn >= 1 && !pipe_wait(free_ + 8 * which, (turn - 1u) & 1u, stop)) break;
             fence_after_sync();
             bool ok = true;
-            for (uint32_t k = 0; k < steps; ++k, ++n) {
-                const uint32_t s = n % S::STAGES, from = base + s * S::STAGE_BYTES;
-                ok = pipe_wait(full + 8 * s, (n / S::STAGES) & 1u, stop);
+            for (uint32_t k = 0; k < steps; ++k) {
+                const uint32_t from = base + s * S::STAGE_BYTES;
+                ok = pipe_wait(full + 8 * s, phase, stop);
                 if (!ok) break;
                 fence_after_sync();
                 const uint32_t scales = from + (LANES + S::HELD_Q) * 128, sp = tmem + S::SCALE_COLUMN + s * S::SET, sq = sp + 16u;
@@ -174,6 +190,10 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const _
                     mma_fp4<PAIR, MX>(sums, p, q, instruction | half << 4 | half << 29, sp + 4 * at, sq + (PAIR ? 8 : 4) * at, k > 0 || i > 0);
                 }
                 mma_commit<PAIR>(empty + 8 * s);
+                if (++s == stages) {
+                    s = 0;
+                    phase ^= 1u;
+                }
             }
             if (!ok) break;
             mma_commit<PAIR>(done + 8 * which);
@@ -187,53 +207,92 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const _
         for (uint32_t t = group; t < a.tiles; t += groups, ++done_tiles) {
             const uint32_t which = done_tiles % S::TILES, turn = done_tiles / S::TILES;
             const uint32_t n = t % a.tiles_n * (PAIR ? 256u : 128u) + (PAIR ? rank * 128u : 0u) + quarter * 32u + lane, m0 = t / a.tiles_n * q_rows;
+            const uint32_t from = tmem + (quarter * 32u << 16) + which * S::MOST_Q;
+            const uint32_t rows = min(q_rows, a.M - m0);     // of A in this tile
+            const bool ends = ACCUMULATE && parts == 1;
+            float old[32];
+            if (ends) load_column(old, m0 + part_of * 32u, n, a);   // before the sums are there
             if (!__all_sync(0xFFFFFFFFu, pipe_wait(done + 8 * which, turn & 1u, stop))) break;
             fence_after_sync();
-            const uint32_t from = tmem + (quarter * 32u << 16) + which * S::MOST_Q;
-            float v[S::MOST_Q / 64][32];
+            const auto taken = [&]() {   // the tile is in registers
+                tmem_wait_load();
+                fence_before_sync();
+                __syncwarp();
+                if (lane == 0) {
+                    if (PAIR) mbar_arrive_cluster(free_lead + 8 * which);
+                    else mbar_arrive_at(free_ + 8 * which);
+                }
+            };
+            if (ends) {
+                // 32 rows after another, the next ones' elements of C on their way meanwhile
 #pragma unroll
-            for (uint32_t i = 0; i < S::MOST_Q / 64; ++i)
-                if ((2 * i + part_of) * 32u < q_rows) tmem_load32(from + (2 * i + part_of) * 32u, v[i]);
-            tmem_wait_load();
-            fence_before_sync();
-            __syncwarp();
-            if (lane == 0) {
-                if (PAIR) mbar_arrive_cluster(free_lead + 8 * which);
-                else asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(free_ + 8 * which) : "memory");
-            }
-            if (parts == 1) {
+                for (uint32_t i = 0; i < S::MOST_Q / 128; ++i) {
+                    const uint32_t at = (4 * i + part_of) * 32u;
+                    float v[32];
+                    __syncwarp();
+                    tmem_load32(from + at, v);
+                    if (i + 1 == S::MOST_Q / 128) taken();
+                    else tmem_wait_load();
 #pragma unroll
-                for (uint32_t i = 0; i < S::MOST_Q / 64; ++i)
-                    if ((2 * i + part_of) * 32u < q_rows) store_column(v[i], m0 + (2 * i + part_of) * 32u, n, a, power_a, power_b);
+                    for (int k = 0; k < 32; ++k) v[k] = old[k] + v[k] * power_a * power_b;
+                    if (i + 1 < S::MOST_Q / 128 && at + 128u < rows) load_column(old, m0 + at + 128u, n, a);
+                    if (at < rows) store_column(v, m0 + at, n, a);
+                }
             } else {
-                // all copies and products of this CTA are done: its part of the sums goes where the stages were
-                float *const mine = reinterpret_cast<float *>(raw + (base - smem_u32(raw)));
+                float v[S::MOST_Q / 128][32];
 #pragma unroll
-                for (uint32_t i = 0; i < S::MOST_Q / 64; ++i)
-                    if ((2 * i + part_of) * 32u < q_rows)
+                for (uint32_t i = 0; i < S::MOST_Q / 128; ++i)
+                    if ((4 * i + part_of) * 32u < rows) tmem_load32(from + (4 * i + part_of) * 32u, v[i]);
+                taken();
+                if (!joined) {
+                    cluster_wait();
+                    joined = true;
+                }
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) mine[((2 * i + part_of) * 32u + k) * LANES + quarter * 32u + lane] = steps ? v[i][k] : 0.0f;
+                for (uint32_t i = 0; i < S::MOST_Q / 128; ++i) {
+                    const uint32_t at = (4 * i + part_of) * 32u;
+                    if (at >= rows) break;
+                    if (PAIR || parts == 1) {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) v[i][k] = v[i][k] * power_a * power_b;
+                        store_column(v[i], m0 + at, n, a);
+                    } else {
+                        // row m of the tile to CTA m % parts, as part `rank` of its row m / parts
+                        uint32_t owner = at % parts, to = received + ((rank * every + at / parts) * LANES + quarter * 32u + lane) * 4u;
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) {
+                            if (at + k < rows) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(map_shared(to, owner)), "f"(v[i][k]) : "memory");
+                            if (++owner == parts) {
+                                owner = 0;
+                                to += LANES * 4u;
+                            }
+                        }
+                    }
+                }
             }
         }
     }
     __syncwarp();
     if (!PAIR && parts > 1) {
+        if (!joined) cluster_wait();
+        __syncwarp();
         cluster_sync_all();
         if (!*stop) {
-            // every CTA adds up its share of the tile's columns, in the order of the contraction
-            const uint32_t t = group, n = t % a.tiles_n * 128u + threadIdx.x % LANES;
+            const uint32_t n = group % a.tiles_n * 128u + threadIdx.x % LANES, m0 = group / a.tiles_n * q_rows;
             const float power_a = power_of(a.a_exponent), power_b = power_of(a.b_exponent);
-            for (uint32_t col = rank + parts * (threadIdx.x / LANES); col < q_rows; col += parts * (WARPS * 32 / LANES)) {
-                float sum[1] = {0.0f};
-                for (uint32_t r = 0; r < parts; ++r) {
+            for (uint32_t i = threadIdx.x / LANES; i * parts + rank < min(q_rows, a.M - m0); i += WARPS * 32 / LANES) {
+                const uint32_t m = m0 + i * parts + rank;
+                float sum[1] = {0.0f}, old[1] = {0.0f};
+                if (ACCUMULATE) load_column(old, m, n, a);
+                for (uint32_t r = 0; r < parts; ++r) {   // in the order of the contraction
                     float v;
-                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(map_shared(base + (col * LANES + threadIdx.x % LANES) * 4u, r)) : "memory");
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(received + ((r * every + i) * LANES + threadIdx.x % LANES) * 4u));
                     sum[0] += v;
                 }
-                store_column(sum, t / a.tiles_n * q_rows + col, n, a, power_a, power_b);
+                sum[0] = old[0] + sum[0] * power_a * power_b;
+                store_column(sum, m, n, a);
             }
         }
-        cluster_sync_all();   // the others may still read this CTA's part
     }
     __syncthreads();
     if (threadIdx.x == 0 && *stop) atomicOr(a.status, QESGD_STATUS_TIMEOUT);
@@ -261,11 +320,11 @@ bool scales_map(CUtensorMap *map, const uint8_t *p, uint64_t rows, uint64_t K, b
                                 CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool PAIR, bool MX>
+template <bool PAIR, bool MX, bool ACCUMULATE>
 int launch(const Fp4MatmulArgs &f, uint32_t dtype, uint32_t q, uint32_t split, int sm_count, cudaStream_t stream)
 {
     using S = Shape<PAIR>;
-    const auto kernel = qesgd_fp4_matmul_kernel<PAIR, MX>;
+    const auto kernel = qesgd_fp4_matmul_kernel<PAIR, MX, ACCUMULATE>;
     const uint64_t row_bytes = qesgd_div_up(f.K, 32) * 16;
     CUtensorMap p, qm, sp, sq;
     if (!qesgd_encode_tiled() || !codes_map(&p, f.b_codes, f.N, row_bytes, 128) || !codes_map(&qm, f.a_codes, f.M, row_bytes, PAIR ? 128u : q) ||
@@ -286,14 +345,41 @@ int launch(const Fp4MatmulArgs &f, uint32_t dtype, uint32_t q, uint32_t split, i
     a.c = f.c;
     a.ldc = f.ldc;
     a.dtype = dtype;
-    a.accumulate = f.accumulate;
     a.status = f.status;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
-    if (e == cudaSuccess && split > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    static std::atomic<uint64_t> told{0};
+    const cudaError_t e = qesgd_prepare(told, (const void *)kernel, S::SMEM, !PAIR);
     if (e != cudaSuccess) return (int)e;
     const uint32_t most = (uint32_t)sm_count / (PAIR ? 2u : 1u), share = PAIR ? 2u : split;
     const uint32_t groups = split > 1 || a.tiles < most ? a.tiles : most;   // a shared contraction: one tile for each cluster
     return (int)qesgd_launch_cluster(kernel, dim3(groups * share), dim3(WARPS * 32), S::SMEM, share, stream, a, p, qm, sp, sq);
+}
+
+template <bool MX, bool ACCUMULATE>
+int launch(const Fp4MatmulArgs &a, uint32_t dtype, int sm_count, cudaStream_t stream)
+{
+    static QesgdClusters known;
+    const uint64_t pairs = qesgd_div_up(a.M, 256) * qesgd_div_up(a.N, 256);
+    if (pairs * 2 >= (uint64_t)sm_count) return launch<true, MX, ACCUMULATE>(a, dtype, 256, 1, sm_count, stream);
+    // Too few tiles for the SMs: as many CTAs share a contraction as bring it to an end first.  A stage of one CTA takes about
+    // 450 clocks to arrive, adding the parts up 2500 and 100 more for each; a cluster larger than the device runs of them
+    // at once for every tile would wait for a second wave.
+    const uint32_t q = a.M <= 32 ? 32 : a.M <= 64 ? 64 : 128;
+    const uint64_t tiles = qesgd_div_up(a.M, q) * qesgd_div_up(a.N, 128), steps = qesgd_div_up(a.K, DEPTH);
+    const void *const kernel = (const void *)qesgd_fp4_matmul_kernel<false, MX, ACCUMULATE>;
+    uint32_t split = 1;
+    uint64_t best = qesgd_div_up(tiles, (uint64_t)sm_count) * steps * 450;
+    static std::atomic<uint64_t> told{0};
+    const cudaError_t e = qesgd_prepare(told, kernel, Shape<false>::SMEM, true);
+    if (e != cudaSuccess) return (int)e;
+    for (uint32_t s = 2; s <= 16 && s <= steps && tiles * s <= (uint64_t)sm_count; ++s) {
+        const uint64_t active = qesgd_active_clusters(known, kernel, WARPS * 32, Shape<false>::SMEM, s);
+        const uint64_t t = qesgd_div_up(tiles, active) * qesgd_div_up(steps, s) * 450 + 2500 + 100 * s;
+        if (t < best) {
+            best = t;
+            split = s;
+        }
+    }
+    return launch<false, MX, ACCUMULATE>(a, dtype, q, split, sm_count, stream);
 }
 
 }  // namespace
@@ -301,13 +387,6 @@ int launch(const Fp4MatmulArgs &f, uint32_t dtype, uint32_t q, uint32_t split, i
 int qesgd_launch_fp4_matmul(const Fp4MatmulArgs &a, uint32_t dtype, uint32_t format, int sm_count, cudaStream_t stream, int *launched)
 {
     *launched = 1;
-    const bool mx = format == QESGD_FP4_MX;
-    const uint64_t pairs = qesgd_div_up(a.M, 256) * qesgd_div_up(a.N, 256);
-    if (pairs * 2 >= (uint64_t)sm_count)
-        return mx ? launch<true, true>(a, dtype, 256, 1, sm_count, stream) : launch<true, false>(a, dtype, 256, 1, sm_count, stream);
-    const uint32_t q = a.M <= 32 ? 32 : a.M <= 64 ? 64 : 128;
-    const uint64_t tiles = qesgd_div_up(a.M, q) * qesgd_div_up(a.N, 128), steps = qesgd_div_up(a.K, DEPTH);
-    uint32_t split = 1;
-    while (split < 16 && tiles * split * 2 <= (uint64_t)sm_count && steps >= split * 2) split *= 2;
-    return mx ? launch<false, true>(a, dtype, q, split, sm_count, stream) : launch<false, false>(a, dtype, q, split, sm_count, stream);
+    if (format == QESGD_FP4_MX) return a.accumulate ? launch<true, true>(a, dtype, sm_count, stream) : launch<true, false>(a, dtype, sm_count, stream);
+    return a.accumulate ? launch<false, true>(a, dtype, sm_count, stream) : launch<false, false>(a, dtype, sm_count, stream);
 }

@@ -2,6 +2,8 @@
 // Nothing here is part of the public ABI (that is include/qesgd.h).
 #pragma once
 
+#include <atomic>
+
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -79,6 +81,20 @@ static const uint64_t QESGD_LR_WORK_FLOATS = (1ull << 20) - QESGD_LR_EPOCH_FLOAT
 // 11.3 -> 5.9 us, of 8 x 10^6 18.5 -> 14.4, decode of 2^24 13.9 -> 11.3, a logistic step of 64 x 2^22
 // 319 -> 311, and no grid was found that is slower.  (With griddepcontrol.launch_dependents at the top of
 // every kernel the successor's CTAs come early: 461 instead of 353 us for an encode of 400 000 CTAs.)
+// What a kernel needs to be told once on every device: dynamic shared memory beyond 48 KB, clusters of more than eight CTAs.
+// `told` is one bit for each device; two threads may both tell, to the same effect.
+inline cudaError_t qesgd_prepare(std::atomic<uint64_t> &told, const void *kernel, int smem, bool large_clusters)
+{
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = 1ull << (device & 63);
+    if (device < 64 && (told.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess && large_clusters) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess && device < 64) told.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
 template <typename... Params, typename... Args>
 inline cudaError_t qesgd_launch_cluster(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, uint32_t cluster, cudaStream_t stream,
                                         const Args &...args)

@@ -9,6 +9,12 @@ typedef CUresult (*QesgdEncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuin
                                        const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                        CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 QesgdEncodeTiledFn qesgd_encode_tiled();   // null where the driver has none
+// Clusters of `cluster` CTAs of a kernel that the current device runs at once (7 of 16 to 74 of 2 on a B200, by how its SMs
+// lie in groups); asked for once, kept in `known` (one entry for each cluster size).
+struct QesgdClusters {
+    int count[64][17];
+};
+uint32_t qesgd_active_clusters(QesgdClusters &known, const void *kernel, uint32_t threads, uint32_t smem, uint32_t cluster);
 
 namespace {
 

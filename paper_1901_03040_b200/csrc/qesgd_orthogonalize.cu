@@ -648,6 +648,7 @@ constexpr uint32_t WHOLE_ROWS = 128, WHOLE_COLS = 256, WHOLE_MAX_CLUSTER = 16;
 constexpr uint32_t BOX_BYTES = OPERAND_BYTES;              // 128 rows of 64 columns
 constexpr uint32_t WHOLE_EXTRA = 1152;                     // diagonals, barrier and the like
 constexpr uint32_t WHOLE_THREADS = 512;
+constexpr int WHOLE_MOST_SMEM = 10 * BOX_BYTES + WHOLE_EXTRA + 1024 + 128 * 128 * 4;
 constexpr uint32_t WHOLE_MIN_SMEM = 120 * 1024;            // one CTA of an SM: CTAs of two clusters must not wait for one another's tensor memory
 
 struct WholeArgs {
@@ -1032,8 +1033,8 @@ cudaError_t launch_whole(const OrthoArgs &o, cudaStream_t stream)
     uint32_t smem = (2 * a.width / BOX_COLS + 2) * BOX_BYTES + WHOLE_EXTRA + 1024 + (cluster > 1 ? 128 * 128 * 4 : 0);
     if (smem < WHOLE_MIN_SMEM) smem = WHOLE_MIN_SMEM;
     const auto kernel = cluster > 1 ? qesgd_ortho_whole_kernel<T, true> : qesgd_ortho_whole_kernel<T, false>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e == cudaSuccess && cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    static std::atomic<uint64_t> told[2];
+    const cudaError_t e = qesgd_prepare(told[cluster > 1], (const void *)kernel, WHOLE_MOST_SMEM, cluster > 1);
     if (e != cudaSuccess) return e;
     return qesgd_launch_cluster(kernel, dim3(cluster, (unsigned)o.batch), dim3(WHOLE_THREADS), smem, cluster, stream, a);
 }
@@ -1073,7 +1074,8 @@ cudaError_t launch_product(ProductArgs a, const ProductMaps &maps, uint32_t spli
     a.tiles_n = (a.cols + S::SIDE - 1) / S::SIDE;
     a.tiles = MODE == UPDATE ? a.tiles_m * a.tiles_n : a.tiles_m * (a.tiles_m + 1) / 2;
     a.split = split;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+    static std::atomic<uint64_t> told{0};
+    const cudaError_t e = qesgd_prepare(told, (const void *)kernel, S::SMEM, false);
     if (e != cudaSuccess) return e;
     const uint32_t share = PAIR ? 2u : split, all = a.tiles * a.batch, most = (uint32_t)sm_count / share;
     return qesgd_launch_cluster(kernel, dim3((split > 1 || all < most ? all : most) * share), dim3(WARPS * 32), S::SMEM, share, stream, a, maps);
