@@ -684,7 +684,7 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
     volatile uint32_t *const stop = reinterpret_cast<volatile uint32_t *>(raw + (slot + 4 - smem_u32(raw)));
     const uint32_t warp = threadIdx.x / 32u, lane = threadIdx.x % 32u, quarter = warp % 4u, part = warp / 4u, r = quarter * 32u + lane;
     const uint32_t rank = CLUSTER ? cluster_rank() : 0u, cluster = CLUSTER ? gridDim.x : 1u;   // gridDim.x: a power of two, `share` or more
-    const uint32_t c0 = rank * a.width;
+    const uint32_t c0 = rank * a.width, slots = 16u / cluster;   // slots: octets of A's columns that a CTA adds up
     if (threadIdx.x == 0) {
         mbar_init_at(bar, 1u);
         *stop = 0u;
@@ -794,10 +794,13 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
             tmem_load16(tmem + (quarter * 32u << 16) + A_COLUMN + c, w);
             tmem_wait_load();
             if (CLUSTER) {
+                // an octet of columns to the CTA that adds it up: they are dealt out in turn
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    store_shared(parts + ((c / 4 + i) * 128u + r) * 16u, make_uint4(__float_as_uint(w[4 * i]), __float_as_uint(w[4 * i + 1]),
-                                                                                  __float_as_uint(w[4 * i + 2]), __float_as_uint(w[4 * i + 3])));
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t o = c / 8u + i / 2u;
+                    store_remote(map_shared(parts + (((rank * slots + o / cluster) * 2u + i % 2u) * 128u + r) * 16u, o % cluster),
+                                 make_uint4(__float_as_uint(w[4 * i]), __float_as_uint(w[4 * i + 1]), __float_as_uint(w[4 * i + 2]), __float_as_uint(w[4 * i + 3])));
+                }
             } else {
                 float own = 0.0f;
 #pragma unroll
@@ -816,31 +819,19 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
         if (CLUSTER) {
             __syncwarp();
             cluster_sync_all();
-            // octets of columns, dealt out to the CTAs in turn
             const uint32_t row = threadIdx.x % 128u;
             for (uint32_t o = rank + cluster * (threadIdx.x / 128u); o < rows / 8u && row < rows; o += cluster * (WHOLE_THREADS / 128u)) {
                 float w[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-                for (uint32_t p0 = 0; p0 < share; p0 += 4) {   // CTAs behind the last column have nothing to add
-                    float4 q[4][2];
+#pragma unroll 4
+                for (uint32_t p = 0; p < share; ++p) {   // CTAs behind the last column have nothing to add
 #pragma unroll
-                    for (uint32_t p = 0; p < 4; ++p) {
-                        const uint32_t from = map_shared(parts + (o * 2u * 128u + row) * 16u, min(p0 + p, share - 1u));
-#pragma unroll
-                        for (int i = 0; i < 2; ++i)
-                            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                                         : "=f"(q[p][i].x), "=f"(q[p][i].y), "=f"(q[p][i].z), "=f"(q[p][i].w)
-                                         : "r"(from + i * 2048u));
+                    for (int i = 0; i < 2; ++i) {
+                        const uint4 q = load_shared(parts + (((p * slots + o / cluster) * 2u + i) * 128u + row) * 16u);
+                        w[4 * i] += __uint_as_float(q.x);
+                        w[4 * i + 1] += __uint_as_float(q.y);
+                        w[4 * i + 2] += __uint_as_float(q.z);
+                        w[4 * i + 3] += __uint_as_float(q.w);
                     }
-#pragma unroll
-                    for (uint32_t p = 0; p < 4; ++p)
-                        if (p0 + p < share)
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                w[4 * i] += q[p][i].x;
-                                w[4 * i + 1] += q[p][i].y;
-                                w[4 * i + 2] += q[p][i].z;
-                                w[4 * i + 3] += q[p][i].w;
-                            }
                 }
                 float own = 0.0f;
 #pragma unroll
@@ -1004,6 +995,25 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
     if (warp == 0) tmem_dealloc<false>(tmem, 512u);
 }
 
+uint32_t whole_cluster(uint64_t n)
+{
+    uint32_t cluster = 1;
+    while (cluster * WHOLE_COLS < n) cluster *= 2;
+    return cluster;
+}
+// Large clusters come one after another where a batch has many (7 of 16 CTAs run at once): 16 matrices of 128 x 4096 take
+// 224 us, and 176 as fifteen products.
+bool takes_whole(uint64_t m, uint64_t n, uint64_t batch)
+{
+    if (m > WHOLE_ROWS || n > WHOLE_COLS * WHOLE_MAX_CLUSTER) return false;
+    const uint32_t cluster = whole_cluster(n);
+    if (cluster < 8) return true;
+    static QesgdClusters known;
+    static std::atomic<uint64_t> told{0};
+    const void *const kernel = (const void *)qesgd_ortho_whole_kernel<float, true>;
+    if (qesgd_prepare(told, kernel, WHOLE_MOST_SMEM, true) != cudaSuccess) return false;
+    return batch <= 2 * qesgd_active_clusters(known, kernel, WHOLE_THREADS, WHOLE_MOST_SMEM, cluster);
+}
 template <typename T>
 cudaError_t launch_whole(const OrthoArgs &o, cudaStream_t stream)
 {
@@ -1026,8 +1036,7 @@ cudaError_t launch_whole(const OrthoArgs &o, cudaStream_t stream)
     a.cc = o.c;
     a.out = static_cast<__nv_bfloat16 *>(o.out);
     a.status = o.status;
-    uint32_t cluster = 1;
-    while (cluster * WHOLE_COLS < a.n) cluster *= 2;
+    const uint32_t cluster = whole_cluster(a.n);
     a.width = (a.n + cluster - 1) / cluster;
     a.width = (a.width + BOX_COLS - 1) / BOX_COLS * BOX_COLS;
     uint32_t smem = (2 * a.width / BOX_COLS + 2) * BOX_BYTES + WHOLE_EXTRA + 1024 + (cluster > 1 ? 128 * 128 * 4 : 0);
@@ -1096,9 +1105,14 @@ cudaError_t launch_product(const ProductArgs &a, const ProductMaps &maps, int sm
     double best = waves(pairs, (double)(sm_count / 2)) * steps * stage(2 * pairs, 512, 690) + 5000;
     uint32_t split = 0;
     for (uint32_t s = 1; s <= 4; s *= 2) {
-        // clusters of s lie within a group of 16 to 20 SMs each: seven of eight SMs take part at best
-        if (s > 1 && (singles * s > sms * 0.875 || steps < 4 * s)) break;
-        const double t = waves(singles * s, sms) * (double)(uint64_t)((steps + s - 1) / s) * stage(singles * s, 450, 650) + 2500 + (s > 1 ? 2000 : 0);
+        if (s > 1 && (singles * s > sms || steps < 4 * s)) break;
+        static QesgdClusters known;
+        static std::atomic<uint64_t> told{0};
+        const void *const kernel = (const void *)qesgd_ortho_product_kernel<MODE, false>;
+        const uint32_t smem = Shape<MODE, false>::SMEM;
+        if (s > 1 && qesgd_prepare(told, kernel, (int)smem, false) != cudaSuccess) break;
+        const double active = s > 1 ? (double)qesgd_active_clusters(known, kernel, WARPS * 32, smem, s) : sms;
+        const double t = waves(singles, active) * (double)(uint64_t)((steps + s - 1) / s) * stage(singles * s, 450, 650) + 2500 + (s > 1 ? 2000 : 0);
         if (t < best) {
             best = t;
             split = s;
@@ -1111,7 +1125,7 @@ cudaError_t launch_product(const ProductArgs &a, const ProductMaps &maps, int sm
 
 int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t stream, int *launched)
 {
-    if ((a.rows < a.cols ? a.rows : a.cols) <= WHOLE_ROWS && (a.rows < a.cols ? a.cols : a.rows) <= WHOLE_COLS * WHOLE_MAX_CLUSTER) {
+    if (takes_whole(a.rows < a.cols ? a.rows : a.cols, a.rows < a.cols ? a.cols : a.rows, a.batch)) {
         *launched = 1;
         return (int)(a.dtype == QESGD_F32 ? launch_whole<float>(a, stream) : a.dtype == QESGD_BF16 ? launch_whole<__nv_bfloat16>(a, stream) : launch_whole<__half>(a, stream));
     }

@@ -347,6 +347,16 @@ def test_orthogonalize(dtype, rows, cols):
     assert G.ctx().qesgd_status() == 0
 
 
+@pytest.mark.parametrize("rows,cols,batch", [(100, 3000, 16), (100, 3000, 5), (2000, 64, 40), (128, 128, 200), (120, 700, 50)])
+def test_orthogonalize_of_many_small_matrices(rows, cols, batch):
+    """More clusters than the device runs at once, and the batch sizes around which single products take over."""
+    x = _gradient(batch, rows, cols, qesgd.BF16, 4)
+    got = _np(_orthogonalize(x, qesgd.BF16, rows, cols, batch))
+    for i in range(0, batch, 1 + batch // 10):
+        want = ref.orthogonalize(_np(x[i]))
+        assert np.linalg.norm(got[i] - want) <= ORTHO_TOLERANCE * np.linalg.norm(want)
+
+
 @pytest.mark.parametrize("rows,cols", [(600, 900), (900, 600), (513, 513)])
 def test_orthogonalize_of_many_larger_matrices(rows, cols):
     """Enough tiles that pairs of SMs share them, in all three products."""
