@@ -119,11 +119,12 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const _
         prefetch_map(&map_sp);
         prefetch_map(&map_sq);
     }
-    if (PAIR) cluster_sync_all();   // both CTAs of the pair are there
+    // Both CTAs of a pair are there, and their barriers.  (The first product of a pair waits for copies that its other CTA
+    // sets off behind its own part of the allocation.)
+    if (PAIR) cluster_sync_all();
     if (warp == 2) tmem_alloc<PAIR>(slot, S::COLUMNS);
     fence_before_sync();
     __syncthreads();
-    if (PAIR) cluster_sync_all();
     fence_after_sync();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(raw + (slot - smem_u32(raw)));
     // this CTA's part of the contraction (of a pair: all of it).  Those who share one leave two stages to what they send
@@ -135,6 +136,7 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const _
     if (!joined) cluster_arrive();
     const uint32_t first = (uint32_t)((uint64_t)a.steps * part / parts), steps = (uint32_t)((uint64_t)a.steps * (part + 1) / parts) - first;
     qesgd_wait_for_previous();
+    qesgd_let_next_start();   // its CTAs come to SMs that have room: this grid has no second wave
 
     if (warp == 0 && elect_one()) {
         uint32_t s = 0, turn = 0;   // the stage, and how often all of them have been gone through

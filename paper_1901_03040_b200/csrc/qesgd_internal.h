@@ -76,7 +76,8 @@ static const uint64_t QESGD_LR_WORK_FLOATS = (1ull << 20) - QESGD_LR_EPOCH_FLOAT
 // launched plainly, start when all before them is done and contain
 // no such wait, so they must not be given the attribute without one (in the epoch kernel ahead of the
 // producers' first copy and the consumers' loads of u).  No kernel but the small grids
-// of the 4-bit quantiser lets its successor start earlier than at its own end: a waiting grid would take resident slots.  Without the overlap a
+// of the 4-bit quantiser and the tensor-core products (all of whose CTAs are resident from the start) lets its successor
+// start earlier than at its own end: a waiting grid would take resident slots.  Without the overlap a
 // kernel costs a whole number of about 2.05 us in a stream: encode + decode-average-apply of 4 x 30000
 // 11.3 -> 5.9 us, of 8 x 10^6 18.5 -> 14.4, decode of 2^24 13.9 -> 11.3, a logistic step of 64 x 2^22
 // 319 -> 311, and no grid was found that is slower.  (With griddepcontrol.launch_dependents at the top of

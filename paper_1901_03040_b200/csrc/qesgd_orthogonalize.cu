@@ -435,19 +435,19 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
         prefetch_map(&maps.p);
         prefetch_map(&maps.q);
     }
-    if (PAIR) cluster_sync_all();   // both CTAs of the pair are there
+    // Both CTAs of a pair are there, and their barriers.  (The first product of a pair waits for copies that its other CTA
+    // sets off behind its own part of the allocation.)
+    if (PAIR) cluster_sync_all();
     if (warp == 2) tmem_alloc<PAIR>(slot, S::COLUMNS);
     fence_before_sync();
     __syncthreads();
-    if (PAIR) cluster_sync_all();
     fence_after_sync();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(raw + (slot - smem_u32(raw)));
     const uint32_t all = a.tiles * a.batch, every = (a.depth + DEPTH - 1) / DEPTH;
     const uint32_t step0 = every * part_k / parts, steps = every * (part_k + 1) / parts - step0;
     qesgd_wait_for_previous();
+    qesgd_let_next_start();   // its CTAs come to SMs that this kernel has left: no grid of these kernels has a second wave
 
-    // the warp that stores has nothing that the others of a cluster wait for
-    if (parts > 1 && warp == 3) cluster_arrive();
     if (warp == 0 && elect_one()) {
         uint32_t n = 0;
         const uint32_t full_lead = PAIR ? map_shared(full, 0) : full;
@@ -515,26 +515,34 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
             }
         }
         if (*stop) drain();
-    } else if (warp == 3 && elect_one()) {
-        uint32_t n = 0;
-        const bool store = MODE != UPDATE || !a.out || a.out_tiled;
-        for (uint32_t t = group; t < all && !*stop; t += groups) {
-            const Tile x = tile_of<MODE>(t, a);
-            for (uint32_t b = box_first; b < box_end; ++b, ++n) {
-                const uint32_t s = n % S::SLOTS, from = ring + s * S::SLOT_BYTES;
-                if (!pipe_wait(worked + 8 * s, (n / S::SLOTS) & 1u, stop)) break;
-                const uint32_t col = x.j * S::SIDE + b * BOX_COLS, row = x.i * S::SIDE + own_rows;
-                if (store && col < a.cols && row < a.rows) {
-                    tma_store_3d(&maps.out, col, row, x.batch, from);
-                    if (MODE == UPDATE && a.lo_out) tma_store_3d(&maps.out_lo, col, row, x.batch, from + OPERAND_BYTES);
-                }
-                store_commit();
-                store_wait_read<0>();
-                mbar_arrive_at(stored + 8 * s);
-            }
+    } else if (warp == 3) {
+        if (parts > 1) {   // the barriers of the cluster come before the box that this warp stores
+            cluster_arrive();
+            cluster_wait();
+            cluster_arrive();
+            cluster_wait();
         }
-        store_wait<0>();
-        if (*stop) drain();
+        if (elect_one()) {
+            uint32_t n = 0;
+            const bool store = MODE != UPDATE || !a.out || a.out_tiled;
+            for (uint32_t t = group; t < all && !*stop; t += groups) {
+                const Tile x = tile_of<MODE>(t, a);
+                for (uint32_t b = box_first; b < box_end; ++b, ++n) {
+                    const uint32_t s = n % S::SLOTS, from = ring + s * S::SLOT_BYTES;
+                    if (!pipe_wait(worked + 8 * s, (n / S::SLOTS) & 1u, stop)) break;
+                    const uint32_t col = x.j * S::SIDE + b * BOX_COLS, row = x.i * S::SIDE + own_rows;
+                    if (store && col < a.cols && row < a.rows) {
+                        tma_store_3d(&maps.out, col, row, x.batch, from);
+                        if (MODE == UPDATE && a.lo_out) tma_store_3d(&maps.out_lo, col, row, x.batch, from + OPERAND_BYTES);
+                    }
+                    store_commit();
+                    store_wait_read<0>();
+                    mbar_arrive_at(stored + 8 * s);
+                }
+            }
+            store_wait<0>();
+            if (*stop) drain();
+        }
     } else if (warp >= 4) {
         const uint32_t quarter = warp % 4u, r = quarter * 32u + lane, part = (warp - 4u) / 4u, thread = threadIdx.x - 128u;
         const uint32_t free_lead = PAIR ? map_shared(free_, 0) : free_;
@@ -558,17 +566,22 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
             ok = __all_sync(FULL, ok && pipe_wait(done + 8 * half, (done_tiles / 2) & 1u, stop));
             fence_after_sync();
             if (parts > 1) {
-                // all products of this CTA are done: the sums that others finish go where the stages were, by four columns
+                // all of the cluster are through with their stages: the sums of a box go to the CTA that finishes it, by four columns
+                __syncwarp();
+                cluster_arrive();
+                cluster_wait();
                 for (uint32_t b = 0; b < BOXES; ++b) {
                     if (b == rank) continue;
                     float v[TAKEN];
                     __syncwarp();
                     tmem_load16(tmem + (quarter * 32u << 16) + b * BOX_COLS + part * TAKEN, v);
                     tmem_wait_load();
+                    const uint32_t to = map_shared(base + ((rank * (BOX_COLS / 4) + part * (TAKEN / 4)) * 128u + r) * 16u, b);
 #pragma unroll
                     for (int i = 0; i < TAKEN / 4; ++i)
-                        store_shared(base + (((b * BOX_COLS + part * TAKEN) / 4 + i) * 128u + r) * 16u,
-                                     make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])));
+                        asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + i * 2048u), "f"(v[4 * i]), "f"(v[4 * i + 1]), "f"(v[4 * i + 2]),
+                                     "f"(v[4 * i + 3])
+                                     : "memory");
                 }
                 __syncwarp();
                 cluster_arrive();
@@ -589,20 +602,14 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
                         v[k] = 0.0f;
                     }
                     for (uint32_t p = 0; p < parts; ++p) {   // in the order of the contraction
-                        const uint32_t from = map_shared(base + (first / 4u * 128u + r) * 16u, p);
-                        float4 f[TAKEN / 4];
-                        if (p != rank)
-#pragma unroll
-                            for (int i = 0; i < TAKEN / 4; ++i)
-                                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                                             : "=f"(f[i].x), "=f"(f[i].y), "=f"(f[i].z), "=f"(f[i].w)
-                                             : "r"(from + i * 2048u));
 #pragma unroll
                         for (int i = 0; i < TAKEN / 4; ++i) {
-                            v[4 * i] += p == rank ? mine[4 * i] : f[i].x;
-                            v[4 * i + 1] += p == rank ? mine[4 * i + 1] : f[i].y;
-                            v[4 * i + 2] += p == rank ? mine[4 * i + 2] : f[i].z;
-                            v[4 * i + 3] += p == rank ? mine[4 * i + 3] : f[i].w;
+                            uint4 f = make_uint4(__float_as_uint(mine[4 * i]), __float_as_uint(mine[4 * i + 1]), __float_as_uint(mine[4 * i + 2]), __float_as_uint(mine[4 * i + 3]));
+                            if (p != rank) f = load_shared(base + ((p * (BOX_COLS / 4) + part * (TAKEN / 4) + i) * 128u + r) * 16u);
+                            v[4 * i] += __uint_as_float(f.x);
+                            v[4 * i + 1] += __uint_as_float(f.y);
+                            v[4 * i + 2] += __uint_as_float(f.z);
+                            v[4 * i + 3] += __uint_as_float(f.w);
                         }
                     }
                 } else if (b + 1 == BOXES) {   // the last of the tile is in registers
@@ -625,10 +632,9 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
         }
     }
     __syncwarp();
-    if (parts > 1) {
-        if (warp < 3) cluster_arrive();
-        if (warp < 4) cluster_wait();
-        cluster_sync_all();   // the others have read this CTA's sums
+    if (parts > 1 && warp < 3) {
+        cluster_sync_all();
+        cluster_sync_all();
     }
     __syncthreads();
     if (threadIdx.x == 0 && *stop) atomicOr(a.status, QESGD_STATUS_TIMEOUT);
