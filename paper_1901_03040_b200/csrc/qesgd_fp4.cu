@@ -192,7 +192,6 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_quantize_rows_kernel(const 
     __shared__ float inverse[128];
     if (FORMAT == QESGD_FP4_NV) fill_inverse(inverse);
     qesgd_wait_for_previous();
-    if (a.small) qesgd_let_next_start();
     const uint32_t o = threadIdx.x % 16u, line = threadIdx.x / 16u;
     const uint32_t col_tiles = (uint32_t)((a.cols + ROW_COLS - 1) / ROW_COLS);
     const uint64_t tiles = (uint64_t)col_tiles * ((a.rows + TILE_ROWS - 1) / TILE_ROWS * 2);
@@ -269,7 +268,6 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_quantize_columns_kernel(con
     if (FORMAT == QESGD_FP4_NV) fill_inverse(inverse);
     __syncthreads();
     qesgd_wait_for_previous();
-    if (a.small) qesgd_let_next_start();
     const uint32_t col_tiles = (uint32_t)((a.cols + SIDE - 1) / SIDE);
     const uint64_t tiles = (uint64_t)col_tiles * ((a.rows + SIDE - 1) / SIDE);
     const uint64_t padded = (a.cols + 31) / 32 * 32, padded_t = (a.rows + 31) / 32 * 32;
@@ -526,11 +524,10 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_tensor_exponent_kernel(cons
 }
 
 template <typename T, int FORMAT, bool SCALED, bool STOCHASTIC>
-cudaError_t launch_quantize(Fp4QuantizeArgs a, cudaStream_t stream)
+cudaError_t launch_quantize(const Fp4QuantizeArgs &a, cudaStream_t stream)
 {
     const uint64_t tiles = qesgd_div_up(a.rows, TILE_ROWS) * (a.codes_t ? qesgd_div_up(a.cols, SIDE) : 2 * qesgd_div_up(a.cols, ROW_COLS));
     const dim3 grid((unsigned)(tiles < 0x7FFFFFFF ? tiles : 0x7FFFFFFF));
-    a.small = tiles <= 128;
     if (!a.codes_t) return qesgd_launch(qesgd_fp4_quantize_rows_kernel<T, FORMAT, SCALED, STOCHASTIC>, grid, dim3(THREADS), stream, a);
     const auto kernel = qesgd_fp4_quantize_columns_kernel<T, FORMAT, SCALED, STOCHASTIC>;
     const int smem = SIDE * SIDE * (int)sizeof(T);

@@ -136,7 +136,6 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const _
     if (!joined) cluster_arrive();
     const uint32_t first = (uint32_t)((uint64_t)a.steps * part / parts), steps = (uint32_t)((uint64_t)a.steps * (part + 1) / parts) - first;
     qesgd_wait_for_previous();
-    qesgd_let_next_start();   // its CTAs come to SMs that have room: this grid has no second wave
 
     if (warp == 0 && elect_one()) {
         uint32_t s = 0, turn = 0;   // the stage, and how often all of them have been gone through

@@ -75,8 +75,7 @@ static const uint64_t QESGD_LR_WORK_FLOATS = (1ull << 20) - QESGD_LR_EPOCH_FLOAT
 // minibatch the same way).  The cooperative local-epoch kernels and the debug build's range self-test do not: they are
 // launched plainly, start when all before them is done and contain
 // no such wait, so they must not be given the attribute without one (in the epoch kernel ahead of the
-// producers' first copy and the consumers' loads of u).  No kernel but the small grids
-// of the 4-bit quantiser and the tensor-core products (all of whose CTAs are resident from the start) lets its successor
+// producers' first copy and the consumers' loads of u).  No kernel lets its successor
 // start earlier than at its own end: a waiting grid would take resident slots.  Without the overlap a
 // kernel costs a whole number of about 2.05 us in a stream: encode + decode-average-apply of 4 x 30000
 // 11.3 -> 5.9 us, of 8 x 10^6 18.5 -> 14.4, decode of 2^24 13.9 -> 11.3, a logistic step of 64 x 2^22
@@ -127,9 +126,6 @@ inline cudaError_t qesgd_launch(void (*kernel)(Params...), dim3 grid, dim3 block
 }
 #ifdef __CUDACC__
 __device__ __forceinline__ void qesgd_wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-// The next kernel of the stream may be set up now (its own wait still lasts until this one is done): for small grids only,
-// which leave it room.
-__device__ __forceinline__ void qesgd_let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 #endif
 
 struct EncodeArgs {
@@ -192,7 +188,6 @@ struct Fp4QuantizeArgs {
     uint8_t *codes, *scales;        // blocks along the rows; may be null
     uint8_t *codes_t, *scales_t;    // the transpose; may be null
     uint32_t vec;                   // x and its rows 16-byte aligned
-    uint32_t small;                 // a grid that leaves the next kernel room
     uint32_t *status;
 };
 struct Fp4DequantizeArgs {

@@ -383,11 +383,14 @@ __device__ __forceinline__ void store_rows(uint32_t batch, uint32_t row0, uint32
     }
 }
 
-template <int MODE, bool PAIR>
+// DEEP: an update whose contraction is long has five stages, and two slots in the second ring, in place of four and three.
+// Pairs: 4096 x 8192 2062 us in place of 2090 (five steps), 2048 x 2048 338 in place of 360; 12 x 512 x 2048 261 in place of 250,
+// 4 x 1024 x 4096 413 in place of 403: from contractions of 2048 on.
+template <int MODE, bool PAIR, bool DEEP>
 struct Shape {
     static constexpr uint32_t SIDE = PAIR ? 256 : 128;       // a tile is square
-    static constexpr int STAGES = MODE == UPDATE ? 4 : 5;
-    static constexpr int SLOTS = 3;                          // of the second ring
+    static constexpr int STAGES = MODE == UPDATE && !DEEP ? 4 : 5;
+    static constexpr int SLOTS = MODE == UPDATE && DEEP ? 2 : 3;   // of the second ring
     static constexpr uint32_t STAGE_BYTES = 2 * OPERAND_BYTES;   // of one CTA: 128 rows of either operand
     static constexpr uint32_t SLOT_BYTES = (MODE == UPDATE ? 2 : 1) * OPERAND_BYTES;
     static constexpr uint32_t COLUMNS = 2 * SIDE;            // of tensor memory: two tiles
@@ -396,10 +399,10 @@ struct Shape {
 
 __device__ __forceinline__ void takers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(TAKERS * 32) : "memory"); }
 
-template <int MODE, bool PAIR>
+template <int MODE, bool PAIR, bool DEEP>
 __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(const __grid_constant__ ProductArgs a, const __grid_constant__ ProductMaps maps)
 {
-    using S = Shape<MODE, PAIR>;
+    using S = Shape<MODE, PAIR, DEEP>;
     constexpr uint32_t BOXES = S::SIDE / BOX_COLS;                   // of a tile, for each CTA
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u, ring = base + S::STAGES * S::STAGE_BYTES;
@@ -446,7 +449,6 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
     const uint32_t all = a.tiles * a.batch, every = (a.depth + DEPTH - 1) / DEPTH;
     const uint32_t step0 = every * part_k / parts, steps = every * (part_k + 1) / parts - step0;
     qesgd_wait_for_previous();
-    qesgd_let_next_start();   // its CTAs come to SMs that this kernel has left: no grid of these kernels has a second wave
 
     if (warp == 0 && elect_one()) {
         uint32_t n = 0;
@@ -1080,11 +1082,11 @@ bool half_map(CUtensorMap *map, const void *p, uint64_t rows, uint64_t cols, uin
                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int MODE, bool PAIR>
+template <int MODE, bool PAIR, bool DEEP>
 cudaError_t launch_product(ProductArgs a, const ProductMaps &maps, uint32_t split, int sm_count, cudaStream_t stream)
 {
-    using S = Shape<MODE, PAIR>;
-    const auto kernel = qesgd_ortho_product_kernel<MODE, PAIR>;
+    using S = Shape<MODE, PAIR, DEEP>;
+    const auto kernel = qesgd_ortho_product_kernel<MODE, PAIR, DEEP>;
     a.tiles_m = (a.rows + S::SIDE - 1) / S::SIDE;
     a.tiles_n = (a.cols + S::SIDE - 1) / S::SIDE;
     a.tiles = MODE == UPDATE ? a.tiles_m * a.tiles_n : a.tiles_m * (a.tiles_m + 1) / 2;
@@ -1114,8 +1116,8 @@ cudaError_t launch_product(const ProductArgs &a, const ProductMaps &maps, int sm
         if (s > 1 && (singles * s > sms || steps < 4 * s)) break;
         static QesgdClusters known;
         static std::atomic<uint64_t> told{0};
-        const void *const kernel = (const void *)qesgd_ortho_product_kernel<MODE, false>;
-        const uint32_t smem = Shape<MODE, false>::SMEM;
+        const void *const kernel = (const void *)qesgd_ortho_product_kernel<MODE, false, false>;
+        const uint32_t smem = Shape<MODE, false, false>::SMEM;
         if (s > 1 && qesgd_prepare(told, kernel, (int)smem, false) != cudaSuccess) break;
         const double active = s > 1 ? (double)qesgd_active_clusters(known, kernel, WARPS * 32, smem, s) : sms;
         const double t = waves(singles, active) * (double)(uint64_t)((steps + s - 1) / s) * stage(singles * s, 450, 650) + 2500 + (s > 1 ? 2000 : 0);
@@ -1124,7 +1126,9 @@ cudaError_t launch_product(const ProductArgs &a, const ProductMaps &maps, int sm
             split = s;
         }
     }
-    return split == 0 ? launch_product<MODE, true>(a, maps, 1, sm_count, stream) : launch_product<MODE, false>(a, maps, split, sm_count, stream);
+    if (split != 0) return launch_product<MODE, false, false>(a, maps, split, sm_count, stream);
+    if (MODE == UPDATE && a.depth >= 2048) return launch_product<MODE, true, MODE == UPDATE>(a, maps, 1, sm_count, stream);
+    return launch_product<MODE, true, false>(a, maps, 1, sm_count, stream);
 }
 
 }  // namespace
