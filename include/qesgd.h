@@ -27,8 +27,8 @@
  *     16 bytes.
  *   - Calls enqueue work on the context's stream and return without waiting;
  *     only qesgd_status and qesgd_destroy synchronise.  The codec calls (encode,
- *     encode_batch, requantize, decode, decode_average_apply/_axpy) do nothing but
- *     launch kernels on that stream, so they may be recorded by CUDA stream capture
+ *     encode_batch, requantize, decode, decode_average_apply/_axpy) and the matrix
+ *     operators do nothing but launch kernels (or set memory) on that stream, so they may be recorded by CUDA stream capture
  *     and replayed as a graph (worth it when a launch is as short as a host call).
  *   - Return value: QESGD_OK or a negative error code.  Nothing is enqueued
  *     when an error is returned.  No call aborts or throws.
@@ -75,7 +75,7 @@ extern "C" {
 
 #define QESGD_STATUS_NONFINITE 1u /* a bucket held NaN/Inf or its norm overflowed fp32; a block of 4-bit
                                      numbers or a matrix to be made orthogonal held NaN/Inf */
-#define QESGD_STATUS_TIMEOUT 2u   /* a bounded wait inside the local-epoch kernel ran out   */
+#define QESGD_STATUS_TIMEOUT 2u   /* a bounded wait inside a local-epoch or tensor-core kernel ran out */
 #define QESGD_STATUS_RANGE 4u     /* debug build only: a codec kernel computed an index outside
                                      its buffer; the access was skipped                       */
 
@@ -387,8 +387,8 @@ int qesgd_fp4_dequantize(qesgd_ctx *ctx, const uint8_t *codes, const uint8_t *sc
 /* C = A B^T, or C + A B^T where accumulate is not 0: A is M x K, B is N x K, both of one format,
  * C is M rows of ldc elements of type dtype.  A linear layer with weight W (out x in): Y = X W^T;
  * dX = dY W as dY by the transpose of W; dW = dY^T X as the transposes of both.  Accumulation in
- * fp32, multiplied by 2^(ta + tb), C added in fp32, rounded once to dtype.  K = 0 gives zeros (or
- * leaves C as it is); C must not overlap an operand. */
+ * fp32, multiplied by 2^(ta + tb), C added in fp32, rounded once to dtype; the same bits in every run.
+ * K = 0 gives zeros (or leaves C as it is); C must not overlap an operand. */
 int qesgd_fp4_matmul(qesgd_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_scales,
                      const int32_t *a_exponent, const uint8_t *b_codes, const uint8_t *b_scales,
                      const int32_t *b_exponent, uint64_t M, uint64_t N, uint64_t K, uint32_t format,
@@ -405,8 +405,8 @@ int qesgd_fp4_matmul(qesgd_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_sc
  * dtype); out: the same in BF16 (ldo, out_stride), which may be x itself where the layouts agree.
  * The products take fp16 operands (scaled by powers of two) and accumulate in fp32; the term a X of
  * the first three steps carries 22 bits.  Five usual steps end 2e-3 of the result from the exact
- * one, of which 1.7e-3 is the final rounding to BF16.  a, b, c finite, |a| <= 16, |b|, |c| <= 32; should they let
- * singular values grow beyond 100 the result saturates.  A matrix of zeros gives zeros; one with a
+ * one, of which 1.7e-3 is the final rounding to BF16.  a, b, c finite, |a| <= 16, |b|, |c| <= 32; where they let
+ * singular values grow beyond 3, intermediates are cut off at fp16's largest number.  A matrix of zeros gives zeros; one with a
  * non-finite element gives zeros and QESGD_STATUS_NONFINITE, the others of the batch are not
  * touched by it.
  * workspace: qesgd_orthogonalize_workspace(rows, cols, batch) bytes of device memory, 256-byte

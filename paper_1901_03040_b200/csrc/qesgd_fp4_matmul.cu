@@ -303,6 +303,22 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const _
     if (warp == 2) tmem_dealloc<PAIR>(tmem, S::COLUMNS);
 }
 
+// A contraction over nothing.
+template <typename T>
+__global__ __launch_bounds__(256) void qesgd_fp4_zeros_kernel(T *c, uint64_t M, uint64_t N, uint64_t ldc)
+{
+    qesgd_wait_for_previous();
+    for (uint64_t m = blockIdx.y; m < M; m += gridDim.y)
+        for (uint64_t n = (uint64_t)blockIdx.x * 256 + threadIdx.x; n < N; n += (uint64_t)gridDim.x * 256) c[m * ldc + n] = T(0);
+}
+template <typename T>
+cudaError_t launch_zeros(const Fp4MatmulArgs &a, cudaStream_t stream)
+{
+    const uint64_t x = qesgd_div_up(a.N, 256);
+    return qesgd_launch(qesgd_fp4_zeros_kernel<T>, dim3((unsigned)(x < 4096 ? x : 4096), (unsigned)(a.M < 65535 ? a.M : 65535)), dim3(256), stream,
+                        static_cast<T *>(a.c), a.M, a.N, a.ldc);
+}
+
 // rows of `bytes` bytes; a box is 128 bytes of box_rows rows, swizzled
 bool codes_map(CUtensorMap *map, const uint8_t *p, uint64_t rows, uint64_t bytes, uint32_t box_rows)
 {
@@ -388,6 +404,7 @@ int launch(const Fp4MatmulArgs &a, uint32_t dtype, int sm_count, cudaStream_t st
 int qesgd_launch_fp4_matmul(const Fp4MatmulArgs &a, uint32_t dtype, uint32_t format, int sm_count, cudaStream_t stream, int *launched)
 {
     *launched = 1;
+    if (a.K == 0) return (int)(dtype == QESGD_F32 ? launch_zeros<uint32_t>(a, stream) : launch_zeros<uint16_t>(a, stream));
     if (format == QESGD_FP4_MX) return a.accumulate ? launch<true, true>(a, dtype, sm_count, stream) : launch<true, false>(a, dtype, sm_count, stream);
     return a.accumulate ? launch<false, true>(a, dtype, sm_count, stream) : launch<false, false>(a, dtype, sm_count, stream);
 }

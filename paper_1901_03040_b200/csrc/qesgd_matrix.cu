@@ -130,10 +130,6 @@ int qesgd_fp4_matmul(qesgd_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_sc
     if (K > 0 && (!valid_held(a_codes, a_scales) || !valid_held(b_codes, b_scales))) return QESGD_EINVAL;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return qesgd_cuda_fail(ctx, (int)cudaErrorInvalidDevice);
-    if (K == 0) {
-        const cudaError_t e = cudaMemset2DAsync(c, ldc * element_bytes(dtype), 0, N * element_bytes(dtype), M, ctx->stream);
-        return e == cudaSuccess ? QESGD_OK : qesgd_cuda_fail(ctx, (int)e);
-    }
     const Fp4MatmulArgs a = {a_codes, a_scales, b_codes, b_scales, a_exponent, b_exponent, M, N, K, ldc, c, accumulate ? 1u : 0u, ctx->d_status};
     int launched = 0;
     const int e = qesgd_launch_fp4_matmul(a, dtype, format, ctx->sm_count, ctx->stream, &launched);

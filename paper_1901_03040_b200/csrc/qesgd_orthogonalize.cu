@@ -1177,7 +1177,7 @@ int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t st
         *launched += 1;
         p.cols = (uint32_t)l.n;
         p.lo_in = step < ORTHO_LO_STEPS;
-        p.lo_out = step + 1 < ORTHO_LO_STEPS;
+        p.lo_out = step + 1 < ORTHO_LO_STEPS && step + 1 < a.steps;
         if (step + 1 == a.steps) {
             p.out = static_cast<__nv_bfloat16 *>(a.out);
             p.ldo = a.ldo;

@@ -491,6 +491,156 @@ def test_other_streams_and_captured_graphs():
         c.close()
 
 
+_FIRST_CALLS = r"""
+import sys, torch
+sys.path.insert(0, sys.argv[1])
+from paper_1901_03040_b200 import qesgd
+torch.cuda.set_device(0)
+stream = torch.cuda.Stream()
+ctx = qesgd.Context(0, stream)
+x = torch.randn(130, 300, device="cuda")
+codes, scales = qesgd.alloc_fp4(130, 300, qesgd.FP4_NV, "cuda")
+codes_t, scales_t = qesgd.alloc_fp4(300, 130, qesgd.FP4_NV, "cuda")
+e = torch.zeros(1, dtype=torch.int32, device="cuda")
+c, back = torch.zeros(130, 130, device="cuda"), torch.zeros(130, 300, device="cuda")
+o, small = torch.zeros(130, 300, dtype=torch.bfloat16, device="cuda"), torch.zeros(20, 300, dtype=torch.bfloat16, device="cuda")
+need = qesgd.orthogonalize_workspace(130, 300)
+work = torch.empty(need, dtype=torch.uint8, device="cuda")
+def run():
+    ctx.qesgd_fp4_tensor_exponent(x, 0, 130, 300, 300, e)
+    ctx.qesgd_fp4_quantize(x, 0, 130, 300, 300, qesgd.FP4_NV, e, 1, 7, 0, 0, codes, scales, codes_t, scales_t)
+    ctx.qesgd_fp4_dequantize(codes, scales, 130, 300, qesgd.FP4_NV, e, back, 0, 300)
+    ctx.qesgd_fp4_matmul(codes, scales, e, codes, scales, e, 130, 130, 300, qesgd.FP4_NV, c, 0, 130)
+    ctx.qesgd_orthogonalize(x, 0, 130, 300, 300, 1, 0, 5, o, 300, 0, work, need)
+    ctx.qesgd_orthogonalize(x, 0, 20, 300, 300, 1, 0, 5, small, 300, 0, work, need)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g, stream=stream):
+    run()
+g.replay()
+torch.cuda.synchronize()
+got = [t.clone() for t in (codes, codes_t, back, c, o, small)]
+for t in (codes, codes_t, back, c, o, small):
+    t.zero_()
+torch.cuda.synchronize()
+run()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, (codes, codes_t, back, c, o, small)))
+assert float(o.float().abs().sum()) > 0 and ctx.qesgd_status() == 0
+ctx.close()
+print("first calls captured")
+"""
+
+
+def test_the_first_calls_of_a_process_may_be_captured():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    out = subprocess.run([sys.executable, "-c", _FIRST_CALLS, root], capture_output=True, text=True, timeout=300)
+    assert out.returncode == 0 and "first calls captured" in out.stdout, (out.stdout + out.stderr)[-3000:]
+
+
+def test_two_host_threads_with_a_context_each():
+    import threading
+    rows, cols, errors = 260, 410, []
+    want = _np(_orthogonalize(_gradient(1, rows, cols, qesgd.F32, 3), qesgd.F32, rows, cols))
+    x = _gradient(1, rows, cols, qesgd.F32, 3)
+
+    def work(i):
+        try:
+            torch.cuda.set_device(0)
+            ctx = qesgd.Context(0, torch.cuda.Stream())
+            need = qesgd.orthogonalize_workspace(rows, cols)
+            out = torch.empty((rows, cols), dtype=torch.bfloat16, device="cuda")
+            ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+            torch.cuda.synchronize()
+            for _ in range(20):
+                ctx.qesgd_orthogonalize(x, qesgd.F32, rows, cols, cols, 1, 0, 5, out, cols, 0, ws, need)
+            assert ctx.qesgd_status() == 0
+            if not (_np(out) == want[0]).all():
+                errors.append(i)
+            ctx.close()
+        except Exception as exc:  # noqa: BLE001
+            errors.append(exc)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors
+
+
+def test_offsets_beyond_32_bits():
+    """Rows so far apart that their offsets pass 2^32 elements: quantise, dequantise, product, orthogonal update."""
+    rows, cols, ld = 140, 300, 32_000_001            # 4.48e9 elements, 9 GB
+    if torch.cuda.mem_get_info()[0] < 12 << 30:
+        pytest.skip("too little memory")
+    buf = torch.empty(rows * ld, dtype=torch.bfloat16, device="cuda")
+    x = torch.as_strided(buf, (rows, cols), (ld, 1))
+    x.copy_(_x(rows, cols, qesgd.BF16, 5))
+    small = x.contiguous()
+    ctx = G.ctx()
+    for fmt in FORMATS:
+        far, _ = _quantize(x, cols, fmt, "rc", dtype=qesgd.BF16)
+        _check_held(far, _np(small), fmt)
+        near = torch.empty((rows, cols), dtype=torch.bfloat16, device="cuda")
+        ctx.qesgd_fp4_dequantize(*far["r"], rows, cols, fmt, None, near, qesgd.BF16, cols)
+        product = torch.empty((rows, rows), dtype=torch.bfloat16, device="cuda")
+        ctx.qesgd_fp4_matmul(*far["r"], None, *far["r"], None, rows, rows, cols, fmt, product, qesgd.BF16, rows)
+        o = _orthogonalize(small[None], qesgd.BF16, rows, cols)[0]
+        for view, want, call in (
+                ((rows, cols), near, lambda v: ctx.qesgd_fp4_dequantize(*far["r"], rows, cols, fmt, None, v, qesgd.BF16, ld)),
+                ((rows, rows), product, lambda v: ctx.qesgd_fp4_matmul(*far["r"], None, *far["r"], None, rows, rows, cols, fmt, v, qesgd.BF16, ld))):
+            v = torch.as_strided(buf, view, (ld, 1))
+            call(v)
+            assert torch.equal(v, want)
+        x.copy_(small)
+        need = qesgd.orthogonalize_workspace(rows, cols)
+        work = torch.empty(need, dtype=torch.uint8, device="cuda")
+        ctx.qesgd_orthogonalize(x, qesgd.BF16, rows, cols, ld, 1, 0, 5, x, ld, 0, work, need)
+        assert torch.equal(x, o)
+        x.copy_(small)
+        e = torch.empty(1, dtype=torch.int32, device="cuda")
+        ctx.qesgd_fp4_tensor_exponent(x, qesgd.BF16, rows, cols, ld, e)
+        assert int(e) == ref.tensor_exponent(_np(small))
+    assert ctx.qesgd_status() == 0
+
+
+def test_more_than_2_to_31_elements():
+    rows, cols = 70_000, 40_000                      # 2.8e9 elements
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("too little memory")
+    x = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")
+    for r in (0, 127, 53_000, 69_900):
+        x[r:r + 100] = torch.randn((min(100, rows - r), cols), generator=torch.Generator(device="cuda").manual_seed(r), device="cuda")
+    ctx, fmt = G.ctx(), qesgd.FP4_MX
+    held = qesgd.alloc_fp4(rows, cols, fmt, "cuda")
+    held_t = qesgd.alloc_fp4(cols, rows, fmt, "cuda")
+    ctx.qesgd_fp4_quantize(x, qesgd.BF16, rows, cols, cols, fmt, None, qesgd.ROUND_STOCHASTIC, 3, 1, 2, *held, *held_t)
+    back = torch.empty((rows, cols), dtype=torch.bfloat16, device="cuda")
+    ctx.qesgd_fp4_dequantize(*held, rows, cols, fmt, None, back, qesgd.BF16, cols)
+    for r in (0, 53_000, 69_900):
+        part = _np(x[r:r + 100])
+        codes, byte, _ = ref.quantize(part, fmt)
+        index = (np.arange(r, r + part.shape[0])[:, None] * cols + np.arange(cols)[None, :])      # cols is a multiple of 32
+        q = np.abs(part) / np.repeat(ref.E8M0[byte], 32, 1)[:, :cols]
+        low = np.searchsorted(ref.GRID, q, side="right") - 1
+        gap = np.where(low < 7, ref.GRID[np.minimum(low + 1, 7)] - ref.GRID[low], 1.0)
+        up = (ref.draws(index, 3, 1, 2) + 0.5) / 65536.0 < (q - ref.GRID[low]) / gap
+        want = np.sign(part) * ref.GRID[np.minimum(low + up, 7)] * np.repeat(ref.E8M0[byte], 32, 1)[:, :cols]
+        assert (_np(back[r:r + 100]) == want).all()
+    # the transpose: its last rows against those of a matrix of their own (rounded to nearest, the draws being others)
+    ctx.qesgd_fp4_quantize(x, qesgd.BF16, rows, cols, cols, fmt, None, qesgd.ROUND_NEAREST, 0, 0, 0, None, None, *held_t)
+    got = torch.empty((cols, rows), dtype=torch.bfloat16, device="cuda")
+    ctx.qesgd_fp4_dequantize(*held_t, cols, rows, fmt, None, got, qesgd.BF16, rows)
+    part = _np(x[:, -40:].T)
+    codes, byte, _ = ref.quantize(part, fmt)
+    assert (_np(got[-40:]) == ref.values(codes, byte, fmt)).all()
+    assert ctx.qesgd_status() == 0
+
+
 def test_refused_calls_enqueue_nothing():
     ctx = G.ctx()
     n = ctx.qesgd_launch_count()
