@@ -398,17 +398,20 @@ __device__ __forceinline__ float scale_value(uint32_t byte)
     return __fmul_rn(__uint_as_float((byte & 0x7Fu) << 20), 0x1p120f);
 }
 
-// A warp takes 256 columns of a row at a time: an octet for each lane where rows of `out` lie on 16 bytes, else neighbouring
-// elements in neighbouring lanes, so that stores of single elements fill whole sectors too.
+// A warp takes 256 columns of a row at a time, an octet for each lane.  Where rows of `out` lie on 16 bytes the octet is
+// stored as it is; else it goes through shared memory, so that neighbouring lanes store neighbouring elements (two at a
+// time where a row of 16-bit elements begins on 4 bytes).
 constexpr int BACK_ROWS = 32, BACK_COLS = 256;
 
 template <typename T, int FORMAT, bool VEC>
 __global__ __launch_bounds__(THREADS) void qesgd_fp4_dequantize_kernel(const __grid_constant__ Fp4DequantizeArgs a)
 {
     constexpr int BLOCK = Format<FORMAT>::BLOCK;
-    constexpr int UNROLL = 4;
+    constexpr int UNROLL = BACK_ROWS / (THREADS / 32);
+    __shared__ __align__(16) T turned[VEC ? 8 : THREADS / 32 * BACK_COLS];
     qesgd_wait_for_previous();
     const uint32_t lane = threadIdx.x % 32u, warp = threadIdx.x / 32u;
+    T *const mine = turned + (VEC ? 0 : warp * BACK_COLS);
     const uint64_t padded = (a.cols + 31) / 32 * 32, scale_tiles = (a.cols + 4 * BLOCK - 1) / (4 * BLOCK);
     const uint32_t col_tiles = (uint32_t)((a.cols + BACK_COLS - 1) / BACK_COLS);
     const uint64_t tiles = (uint64_t)col_tiles * ((a.rows + BACK_ROWS - 1) / BACK_ROWS);
@@ -418,68 +421,65 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_dequantize_kernel(const __g
     for (uint64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const uint64_t row0 = tile / col_tiles * BACK_ROWS;
         const uint32_t col0 = (uint32_t)(tile % col_tiles) * BACK_COLS;
-        // within a tile of scales: rows differ by 16 bytes, BACK_ROWS of them by less than one quarter
+        // within a tile of scales: 32 rows lie 16 bytes apart, then the next quarter begins
+        static_assert(BACK_ROWS == 32, "a quarter of a tile of scales");
         const uint8_t *const scales = a.scales + row0 / 128 * scale_tiles * SCALE_TILE + row0 / 32 % 4 * 4;
-        static_assert(BACK_ROWS == 32, "a row of scales for each of the rows");
         const uint32_t rows = (uint32_t)min((uint64_t)BACK_ROWS, a.rows - row0);
-        if (VEC) {
-            const uint64_t c = col0 + lane * 8u, block = c / BLOCK;
-            if (c >= a.cols) continue;
-            const uint8_t *const at = scales + block / 4 * SCALE_TILE + block % 4 + warp * 16u;
-            const uint8_t *const codes = a.codes + ((row0 + warp) * padded + c) / 2;
-            T *out = static_cast<T *>(a.out) + (row0 + warp) * a.ldo + c;
-            uint32_t w[UNROLL], byte[UNROLL];
+        const uint32_t cols = (uint32_t)min((uint64_t)BACK_COLS, a.cols - col0);   // of this tile
+        const uint32_t c = lane * 8u, block = c / BLOCK;                           // col0 begins a tile of scales
+        const uint8_t *const at = scales + (col0 / (4u * BLOCK) + block / 4u) * SCALE_TILE + block % 4u + warp * 16u;
+        const uint8_t *const codes = a.codes + ((row0 + warp) * padded + col0 + c) / 2;
+        T *out = static_cast<T *>(a.out) + (row0 + warp) * a.ldo + col0;
+        uint32_t w[UNROLL], byte[UNROLL];
 #pragma unroll
-            for (int i = 0; i < UNROLL; ++i) {
-                const bool inside = warp + i * (THREADS / 32) < rows;
-                byte[i] = inside ? at[i * (THREADS / 32) * 16] : 0u;
-                w[i] = inside ? *reinterpret_cast<const uint32_t *>(codes + i * (THREADS / 64) * padded) : 0u;
+        for (int i = 0; i < UNROLL; ++i) {
+            const bool inside = warp + i * (THREADS / 32) < rows && c < cols;
+            byte[i] = inside ? at[i * (THREADS / 32) * 16] : 0u;
+            w[i] = inside ? *reinterpret_cast<const uint32_t *>(codes + i * (THREADS / 64) * padded) : 0u;
+        }
+#pragma unroll
+        for (int i = 0; i < UNROLL; ++i, out += (THREADS / 32) * a.ldo) {
+            if (warp + i * (THREADS / 32) >= rows) break;
+            const float scale = __fmul_rn(scale_value<FORMAT>(byte[i]), near);
+            float f[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 p = values_of((w[i] >> (8 * j)) & 0xFFu);
+                f[2 * j] = __fmul_rn(p.x, scale);
+                f[2 * j + 1] = __fmul_rn(p.y, scale);
             }
+            if (far != 1.0f)
 #pragma unroll
-            for (int i = 0; i < UNROLL; ++i, out += (THREADS / 32) * a.ldo) {
-                if (warp + i * (THREADS / 32) >= rows) break;
-                const float scale = __fmul_rn(scale_value<FORMAT>(byte[i]), near);
-                float f[8];
+                for (int j = 0; j < 8; ++j) f[j] = __fmul_rn(f[j], far);
+            __align__(16) T v[8];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float2 p = values_of((w[i] >> (8 * j)) & 0xFFu);
-                    f[2 * j] = __fmul_rn(p.x, scale);
-                    f[2 * j + 1] = __fmul_rn(p.y, scale);
-                }
-                if (far != 1.0f)
+            for (int j = 0; j < 8; ++j) v[j] = from_float<T>(f[j]);
+            if (VEC) {
+                if (c + 8 <= cols) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) f[j] = __fmul_rn(f[j], far);
-                __align__(16) T v[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = from_float<T>(f[j]);
-                if (c + 8 <= a.cols) {
-#pragma unroll
-                    for (int n = 0; n < (int)sizeof(T) / 2; ++n) reinterpret_cast<uint4 *>(out)[n] = reinterpret_cast<const uint4 *>(v)[n];
+                    for (int n = 0; n < (int)sizeof(T) / 2; ++n) reinterpret_cast<uint4 *>(out + c)[n] = reinterpret_cast<const uint4 *>(v)[n];
                 } else {
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        if (c + j < a.cols) out[j] = v[j];
+                        if (c + j < cols) out[c + j] = v[j];
                 }
+                continue;
             }
-        } else {
-            for (uint32_t r = warp; r < rows; r += THREADS / 32) {
-                const uint8_t *const codes = a.codes + (row0 + r) * (padded / 2);
-                T *const out = static_cast<T *>(a.out) + (row0 + r) * a.ldo;
-                uint32_t held[BACK_COLS / 32], byte[BACK_COLS / 32];
+            __syncwarp();
 #pragma unroll
-                for (uint32_t i = 0; i < BACK_COLS / 32; ++i) {
-                    const uint64_t c = col0 + i * 32u + lane, block = c / BLOCK;
-                    held[i] = c < a.cols ? codes[c / 2] : 0u;
-                    byte[i] = c < a.cols ? scales[block / 4 * SCALE_TILE + r * 16u + block % 4] : 0u;
-                }
+            for (int n = 0; n < (int)sizeof(T) / 2; ++n) reinterpret_cast<uint4 *>(mine + c)[n] = reinterpret_cast<const uint4 *>(v)[n];
+            __syncwarp();
+            if (sizeof(T) == 2 && reinterpret_cast<uintptr_t>(out) % 4 == 0) {
 #pragma unroll
-                for (uint32_t i = 0; i < BACK_COLS / 32; ++i) {
-                    const uint64_t c = col0 + i * 32u + lane;
-                    if (c >= a.cols) break;
-                    const float2 p = values_of(held[i]);
-                    const float scale = __fmul_rn(scale_value<FORMAT>(byte[i]), near);
-                    out[c] = from_float<T>(__fmul_rn(__fmul_rn(c % 2 ? p.y : p.x, scale), far));
+                for (uint32_t j = 0; j < BACK_COLS / 64; ++j) {
+                    const uint32_t n = j * 64u + lane * 2u;
+                    if (n + 2 <= cols) *reinterpret_cast<uint32_t *>(out + n) = *reinterpret_cast<const uint32_t *>(mine + n);
+                    else if (n < cols) out[n] = mine[n];
                 }
+            } else {
+#pragma unroll
+                for (uint32_t j = 0; j < BACK_COLS / 32; ++j)
+                    if (j * 32u + lane < cols) out[j * 32u + lane] = mine[j * 32u + lane];
             }
         }
     }
@@ -488,27 +488,42 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_dequantize_kernel(const __g
 // ------------------------------------------------ exponent of a tensor ----
 // Every CTA raises the result, which starts below any exponent, to that of its own largest magnitude: a maximum of
 // integers, the same whatever the order.
+constexpr uint32_t TOP_COLS = 2048;
 template <typename T>
 __global__ __launch_bounds__(THREADS) void qesgd_fp4_tensor_exponent_kernel(const T *x, uint64_t rows, uint64_t cols, uint64_t ldx, bool vec,
                                                                             int32_t *out, uint32_t *status)
 {
     __shared__ uint32_t tops[THREADS / 32];
     qesgd_wait_for_previous();
-    // a warp takes 256 columns of a row at a time
-    const uint32_t lane = threadIdx.x % 32u;
-    const uint32_t spans = (uint32_t)((cols + 255) / 256);
-    const uint64_t all = (uint64_t)spans * rows, warps = (uint64_t)gridDim.x * (THREADS / 32);
+    // a warp takes a row's 2048 columns, 256 at a time
+    const uint32_t lane = threadIdx.x % 32u, warp = threadIdx.x / 32u;
+    const uint32_t spans = (uint32_t)((cols + TOP_COLS - 1) / TOP_COLS);
+    const uint64_t tiles = (uint64_t)spans * ((rows + THREADS / 32 - 1) / (THREADS / 32));
     uint32_t top = 0u;
     bool bad = false;
-    for (uint64_t n = (uint64_t)blockIdx.x * (THREADS / 32) + threadIdx.x / 32u; n < all; n += warps) {
-        const uint64_t c = n % spans * 256u + lane * 8u;
-        float v[8];
-        values(load_octet(x + n / spans * ldx, c, cols, vec), v);
+    for (uint64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const uint64_t r = tile / spans * (THREADS / 32) + warp;
+        if (r >= rows) continue;
+        const uint64_t first = tile % spans * TOP_COLS;
+        const T *const row = x + r * ldx;
+#pragma unroll 4
+        for (uint32_t i = 0; i < TOP_COLS / 256; ++i) {
+            const uint64_t c = first + i * 256u + lane * 8u;
+            if (c >= cols) break;
+            const Octet<T> o = load_octet(row, c, cols, vec);
+            const uint32_t m = top_of(o);
+            if (m < 0x7F800000u) {
+                top = max(top, m);
+            } else {   // something is not finite: the rest counts
+                float v[8];
+                values(o, v);
+                bad = true;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t m = __float_as_uint(v[j]) & 0x7FFFFFFFu;
-            bad |= m >= 0x7F800000u;
-            top = max(top, m >= 0x7F800000u ? 0u : m);
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t e = __float_as_uint(v[j]) & 0x7FFFFFFFu;
+                    top = max(top, e >= 0x7F800000u ? 0u : e);
+                }
+            }
         }
     }
     top = __reduce_max_sync(FULL, top);
@@ -563,7 +578,7 @@ template <typename T>
 cudaError_t launch_exponent(const void *x, uint64_t rows, uint64_t cols, uint64_t ldx, bool vec, int32_t *out, uint32_t *status,
                             int sm_count, cudaStream_t stream)
 {
-    const uint64_t ctas = qesgd_div_up(qesgd_div_up(cols, 256) * rows, THREADS / 32 * 4), most = (uint64_t)sm_count * 8;
+    const uint64_t ctas = qesgd_div_up(cols, TOP_COLS) * qesgd_div_up(rows, THREADS / 32), most = (uint64_t)sm_count * 8;
     return qesgd_launch(qesgd_fp4_tensor_exponent_kernel<T>, dim3((unsigned)(ctas < most ? ctas : most)), dim3(THREADS), stream,
                         static_cast<const T *>(x), rows, cols, ldx, vec, out, status);
 }

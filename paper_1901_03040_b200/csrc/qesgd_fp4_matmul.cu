@@ -375,27 +375,30 @@ template <bool MX, bool ACCUMULATE>
 int launch(const Fp4MatmulArgs &a, uint32_t dtype, int sm_count, cudaStream_t stream)
 {
     static QesgdClusters known;
-    const uint64_t pairs = qesgd_div_up(a.M, 256) * qesgd_div_up(a.N, 256);
-    if (pairs * 2 >= (uint64_t)sm_count) return launch<true, MX, ACCUMULATE>(a, dtype, 256, 1, sm_count, stream);
-    // Too few tiles for the SMs: as many CTAs share a contraction as bring it to an end first.  A stage of one CTA takes about
-    // 450 clocks to arrive, adding the parts up 2500 and 100 more for each; a cluster larger than the device runs of them
-    // at once for every tile would wait for a second wave.
+    // By modelled clocks: a stage of a pair takes about 700 to arrive and be multiplied, one of a single CTA 450 where others
+    // are few, 600 with all SMs at it.  Too few tiles for the SMs: as many CTAs share a contraction as bring it to an end first;
+    // adding the parts up takes 2500 and 100 more for each, and a cluster larger than the device runs of them at once for
+    // every tile would wait for a second wave.
     const uint32_t q = a.M <= 32 ? 32 : a.M <= 64 ? 64 : 128;
+    const uint64_t sms = (uint64_t)sm_count, pairs = qesgd_div_up(a.M, 256) * qesgd_div_up(a.N, 256);
     const uint64_t tiles = qesgd_div_up(a.M, q) * qesgd_div_up(a.N, 128), steps = qesgd_div_up(a.K, DEPTH);
+    const auto stage = [&](uint64_t ctas) { return 450 + 150 * (ctas < sms ? ctas : sms) / sms; };
+    const uint64_t by_pairs = qesgd_div_up(pairs, sms / 2) * steps * 700 + 1500;
     const void *const kernel = (const void *)qesgd_fp4_matmul_kernel<false, MX, ACCUMULATE>;
     uint32_t split = 1;
-    uint64_t best = qesgd_div_up(tiles, (uint64_t)sm_count) * steps * 450;
+    uint64_t best = qesgd_div_up(tiles, sms) * steps * stage(tiles);
     static std::atomic<uint64_t> told{0};
     const cudaError_t e = qesgd_prepare(told, kernel, Shape<false>::SMEM, true);
     if (e != cudaSuccess) return (int)e;
-    for (uint32_t s = 2; s <= 16 && s <= steps && tiles * s <= (uint64_t)sm_count; ++s) {
+    for (uint32_t s = 2; s <= 16 && s <= steps && tiles * s <= sms; ++s) {
         const uint64_t active = qesgd_active_clusters(known, kernel, WARPS * 32, Shape<false>::SMEM, s);
-        const uint64_t t = qesgd_div_up(tiles, active) * qesgd_div_up(steps, s) * 450 + 2500 + 100 * s;
+        const uint64_t t = qesgd_div_up(tiles, active) * qesgd_div_up(steps, s) * stage(tiles * s) + 2500 + 100 * s;
         if (t < best) {
             best = t;
             split = s;
         }
     }
+    if (by_pairs < best) return launch<true, MX, ACCUMULATE>(a, dtype, 256, 1, sm_count, stream);
     return launch<false, MX, ACCUMULATE>(a, dtype, q, split, sm_count, stream);
 }
 
