@@ -52,18 +52,17 @@ __device__ __forceinline__ int tensor_exponent(const int32_t *p) { return p ? cl
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
 
 // A block's scale, from the bits of its largest magnitude: the byte that is kept, and what its elements are multiplied by
-// (and, NV, divided by).
+// (and, NV, by the reciprocal of s).
 struct Scale {
     uint32_t byte;
     float mul;    // 2^-e (MX), 2^-t (NV)
-    float div;    // s (NV)
-    float inv;    // fl32(1 / s) (NV), 0 for s = 0
+    float2 inv;   // 1 / s in two terms (NV), 0 for s = 0
     bool bad;     // something in the block is not finite
 };
 __device__ __forceinline__ float e4m3(uint32_t code, float factor) { return __fmul_rn(__uint_as_float(code << 20), factor); }   // factor: a power of two or 6 of them, times 2^120
-// inverse: fl32(1 / s) of every E4M3 number, in shared memory (__frcp_rn of each block's takes ten instructions)
+// inverse: 1 / s of every E4M3 number, in shared memory (__frcp_rn of each block's takes ten instructions)
 template <int FORMAT, bool SCALED>
-__device__ __forceinline__ Scale block_scale(uint32_t top, float to_tensor, const float *inverse)
+__device__ __forceinline__ Scale block_scale(uint32_t top, float to_tensor, const float2 *inverse)
 {
     Scale s;
     s.bad = top >= 0x7F800000u;
@@ -72,7 +71,7 @@ __device__ __forceinline__ Scale block_scale(uint32_t top, float to_tensor, cons
         // mantissa carries
         s.byte = s.bad ? 0u : (uint32_t)max((int)((top + 0x3FFFFFu) >> 23) - 2, 0);
         s.mul = __uint_as_float((254u - s.byte) << 23);
-        s.div = s.inv = 1.0f;
+        s.inv = make_float2(1.0f, 0.0f);
     } else {
         // The bits of an E4M3 number are bits 20..26 of the float 2^-120 times it, subnormals included.  A quotient by 6 that is
         // rounded down, and then up to such bits, is right or one number short; 6 s is exact.
@@ -82,28 +81,27 @@ __device__ __forceinline__ Scale block_scale(uint32_t top, float to_tensor, cons
         code = min(code + (e4m3(code, 6.0f * 0x1p120f) < v ? 1u : 0u), 126u);
         if (SCALED) code = max(code, s.bad || top == 0u ? 0u : 1u);   // top * 2^-t may be 0
         s.byte = code;
-        s.div = e4m3(code, 0x1p120f);
         s.inv = inverse[code];
         s.mul = to_tensor;
     }
     return s;
 }
-__device__ __forceinline__ void fill_inverse(float *inverse)
+__device__ __forceinline__ void fill_inverse(float2 *inverse)
 {
-    if (threadIdx.x < 128) inverse[threadIdx.x] = threadIdx.x ? __frcp_rn(e4m3(threadIdx.x, 0x1p120f)) : 0.0f;
+    if (threadIdx.x >= 128) return;
+    const float s = e4m3(threadIdx.x, 0x1p120f), r = threadIdx.x ? __frcp_rn(s) : 0.0f;
+    inverse[threadIdx.x] = make_float2(r, __fmul_rn(__fmaf_rn(-r, s, 1.0f), r));
 }
-// x over the block's scale, correctly rounded.  NV: the quotient by the rounded reciprocal, corrected by its residual; s has
-// 4 significant bits, so a quotient lies on a rounding border or at least 2^-5 units in the last place from it, far
-// more than the correction is off.  SCALED: there is a tensor exponent, and x * 2^-t may leave the float range; an
-// infinite quotient is clipped to 6 either way.
+// x over the block's scale, correctly rounded.  NV: x times 1 / s in two terms is 2^-47 off the quotient at most; s has 4
+// significant bits, so a quotient lies on a rounding border or at least 2^-5 units in the last place from it.  (One
+// term is not enough for 16-bit x either: 1.25 times 1.875 times fl32(1 / 1.875) passes the tie at 1.25.)  SCALED: there is
+// a tensor exponent, and x * 2^-t may leave the float range: it is clipped to 6 either way.
 template <int FORMAT, bool SCALED>
 __device__ __forceinline__ float over_scale(float x, const Scale &s)
 {
     if (FORMAT == QESGD_FP4_MX) return __fmul_rn(x, s.mul);
-    const float y = SCALED ? __fmul_rn(x, s.mul) : x;
-    const float q = __fmul_rn(y, s.inv);
-    const float r = __fmaf_rn(__fmaf_rn(-q, s.div, y), s.inv, q);
-    return !SCALED || fabsf(q) < 3.402823466e38f ? r : q;
+    const float y = SCALED ? fminf(fmaxf(__fmul_rn(x, s.mul), -3.402823466e38f), 3.402823466e38f) : x;
+    return __fmaf_rn(y, s.inv.x, __fmul_rn(y, s.inv.y));
 }
 
 // Eight elements of one block -> their codes.
@@ -163,7 +161,7 @@ __device__ __forceinline__ uint32_t over_block(uint32_t top)
 }
 // Two octets of a row -> two words of codes, and their block's scale.
 template <typename T, int FORMAT, bool SCALED, bool STOCHASTIC>
-__device__ __forceinline__ uint2 quantize_span(const Octet<T> (&x)[2], uint64_t n, float to_tensor, const float *inverse, const Fp4QuantizeArgs &a, Scale &s)
+__device__ __forceinline__ uint2 quantize_span(const Octet<T> (&x)[2], uint64_t n, float to_tensor, const float2 *inverse, const Fp4QuantizeArgs &a, Scale &s)
 {
     s = block_scale<FORMAT, SCALED>(over_block<FORMAT>(max(top_of(x[0]), top_of(x[1]))), to_tensor, inverse);
     uint32_t w[2];
@@ -189,7 +187,7 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_quantize_rows_kernel(const 
     constexpr int TILES = ROW_COLS / BLOCK / 4;        // of scales
     constexpr int UNROLL = sizeof(T) == 4 ? 1 : 2;
     __shared__ __align__(16) uint8_t scales[TILES * SCALE_TILE];   // rows 0 to 63 in the first 8 of every 16 bytes
-    __shared__ float inverse[128];
+    __shared__ float2 inverse[128];
     if (FORMAT == QESGD_FP4_NV) fill_inverse(inverse);
     qesgd_wait_for_previous();
     const uint32_t o = threadIdx.x % 16u, line = threadIdx.x / 16u;
@@ -209,15 +207,24 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_quantize_rows_kernel(const 
         const uint64_t c = col0 + o * 16u;
         const T *from = static_cast<const T *>(a.x) + (row0 + line) * a.ldx;
         uint64_t n = ((row0 + line) * padded + c) / 8;
-#pragma unroll 1
-        for (uint32_t r0 = line; r0 < (rows + 1u) / 2u * 2u; r0 += THREADS / 16 * UNROLL) {   // both halves of a warp stay together
-            Octet<T> x[UNROLL][2];
+        const auto load = [&](Octet<T> (&x)[UNROLL][2], uint32_t r0) {
 #pragma unroll
             for (int i = 0; i < UNROLL; ++i)
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
                     x[i][k] = r0 + i * (THREADS / 16) < rows ? load_octet(from + i * (THREADS / 16) * a.ldx, c + 8 * k, a.cols, a.vec) : no_octet<T>();
             from += UNROLL * (THREADS / 16) * a.ldx;
+        };
+        Octet<T> next[UNROLL][2];
+        load(next, line);
+#pragma unroll 1
+        for (uint32_t r0 = line; r0 < (rows + 1u) / 2u * 2u; r0 += THREADS / 16 * UNROLL) {   // both halves of a warp stay together
+            Octet<T> x[UNROLL][2];
+#pragma unroll
+            for (int i = 0; i < UNROLL; ++i)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) x[i][k] = next[i][k];
+            load(next, r0 + THREADS / 16 * UNROLL);
 #pragma unroll
             for (int i = 0; i < UNROLL; ++i, n += (THREADS / 16) * (padded / 8)) {
                 const uint32_t r = r0 + i * (THREADS / 16);
@@ -264,7 +271,7 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_quantize_columns_kernel(con
     constexpr int BLOCKS = SIDE / BLOCK;
     extern __shared__ __align__(16) uint8_t held[];
     __shared__ __align__(16) uint8_t scales[2][SIDE * BLOCKS];
-    __shared__ float inverse[128];
+    __shared__ float2 inverse[128];
     if (FORMAT == QESGD_FP4_NV) fill_inverse(inverse);
     __syncthreads();
     qesgd_wait_for_previous();
@@ -506,22 +513,28 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_tensor_exponent_kernel(cons
         if (r >= rows) continue;
         const uint64_t first = tile % spans * TOP_COLS;
         const T *const row = x + r * ldx;
-#pragma unroll 4
-        for (uint32_t i = 0; i < TOP_COLS / 256; ++i) {
-            const uint64_t c = first + i * 256u + lane * 8u;
-            if (c >= cols) break;
-            const Octet<T> o = load_octet(row, c, cols, vec);
-            const uint32_t m = top_of(o);
-            if (m < 0x7F800000u) {
-                top = max(top, m);
-            } else {   // something is not finite: the rest counts
-                float v[8];
-                values(o, v);
-                bad = true;
+#pragma unroll 1
+        for (uint32_t i = 0; i < TOP_COLS / 256; i += 4) {
+            Octet<T> o[4];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint32_t e = __float_as_uint(v[j]) & 0x7FFFFFFFu;
-                    top = max(top, e >= 0x7F800000u ? 0u : e);
+            for (uint32_t k = 0; k < 4; ++k) {
+                const uint64_t c = first + (i + k) * 256u + lane * 8u;
+                o[k] = c < cols ? load_octet(row, c, cols, vec) : no_octet<T>();
+            }
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k) {
+                const uint32_t m = top_of(o[k]);
+                if (m < 0x7F800000u) {
+                    top = max(top, m);
+                } else {   // something is not finite: the rest counts
+                    float v[8];
+                    values(o[k], v);
+                    bad = true;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const uint32_t e = __float_as_uint(v[j]) & 0x7FFFFFFFu;
+                        top = max(top, e >= 0x7F800000u ? 0u : e);
+                    }
                 }
             }
         }
