@@ -181,7 +181,7 @@ __device__ __forceinline__ uint2 quantize_span(const Octet<T> (&x)[2], uint64_t 
 constexpr int ROW_COLS = 256, HALF_ROWS = TILE_ROWS / 2;
 
 template <typename T, int FORMAT, bool SCALED, bool STOCHASTIC>
-__global__ __launch_bounds__(THREADS) void qesgd_fp4_quantize_rows_kernel(const __grid_constant__ Fp4QuantizeArgs a)
+__global__ __launch_bounds__(THREADS, 4) void qesgd_fp4_quantize_rows_kernel(const __grid_constant__ Fp4QuantizeArgs a)
 {
     constexpr int BLOCK = Format<FORMAT>::BLOCK;
     constexpr int TILES = ROW_COLS / BLOCK / 4;        // of scales
