@@ -200,7 +200,7 @@ constexpr uint32_t BOX_COLS = 64;
 
 struct ProductArgs {
     uint32_t rows, cols, depth, batch;
-    uint32_t tiles_m, tiles_n, tiles;         // tiles of one matrix
+    uint32_t tiles_m, tiles;                  // tiles along the rows of one matrix, and of all of it
     __half *mirror;                           // GRAM: F, POLY: B, for the elements below the diagonal
     float *d, *db;                            // diagonals of A and of B
     uint32_t lo_in, lo_out;                   // UPDATE: whether X and X' have a second term
@@ -214,25 +214,35 @@ struct ProductArgs {
 // P and Q; what the end of a tile reads (F, or X and its second term) and writes
 struct ProductMaps {
     CUtensorMap p, q, in, in_lo, out, out_lo;
+    CUtensorMap q_narrow;   // Q of narrow tiles, for the launch to choose
 };
 
 struct Tile {
-    uint32_t batch, i, j;
+    uint32_t batch, row, col;   // col: where its columns begin
+    bool mirror;                // above the diagonal: stored below it too
 };
-template <int MODE>
+template <int MODE, uint32_t SIDE, uint32_t WIDTH>
 __device__ __forceinline__ Tile tile_of(uint32_t t, const ProductArgs &a)
 {
     Tile x;
     x.batch = t / a.tiles;
     t -= x.batch * a.tiles;
+    uint32_t i, j;
     if (MODE == UPDATE) {
-        x.j = t / a.tiles_m;
-        x.i = t % a.tiles_m;
-    } else {
-        x.i = 0;
-        while (t >= a.tiles_m - x.i) t -= a.tiles_m - x.i++;
-        x.j = x.i + t;
+        j = t / a.tiles_m;
+        i = t % a.tiles_m;
+        x.col = j * WIDTH;
+        x.mirror = false;
+    } else {   // squares of SIDE from the diagonal on, in strips of WIDTH
+        const uint32_t strip = t % (SIDE / WIDTH);
+        t /= SIDE / WIDTH;
+        i = 0;
+        while (t >= a.tiles_m - i) t -= a.tiles_m - i++;
+        j = i + t;
+        x.col = j * SIDE + strip * WIDTH;
+        x.mirror = i != j;
     }
+    x.row = i * SIDE;
     return x;
 }
 
@@ -386,24 +396,27 @@ __device__ __forceinline__ void store_rows(uint32_t batch, uint32_t row0, uint32
 // DEEP: an update whose contraction is long has five stages, and two slots in the second ring, in place of four and three.
 // Pairs: 4096 x 8192 2062 us in place of 2090 (five steps), 2048 x 2048 338 in place of 360; 12 x 512 x 2048 261 in place of 250,
 // 4 x 1024 x 4096 413 in place of 403: from contractions of 2048 on.
-template <int MODE, bool PAIR, bool DEEP>
+// NARROW: a single CTA's tile has 64 columns in place of 128.
+template <int MODE, bool PAIR, bool DEEP, bool NARROW>
 struct Shape {
-    static constexpr uint32_t SIDE = PAIR ? 256 : 128;       // a tile is square
+    static constexpr uint32_t SIDE = PAIR ? 256 : 128;       // rows of a tile
+    static constexpr uint32_t WIDTH = NARROW ? 64 : SIDE;    // and columns
+    static constexpr uint32_t Q_BYTES = NARROW ? OPERAND_BYTES / 2 : OPERAND_BYTES;
     static constexpr int STAGES = MODE == UPDATE && !DEEP ? 4 : 5;
     static constexpr int SLOTS = MODE == UPDATE && DEEP ? 2 : 3;   // of the second ring
     static constexpr uint32_t STAGE_BYTES = 2 * OPERAND_BYTES;   // of one CTA: 128 rows of either operand
     static constexpr uint32_t SLOT_BYTES = (MODE == UPDATE ? 2 : 1) * OPERAND_BYTES;
-    static constexpr uint32_t COLUMNS = 2 * SIDE;            // of tensor memory: two tiles
+    static constexpr uint32_t COLUMNS = 2 * WIDTH;           // of tensor memory: two tiles
     static constexpr uint32_t SMEM = STAGES * STAGE_BYTES + SLOTS * SLOT_BYTES + 1024 + 256 + SIDE * 4;
 };
 
 __device__ __forceinline__ void takers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(TAKERS * 32) : "memory"); }
 
-template <int MODE, bool PAIR, bool DEEP>
+template <int MODE, bool PAIR, bool DEEP, bool NARROW>
 __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(const __grid_constant__ ProductArgs a, const __grid_constant__ ProductMaps maps)
 {
-    using S = Shape<MODE, PAIR, DEEP>;
-    constexpr uint32_t BOXES = S::SIDE / BOX_COLS;                   // of a tile, for each CTA
+    using S = Shape<MODE, PAIR, DEEP, NARROW>;
+    constexpr uint32_t BOXES = S::WIDTH / BOX_COLS;                   // of a tile, for each CTA
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u, ring = base + S::STAGES * S::STAGE_BYTES;
     const uint32_t bars = ring + S::SLOTS * S::SLOT_BYTES;
@@ -454,17 +467,17 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
         uint32_t n = 0;
         const uint32_t full_lead = PAIR ? map_shared(full, 0) : full;
         for (uint32_t t = group; t < all && !*stop; t += groups) {
-            const Tile x = tile_of<MODE>(t, a);
-            const uint32_t row = x.i * S::SIDE + own_rows, col = x.j * S::SIDE + own_rows;
+            const Tile x = tile_of<MODE, S::SIDE, S::WIDTH>(t, a);
+            const uint32_t row = x.row + own_rows, col = x.col + own_rows;
             for (uint32_t k = 0; k < steps; ++k, ++n) {
                 const uint32_t s = n % S::STAGES, to = base + s * S::STAGE_BYTES;
                 if (n >= S::STAGES && !pipe_wait(empty + 8 * s, (n / S::STAGES - 1u) & 1u, stop)) break;
                 const uint32_t at = (step0 + k) * DEPTH;
-                if (!PAIR || rank == 0) mbar_expect_at(full + 8 * s, S::STAGE_BYTES * (PAIR ? 2u : 1u));
+                if (!PAIR || rank == 0) mbar_expect_at(full + 8 * s, (OPERAND_BYTES + S::Q_BYTES) * (PAIR ? 2u : 1u));
                 tma_load_3d<PAIR>(to, &maps.p, at, row, x.batch, full_lead + 8 * s);
                 if (MODE == UPDATE) {
                     tma_load_3d<PAIR>(to + OPERAND_BYTES, &maps.q, col, at, x.batch, full_lead + 8 * s);
-                    tma_load_3d<PAIR>(to + OPERAND_BYTES + OPERAND_BYTES / 2, &maps.q, col + 64u, at, x.batch, full_lead + 8 * s);
+                    if (!NARROW) tma_load_3d<PAIR>(to + OPERAND_BYTES + OPERAND_BYTES / 2, &maps.q, col + 64u, at, x.batch, full_lead + 8 * s);
                 } else {
                     tma_load_3d<PAIR>(to + OPERAND_BYTES, &maps.q, at, col, x.batch, full_lead + 8 * s);
                 }
@@ -472,11 +485,11 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
         }
         if (*stop) drain();
     } else if (warp == 1 && (!PAIR || rank == 0) && elect_one()) {
-        // fp16 operands, fp32 sums, SIDE x SIDE; Q of UPDATE has its contraction across the rows
-        constexpr uint32_t INSTRUCTION = 1u << 4 | (MODE == UPDATE ? 1u << 16 : 0u) | (S::SIDE / 8) << 17 | (S::SIDE / 16) << 24;
+        // fp16 operands, fp32 sums, SIDE x WIDTH; Q of UPDATE has its contraction across the rows
+        constexpr uint32_t INSTRUCTION = 1u << 4 | (MODE == UPDATE ? 1u << 16 : 0u) | (S::WIDTH / 8) << 17 | (S::SIDE / 16) << 24;
         uint32_t n = 0, done_tiles = 0;
         for (uint32_t t = group; t < all && !*stop; t += groups, ++done_tiles) {
-            const uint32_t half = done_tiles & 1u, sums = tmem + half * S::SIDE;
+            const uint32_t half = done_tiles & 1u, sums = tmem + half * S::WIDTH;
             if (done_tiles >= 2 && !pipe_wait(free_ + 8 * half, (done_tiles / 2 - 1u) & 1u, stop)) break;
             fence_after_sync();
             bool ok = true;
@@ -501,7 +514,7 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
     } else if (warp == 2 && elect_one()) {
         uint32_t n = 0;
         for (uint32_t t = group; t < all && !*stop; t += groups) {
-            const Tile x = tile_of<MODE>(t, a);
+            const Tile x = tile_of<MODE, S::SIDE, S::WIDTH>(t, a);
             for (uint32_t b = box_first; b < box_end; ++b, ++n) {
                 const uint32_t s = n % S::SLOTS, to = ring + s * S::SLOT_BYTES;
                 if (n >= S::SLOTS && !pipe_wait(stored + 8 * s, (n / S::SLOTS - 1u) & 1u, stop)) break;
@@ -509,7 +522,7 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
                     mbar_arrive_at(filled + 8 * s);
                     continue;
                 }
-                const uint32_t col = x.j * S::SIDE + b * BOX_COLS, row = x.i * S::SIDE + own_rows;
+                const uint32_t col = x.col + b * BOX_COLS, row = x.row + own_rows;
                 const bool lo = MODE == UPDATE && a.lo_in;
                 mbar_expect_at(filled + 8 * s, lo ? 2 * OPERAND_BYTES : OPERAND_BYTES);
                 tma_load_3d<false>(to, &maps.in, col, row, x.batch, filled + 8 * s);
@@ -528,11 +541,11 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
             uint32_t n = 0;
             const bool store = MODE != UPDATE || !a.out || a.out_tiled;
             for (uint32_t t = group; t < all && !*stop; t += groups) {
-                const Tile x = tile_of<MODE>(t, a);
+                const Tile x = tile_of<MODE, S::SIDE, S::WIDTH>(t, a);
                 for (uint32_t b = box_first; b < box_end; ++b, ++n) {
                     const uint32_t s = n % S::SLOTS, from = ring + s * S::SLOT_BYTES;
                     if (!pipe_wait(worked + 8 * s, (n / S::SLOTS) & 1u, stop)) break;
-                    const uint32_t col = x.j * S::SIDE + b * BOX_COLS, row = x.i * S::SIDE + own_rows;
+                    const uint32_t col = x.col + b * BOX_COLS, row = x.row + own_rows;
                     if (store && col < a.cols && row < a.rows) {
                         tma_store_3d(&maps.out, col, row, x.batch, from);
                         if (MODE == UPDATE && a.lo_out) tma_store_3d(&maps.out_lo, col, row, x.batch, from + OPERAND_BYTES);
@@ -552,14 +565,14 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
         // after a wait that ran out the loops are gone through without work: the barriers of these warps stay in step
         bool ok = true;
         for (uint32_t t = group; t < all; t += groups, ++done_tiles) {
-            const Tile x = tile_of<MODE>(t, a);
-            const uint32_t half = done_tiles & 1u, row0 = x.i * S::SIDE + own_rows, row = row0 + r;
+            const Tile x = tile_of<MODE, S::SIDE, S::WIDTH>(t, a);
+            const uint32_t half = done_tiles & 1u, row0 = x.row + own_rows, row = row0 + r;
             float linear = 0.0f;
             if (MODE != GRAM && row < a.rows) linear = __ldcg((MODE == POLY ? a.d : a.db) + x.batch * a.d_stride + row) + (MODE == UPDATE ? a.ca : 0.0f);
             if (MODE == POLY) {
                 takers_sync();   // the last tile's have been read
-                if (thread < S::SIDE) {
-                    const uint32_t c = x.j * S::SIDE + thread;
+                if (thread < S::WIDTH) {
+                    const uint32_t c = x.col + thread;
                     const float d = c < a.cols ? __ldcg(a.d + x.batch * a.d_stride + c) : 0.0f;
                     asm volatile("st.shared.f32 [%0], %1;" ::"r"(across + thread * 4u), "f"(d));
                 }
@@ -593,7 +606,7 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
                 const uint32_t s = n % S::SLOTS, box = ring + s * S::SLOT_BYTES, first = b * BOX_COLS + part * TAKEN;
                 float v[TAKEN];
                 __syncwarp();
-                tmem_load16(tmem + (quarter * 32u << 16) + half * S::SIDE + first, v);
+                tmem_load16(tmem + (quarter * 32u << 16) + half * S::WIDTH + first, v);
                 ok = __all_sync(FULL, ok && pipe_wait(filled + 8 * s, (n / S::SLOTS) & 1u, stop));
                 tmem_wait_load();
                 if (parts > 1) {
@@ -622,10 +635,10 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
                         else mbar_arrive_at(free_ + 8 * half);
                     }
                 }
-                if (ok) finish<MODE>(v, x.batch, row, x.j * S::SIDE + first, box, r, part * OCTETS, linear, across + first * 4u, x.i != x.j, a);
+                if (ok) finish<MODE>(v, x.batch, row, x.col + first, box, r, part * OCTETS, linear, across + first * 4u, x.mirror, a);
                 if (MODE == UPDATE && a.out && !a.turned && !a.out_tiled) {
                     takers_sync();
-                    if (ok) store_rows(x.batch, row0, x.j * S::SIDE + b * BOX_COLS, box, thread, a);
+                    if (ok) store_rows(x.batch, row0, x.col + b * BOX_COLS, box, thread, a);
                 }
                 fence_async_shared();
                 __syncwarp();
@@ -1082,14 +1095,13 @@ bool half_map(CUtensorMap *map, const void *p, uint64_t rows, uint64_t cols, uin
                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int MODE, bool PAIR, bool DEEP>
+template <int MODE, bool PAIR, bool DEEP, bool NARROW>
 cudaError_t launch_product(ProductArgs a, const ProductMaps &maps, uint32_t split, int sm_count, cudaStream_t stream)
 {
-    using S = Shape<MODE, PAIR, DEEP>;
-    const auto kernel = qesgd_ortho_product_kernel<MODE, PAIR, DEEP>;
+    using S = Shape<MODE, PAIR, DEEP, NARROW>;
+    const auto kernel = qesgd_ortho_product_kernel<MODE, PAIR, DEEP, NARROW>;
     a.tiles_m = (a.rows + S::SIDE - 1) / S::SIDE;
-    a.tiles_n = (a.cols + S::SIDE - 1) / S::SIDE;
-    a.tiles = MODE == UPDATE ? a.tiles_m * a.tiles_n : a.tiles_m * (a.tiles_m + 1) / 2;
+    a.tiles = MODE == UPDATE ? a.tiles_m * ((a.cols + S::WIDTH - 1) / S::WIDTH) : a.tiles_m * (a.tiles_m + 1) / 2 * (S::SIDE / S::WIDTH);
     a.split = split;
     static std::atomic<uint64_t> told{0};
     const cudaError_t e = qesgd_prepare(told, (const void *)kernel, S::SMEM, false);
@@ -1099,7 +1111,7 @@ cudaError_t launch_product(ProductArgs a, const ProductMaps &maps, uint32_t spli
 }
 // Pairs or single CTAs, and how many CTAs share a contraction: by modelled time.
 template <int MODE>
-cudaError_t launch_product(const ProductArgs &a, const ProductMaps &maps, int sm_count, cudaStream_t stream)
+cudaError_t launch_product(const ProductArgs &a, ProductMaps maps, int sm_count, cudaStream_t stream)
 {
     const auto tiles = [&](uint64_t side) {
         const uint64_t m = (a.rows + side - 1) / side, n = (a.cols + side - 1) / side;
@@ -1116,8 +1128,8 @@ cudaError_t launch_product(const ProductArgs &a, const ProductMaps &maps, int sm
         if (s > 1 && (singles * s > sms || steps < 4 * s)) break;
         static QesgdClusters known;
         static std::atomic<uint64_t> told{0};
-        const void *const kernel = (const void *)qesgd_ortho_product_kernel<MODE, false, false>;
-        const uint32_t smem = Shape<MODE, false, false>::SMEM;
+        const void *const kernel = (const void *)qesgd_ortho_product_kernel<MODE, false, false, false>;
+        const uint32_t smem = Shape<MODE, false, false, false>::SMEM;
         if (s > 1 && qesgd_prepare(told, kernel, (int)smem, false) != cudaSuccess) break;
         const double active = s > 1 ? (double)qesgd_active_clusters(known, kernel, WARPS * 32, smem, s) : sms;
         const double t = waves(singles, active) * (double)(uint64_t)((steps + s - 1) / s) * stage(singles * s, 450, 650) + 2500 + (s > 1 ? 2000 : 0);
@@ -1126,9 +1138,16 @@ cudaError_t launch_product(const ProductArgs &a, const ProductMaps &maps, int sm
             split = s;
         }
     }
-    if (split != 0) return launch_product<MODE, false, false>(a, maps, split, sm_count, stream);
-    if (MODE == UPDATE && a.depth >= 2048) return launch_product<MODE, true, MODE == UPDATE>(a, maps, 1, sm_count, stream);
-    return launch_product<MODE, true, false>(a, maps, 1, sm_count, stream);
+    // narrow tiles: 350 to 500 clocks a stage, and 1200 less at the end
+    const double strips = MODE == UPDATE ? (double)(((uint64_t)a.rows + 127) / 128 * ((a.cols + 63) / 64) * a.batch) : 2 * singles;
+    const bool narrow = waves(strips, sms) * steps * stage(strips, 350, 500) + 1300 < best;
+    if (narrow) {
+        if (MODE != UPDATE) maps.q = maps.q_narrow;
+        return launch_product<MODE, false, false, true>(a, maps, 1, sm_count, stream);
+    }
+    if (split != 0) return launch_product<MODE, false, false, false>(a, maps, split, sm_count, stream);
+    if (MODE == UPDATE && a.depth >= 2048) return launch_product<MODE, true, MODE == UPDATE, false>(a, maps, 1, sm_count, stream);
+    return launch_product<MODE, true, false, false>(a, maps, 1, sm_count, stream);
 }
 
 }  // namespace
@@ -1141,10 +1160,12 @@ int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t st
     }
     const OrthoLayout l = qesgd_ortho_layout(a.rows, a.cols, a.batch);
     const auto at = [&](uint64_t off) { return reinterpret_cast<__half *>(a.workspace + off); };
-    CUtensorMap hi[2], lo[2], across[2], f, b;   // X by rows and its second term, X across its rows, F, B
-    bool ok = half_map(&f, at(l.off_a), l.m, l.m, l.ld_a, a.batch, l.a_stride, 128) && half_map(&b, at(l.off_b), l.m, l.m, l.ld_a, a.batch, l.a_stride, 128);
+    CUtensorMap hi[2], lo[2], across[2], f, b, hi_64[2], f_64;   // X by rows and its second term, X across its rows, F, B; 64 rows of them
+    bool ok = half_map(&f, at(l.off_a), l.m, l.m, l.ld_a, a.batch, l.a_stride, 128) && half_map(&b, at(l.off_b), l.m, l.m, l.ld_a, a.batch, l.a_stride, 128) &&
+              half_map(&f_64, at(l.off_a), l.m, l.m, l.ld_a, a.batch, l.a_stride, 64);
     for (int i = 0; i < 2; ++i)
         ok = ok && half_map(&hi[i], at(l.off_hi[i]), l.m, l.n, l.ld_x, a.batch, l.x_stride, 128) &&
+             half_map(&hi_64[i], at(l.off_hi[i]), l.m, l.n, l.ld_x, a.batch, l.x_stride, 64) &&
              half_map(&lo[i], at(l.off_lo[i]), l.m, l.n, l.ld_x, a.batch, l.x_stride, 128) &&
              half_map(&across[i], at(l.off_hi[i]), l.m, l.n, l.ld_x, a.batch, l.x_stride, DEPTH);
     if (!ok) return (int)cudaErrorInvalidValue;
@@ -1167,12 +1188,12 @@ int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t st
         p.rows = p.cols = (uint32_t)l.m;
         p.depth = (uint32_t)l.n;
         p.mirror = at(l.off_a);
-        e = launch_product<GRAM>(p, {hi[now], hi[now], f, f, f, f}, sm_count, stream);
+        e = launch_product<GRAM>(p, {hi[now], hi[now], f, f, f, f, hi_64[now]}, sm_count, stream);
         if (e != cudaSuccess) return (int)e;
         *launched += 1;
         p.depth = (uint32_t)l.m;
         p.mirror = at(l.off_b);
-        e = launch_product<POLY>(p, {f, f, f, f, b, b}, sm_count, stream);
+        e = launch_product<POLY>(p, {f, f, f, f, b, b, f_64}, sm_count, stream);
         if (e != cudaSuccess) return (int)e;
         *launched += 1;
         p.cols = (uint32_t)l.n;
@@ -1188,7 +1209,7 @@ int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t st
             p.out_tiled = !p.turned && qesgd_aligned(a.out, 16) && a.ldo % 8 == 0 && stride % 8 == 0 &&
                           half_map(&hi[next], a.out, l.m, l.n, a.ldo, a.batch, stride, 128, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16);
         }
-        e = launch_product<UPDATE>(p, {b, across[now], hi[now], lo[now], hi[next], lo[next]}, sm_count, stream);
+        e = launch_product<UPDATE>(p, {b, across[now], hi[now], lo[now], hi[next], lo[next], across[now]}, sm_count, stream);
         if (e != cudaSuccess) return (int)e;
         *launched += 1;
     }
