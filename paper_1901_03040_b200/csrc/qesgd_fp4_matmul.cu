@@ -43,49 +43,91 @@ struct ProductArgs {
     const int32_t *a_exponent, *b_exponent;
     void *c;
     uint64_t ldc;
-    uint32_t dtype;
+    uint32_t pairs;                           // rows of 16-bit elements that lie on 4 bytes
     uint32_t *status;
 };
 
 // Column n of COUNT rows of C from row m on: what is there, and what comes there.
 template <typename T, int COUNT>
-__device__ __forceinline__ void load_column(float (&old)[COUNT], const T *c, uint32_t m, const ProductArgs &a)
-{
-#pragma unroll
-    for (int k = 0; k < COUNT; ++k, c += a.ldc) old[k] = m + k < a.M ? to_float(*c) : 0.0f;
-}
-template <int COUNT>
 __device__ __forceinline__ void load_column(float (&old)[COUNT], uint32_t m, uint32_t n, const ProductArgs &a)
 {
     if (n >= a.N || m >= a.M) return;
-    const uint64_t at = m * a.ldc + n;
-    if (a.dtype == QESGD_F32) load_column(old, static_cast<const float *>(a.c) + at, m, a);
-    else if (a.dtype == QESGD_BF16) load_column(old, static_cast<const __nv_bfloat16 *>(a.c) + at, m, a);
-    else load_column(old, static_cast<const __half *>(a.c) + at, m, a);
-}
-template <typename T, int COUNT>
-__device__ __forceinline__ void store_column(const float (&v)[COUNT], T *c, uint32_t m, const ProductArgs &a)
-{
+    const T *c = static_cast<const T *>(a.c) + (m * a.ldc + n);
+    if (m + COUNT <= a.M) {
 #pragma unroll
-    for (int k = 0; k < COUNT; ++k, c += a.ldc)
-        if (m + k < a.M) *c = from_float<T>(v[k]);
+        for (int k = 0; k < COUNT; ++k, c += a.ldc) old[k] = to_float(*c);
+    } else {
+#pragma unroll
+        for (int k = 0; k < COUNT; ++k, c += a.ldc) old[k] = m + k < a.M ? to_float(*c) : 0.0f;
+    }
 }
-template <int COUNT>
+// Two floats as two 16-bit elements, the first below.
+__device__ __forceinline__ uint32_t packed(float a, float b, __nv_bfloat16)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ uint32_t packed(float a, float b, __half)
+{
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+// For 32 lanes on 32 neighbouring columns, all inside, COUNT rows, all inside, rows on 4 bytes: neighbouring lanes
+// exchange an element each, and store two of one row at a time, the even lanes in even rows, the odd ones in odd rows.
+template <typename T, int COUNT>
+__device__ __forceinline__ void store_column_pairs(const float (&v)[COUNT], T *c, uint32_t lane, const ProductArgs &a)
+{
+    const bool odd = lane & 1u;
+    c += odd ? (int64_t)a.ldc - 1 : 0;
+#pragma unroll
+    for (int k = 0; k < COUNT; k += 2, c += 2 * a.ldc) {
+        const float other = __shfl_xor_sync(0xFFFFFFFFu, odd ? v[k] : v[k + 1], 1);
+        *reinterpret_cast<uint32_t *>(c) = odd ? packed(other, v[k + 1], T()) : packed(v[k], other, T());
+    }
+}
+// All lanes of a warp come here; n is the lane's own column.
+template <typename T, int COUNT>
 __device__ __forceinline__ void store_column(const float (&v)[COUNT], uint32_t m, uint32_t n, const ProductArgs &a)
 {
+    T *c = static_cast<T *>(a.c) + (m * a.ldc + n);
+    if constexpr (sizeof(T) == 2 && COUNT % 2 == 0) {
+        const uint32_t lane = threadIdx.x % 32u;
+        if (a.pairs && n - lane + 32u <= a.N && m + COUNT <= a.M) {
+            store_column_pairs(v, c, lane, a);
+            return;
+        }
+    }
     if (n >= a.N || m >= a.M) return;
-    const uint64_t at = m * a.ldc + n;
-    if (a.dtype == QESGD_F32) store_column(v, static_cast<float *>(a.c) + at, m, a);
-    else if (a.dtype == QESGD_BF16) store_column(v, static_cast<__nv_bfloat16 *>(a.c) + at, m, a);
-    else store_column(v, static_cast<__half *>(a.c) + at, m, a);
+    if (m + COUNT <= a.M) {
+#pragma unroll
+        for (int k = 0; k < COUNT; ++k, c += a.ldc) *c = from_float<T>(v[k]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < COUNT; ++k, c += a.ldc)
+            if (m + k < a.M) *c = from_float<T>(v[k]);
+    }
 }
-__device__ __forceinline__ float power_of(const int32_t *exponent)
+// 2^(ta + tb), in two factors where it is no 32-bit number.
+struct Power {
+    float first, second;
+};
+__device__ __forceinline__ Power power_of(const ProductArgs &a)
 {
-    const int t = exponent ? min(max(__ldcg(exponent), -126), 126) : 0;
-    return __uint_as_float((uint32_t)(t + 127) << 23);
+    const int ta = a.a_exponent ? min(max(__ldcg(a.a_exponent), -126), 126) : 0, tb = a.b_exponent ? min(max(__ldcg(a.b_exponent), -126), 126) : 0;
+    const int t = ta + tb, first = t < -126 ? -126 : t > 126 ? 126 : t;
+    return {__uint_as_float((uint32_t)(first + 127) << 23), __uint_as_float((uint32_t)(t - first + 127) << 23)};
+}
+template <int COUNT>
+__device__ __forceinline__ void times(float (&v)[COUNT], const Power &p)
+{
+#pragma unroll
+    for (int k = 0; k < COUNT; ++k) v[k] *= p.first;
+    if (p.second != 1.0f)
+#pragma unroll
+        for (int k = 0; k < COUNT; ++k) v[k] *= p.second;
 }
 
-template <bool PAIR, bool MX, bool ACCUMULATE>
+template <typename T, bool PAIR, bool MX, bool ACCUMULATE>
 __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const __grid_constant__ ProductArgs a, const __grid_constant__ CUtensorMap map_p,
                                                                          const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_sp,
                                                                          const __grid_constant__ CUtensorMap map_sq)
@@ -203,7 +245,7 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const _
     } else if (warp >= 4) {
         const uint32_t quarter = warp % 4u, part_of = (warp - 4u) / 4u;
         const uint32_t free_lead = PAIR ? map_shared(free_, 0) : free_;
-        const float power_a = power_of(a.a_exponent), power_b = power_of(a.b_exponent);
+        const Power power = power_of(a);
         uint32_t done_tiles = 0;
         for (uint32_t t = group; t < a.tiles; t += groups, ++done_tiles) {
             const uint32_t which = done_tiles % S::TILES, turn = done_tiles / S::TILES;
@@ -211,8 +253,13 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const _
             const uint32_t from = tmem + (quarter * 32u << 16) + which * S::MOST_Q;
             const uint32_t rows = min(q_rows, a.M - m0);     // of A in this tile
             const bool ends = ACCUMULATE && parts == 1;
-            float old[32];
-            if (ends) load_column(old, m0 + part_of * 32u, n, a);   // before the sums are there
+            // 16 rows of A after another: their elements of C are on their way before the sums are there, the next ones' while
+            // these are stored (32 at a time did not fit the registers: 1531 x 999 x 2347 13.4 us, and 10.2 with half of them
+            // in local memory)
+            constexpr uint32_t PARTS = S::MOST_Q / 128 * 2;
+            const auto part_at = [&](uint32_t i) { return (4 * (i / 2) + part_of) * 32u + i % 2 * 16u; };
+            float old[2][16];
+            if (ends) load_column<T>(old[0], m0 + part_at(0), n, a);
             if (!__all_sync(0xFFFFFFFFu, pipe_wait(done + 8 * which, turn & 1u, stop))) break;
             fence_after_sync();
             const auto taken = [&]() {   // the tile is in registers
@@ -225,19 +272,18 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const _
                 }
             };
             if (ends) {
-                // 32 rows after another, the next ones' elements of C on their way meanwhile
 #pragma unroll
-                for (uint32_t i = 0; i < S::MOST_Q / 128; ++i) {
-                    const uint32_t at = (4 * i + part_of) * 32u;
-                    float v[32];
+                for (uint32_t i = 0; i < PARTS; ++i) {
+                    float v[16];
                     __syncwarp();
-                    tmem_load32(from + at, v);
-                    if (i + 1 == S::MOST_Q / 128) taken();
+                    tmem_load16(from + part_at(i), v);
+                    if (i + 1 < PARTS && part_at(i + 1) < rows) load_column<T>(old[(i + 1) % 2], m0 + part_at(i + 1), n, a);
+                    if (i + 1 == PARTS) taken();
                     else tmem_wait_load();
+                    times(v, power);
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) v[k] = old[k] + v[k] * power_a * power_b;
-                    if (i + 1 < S::MOST_Q / 128 && at + 128u < rows) load_column(old, m0 + at + 128u, n, a);
-                    if (at < rows) store_column(v, m0 + at, n, a);
+                    for (int k = 0; k < 16; ++k) v[k] += old[i % 2][k];
+                    if (part_at(i) < rows) store_column<T>(v, m0 + part_at(i), n, a);
                 }
             } else {
                 float v[S::MOST_Q / 128][32];
@@ -254,9 +300,8 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const _
                     const uint32_t at = (4 * i + part_of) * 32u;
                     if (at >= rows) break;
                     if (PAIR || parts == 1) {
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) v[i][k] = v[i][k] * power_a * power_b;
-                        store_column(v[i], m0 + at, n, a);
+                        times(v[i], power);
+                        store_column<T>(v[i], m0 + at, n, a);
                     } else {
                         // row m of the tile to CTA m % parts, as part `rank` of its row m / parts
                         uint32_t owner = at % parts, to = received + ((rank * every + at / parts) * LANES + quarter * 32u + lane) * 4u;
@@ -280,18 +325,32 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const _
         cluster_sync_all();
         if (!*stop) {
             const uint32_t n = group % a.tiles_n * 128u + threadIdx.x % LANES, m0 = group / a.tiles_n * q_rows;
-            const float power_a = power_of(a.a_exponent), power_b = power_of(a.b_exponent);
-            for (uint32_t i = threadIdx.x / LANES; i * parts + rank < min(q_rows, a.M - m0); i += WARPS * 32 / LANES) {
-                const uint32_t m = m0 + i * parts + rank;
-                float sum[1] = {0.0f}, old[1] = {0.0f};
-                if (ACCUMULATE) load_column(old, m, n, a);
-                for (uint32_t r = 0; r < parts; ++r) {   // in the order of the contraction
-                    float v;
-                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(received + ((r * every + i) * LANES + threadIdx.x % LANES) * 4u));
-                    sum[0] += v;
+            const Power power = power_of(a);
+            constexpr uint32_t GROUPS = WARPS * 32 / LANES, ROWS = 4;   // a group of threads takes 4 rows at a time
+            const uint32_t rows = min(q_rows, a.M - m0);
+            for (uint32_t i0 = threadIdx.x / LANES; i0 * parts + rank < rows; i0 += ROWS * GROUPS) {
+                float sum[ROWS][1], old[ROWS][1];
+#pragma unroll
+                for (uint32_t k = 0; k < ROWS; ++k) {
+                    const uint32_t row = (i0 + k * GROUPS) * parts + rank;
+                    sum[k][0] = old[k][0] = 0.0f;
+                    if (ACCUMULATE && row < rows) load_column<T>(old[k], m0 + row, n, a);
                 }
-                sum[0] = old[0] + sum[0] * power_a * power_b;
-                store_column(sum, m, n, a);
+                for (uint32_t r = 0; r < parts; ++r)   // in the order of the contraction
+#pragma unroll
+                    for (uint32_t k = 0; k < ROWS; ++k) {
+                        const uint32_t i = min(i0 + k * GROUPS, every - 1u);
+                        float v;
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(received + ((r * every + i) * LANES + threadIdx.x % LANES) * 4u));
+                        sum[k][0] += v;
+                    }
+#pragma unroll
+                for (uint32_t k = 0; k < ROWS; ++k) {
+                    const uint32_t row = (i0 + k * GROUPS) * parts + rank;
+                    times(sum[k], power);
+                    sum[k][0] += old[k][0];
+                    if (row < rows) store_column<T>(sum[k], m0 + row, n, a);
+                }
             }
         }
     }
@@ -337,11 +396,11 @@ bool scales_map(CUtensorMap *map, const uint8_t *p, uint64_t rows, uint64_t K, b
                                 CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool PAIR, bool MX, bool ACCUMULATE>
-int launch(const Fp4MatmulArgs &f, uint32_t dtype, uint32_t q, uint32_t split, int sm_count, cudaStream_t stream)
+template <typename T, bool PAIR, bool MX, bool ACCUMULATE>
+int launch(const Fp4MatmulArgs &f, uint32_t q, uint32_t split, int sm_count, cudaStream_t stream)
 {
     using S = Shape<PAIR>;
-    const auto kernel = qesgd_fp4_matmul_kernel<PAIR, MX, ACCUMULATE>;
+    const auto kernel = qesgd_fp4_matmul_kernel<T, PAIR, MX, ACCUMULATE>;
     const uint64_t row_bytes = qesgd_div_up(f.K, 32) * 16;
     CUtensorMap p, qm, sp, sq;
     if (!qesgd_encode_tiled() || !codes_map(&p, f.b_codes, f.N, row_bytes, 128) || !codes_map(&qm, f.a_codes, f.M, row_bytes, PAIR ? 128u : q) ||
@@ -361,7 +420,7 @@ int launch(const Fp4MatmulArgs &f, uint32_t dtype, uint32_t q, uint32_t split, i
     a.b_exponent = f.b_exponent;
     a.c = f.c;
     a.ldc = f.ldc;
-    a.dtype = dtype;
+    a.pairs = sizeof(T) == 2 && qesgd_aligned(f.c, 4) && f.ldc % 2 == 0;
     a.status = f.status;
     static std::atomic<uint64_t> told{0};
     const cudaError_t e = qesgd_prepare(told, (const void *)kernel, S::SMEM, !PAIR);
@@ -371,8 +430,8 @@ int launch(const Fp4MatmulArgs &f, uint32_t dtype, uint32_t q, uint32_t split, i
     return (int)qesgd_launch_cluster(kernel, dim3(groups * share), dim3(WARPS * 32), S::SMEM, share, stream, a, p, qm, sp, sq);
 }
 
-template <bool MX, bool ACCUMULATE>
-int launch(const Fp4MatmulArgs &a, uint32_t dtype, int sm_count, cudaStream_t stream)
+template <typename T, bool MX, bool ACCUMULATE>
+int launch(const Fp4MatmulArgs &a, int sm_count, cudaStream_t stream)
 {
     static QesgdClusters known;
     // By modelled clocks: a stage of a pair takes about 700 to arrive and be multiplied, one of a single CTA 450 where others
@@ -384,7 +443,7 @@ int launch(const Fp4MatmulArgs &a, uint32_t dtype, int sm_count, cudaStream_t st
     const uint64_t tiles = qesgd_div_up(a.M, q) * qesgd_div_up(a.N, 128), steps = qesgd_div_up(a.K, DEPTH);
     const auto stage = [&](uint64_t ctas) { return 450 + 150 * (ctas < sms ? ctas : sms) / sms; };
     const uint64_t by_pairs = qesgd_div_up(pairs, sms / 2) * steps * 700 + 1500;
-    const void *const kernel = (const void *)qesgd_fp4_matmul_kernel<false, MX, ACCUMULATE>;
+    const void *const kernel = (const void *)qesgd_fp4_matmul_kernel<T, false, MX, ACCUMULATE>;
     uint32_t split = 1;
     uint64_t best = qesgd_div_up(tiles, sms) * steps * stage(tiles);
     static std::atomic<uint64_t> told{0};
@@ -398,8 +457,15 @@ int launch(const Fp4MatmulArgs &a, uint32_t dtype, int sm_count, cudaStream_t st
             split = s;
         }
     }
-    if (by_pairs < best) return launch<true, MX, ACCUMULATE>(a, dtype, 256, 1, sm_count, stream);
-    return launch<false, MX, ACCUMULATE>(a, dtype, q, split, sm_count, stream);
+    if (by_pairs < best) return launch<T, true, MX, ACCUMULATE>(a, 256, 1, sm_count, stream);
+    return launch<T, false, MX, ACCUMULATE>(a, q, split, sm_count, stream);
+}
+
+template <typename T>
+int launch(const Fp4MatmulArgs &a, uint32_t format, int sm_count, cudaStream_t stream)
+{
+    if (format == QESGD_FP4_MX) return a.accumulate ? launch<T, true, true>(a, sm_count, stream) : launch<T, true, false>(a, sm_count, stream);
+    return a.accumulate ? launch<T, false, true>(a, sm_count, stream) : launch<T, false, false>(a, sm_count, stream);
 }
 
 }  // namespace
@@ -408,6 +474,9 @@ int qesgd_launch_fp4_matmul(const Fp4MatmulArgs &a, uint32_t dtype, uint32_t for
 {
     *launched = 1;
     if (a.K == 0) return (int)(dtype == QESGD_F32 ? launch_zeros<uint32_t>(a, stream) : launch_zeros<uint16_t>(a, stream));
-    if (format == QESGD_FP4_MX) return a.accumulate ? launch<true, true>(a, dtype, sm_count, stream) : launch<true, false>(a, dtype, sm_count, stream);
-    return a.accumulate ? launch<false, true>(a, dtype, sm_count, stream) : launch<false, false>(a, dtype, sm_count, stream);
+    switch (dtype) {
+        case QESGD_F32: return launch<float>(a, format, sm_count, stream);
+        case QESGD_BF16: return launch<__nv_bfloat16>(a, format, sm_count, stream);
+        default: return launch<__half>(a, format, sm_count, stream);
+    }
 }
