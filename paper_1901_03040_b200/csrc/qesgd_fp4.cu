@@ -3,9 +3,13 @@
 //
 // This file must be compiled with -fmad=false: the choice of a level is a sequence of single IEEE operations.
 //
-// All of it is bound by memory.  The unit of work is an octet, 8 consecutive elements of a row in one lane: 16 or 32
-// bytes of input, one Philox4x32-10 block of 8 draws, one 32-bit word of codes.  A block of 16 is two lanes, one of 32
-// four, so its largest magnitude takes one or two shuffles.
+// A lane has 16 consecutive elements of a row, two octets: 32 or 64 bytes of input, two Philox4x32-10 blocks of 8 draws
+// each, two 32-bit words of codes.  A block of 16 is in one lane, one of 32 in two neighbours, so its largest magnitude
+// takes no shuffle or one.
+//
+// Memory is the floor; the instructions are what bounds it: 26 an element with draws (5 of them Philox's), 20 without and
+// for both axes.  4096 x 4096 fp32 with draws and its way back to bf16 27 us together, where the bytes take 18; 8192 x 8192
+// bf16 along both axes and both ways back 116 us, where they take 85.
 #include "qesgd_matrix.cuh"
 
 namespace {
@@ -104,6 +108,23 @@ __device__ __forceinline__ float over_scale(float x, const Scale &s)
     return __fmaf_rn(y, s.inv.x, __fmul_rn(y, s.inv.y));
 }
 
+// The same for two elements at once (sm_100 multiplies and adds pairs of floats in one instruction: 8192 x 8192 along both
+// axes and back 118 -> 116 us).
+template <int FORMAT, bool SCALED>
+__device__ __forceinline__ void over_scale(float &a, float &b, const Scale &s)
+{
+    if (SCALED) {
+        a = over_scale<FORMAT, SCALED>(a, s);
+        b = over_scale<FORMAT, SCALED>(b, s);
+    } else if (FORMAT == QESGD_FP4_MX) {
+        asm("{\n.reg .b64 x, m;\nmov.b64 x, {%0, %1};\nmov.b64 m, {%2, %2};\nmul.rn.f32x2 x, x, m;\nmov.b64 {%0, %1}, x;\n}" : "+f"(a), "+f"(b) : "f"(s.mul));
+    } else {
+        asm("{\n.reg .b64 x, h, l;\nmov.b64 x, {%0, %1};\nmov.b64 h, {%2, %2};\nmov.b64 l, {%3, %3};\nmul.rn.f32x2 l, x, l;\nfma.rn.f32x2 x, x, h, l;\nmov.b64 {%0, %1}, x;\n}"
+            : "+f"(a), "+f"(b)
+            : "f"(s.inv.x), "f"(s.inv.y));
+    }
+}
+
 // Eight elements of one block -> their codes.
 template <int FORMAT, bool SCALED, bool STOCHASTIC>
 __device__ __forceinline__ uint32_t quantize_octet(const float (&v)[8], const Scale &s, const uint32_t (&draw)[4])
@@ -112,7 +133,9 @@ __device__ __forceinline__ uint32_t quantize_octet(const float (&v)[8], const Sc
     if (!STOCHASTIC) {
         float q[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] = over_scale<FORMAT, SCALED>(v[j], s);
+        for (int j = 0; j < 8; ++j) q[j] = v[j];
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) over_scale<FORMAT, SCALED>(q[j], q[j + 1], s);
         asm("{\n"
             ".reg .b8 b0, b1, b2, b3;\n"
             "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n"
