@@ -94,12 +94,6 @@ __device__ __forceinline__ uint32_t half_pair(float a, float b)
     return r;
 }
 __device__ __forceinline__ float2 float_pair(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2 *>(&h)); }
-// What rounding two floats to the fp16 pair h has left behind.
-__device__ __forceinline__ uint32_t rest_pair(float a, float b, uint32_t h)
-{
-    const float2 kept = float_pair(h);
-    return half_pair(a - kept.x, b - kept.y);
-}
 // a * b + c on two floats at once
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
 {
@@ -108,6 +102,17 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
         : "=f"(r.x), "=f"(r.y)
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
     return r;
+}
+__device__ __forceinline__ void add(float &a, float &b, float c, float d)
+{
+    asm("{\n.reg .b64 x, y;\nmov.b64 x, {%0, %1};\nmov.b64 y, {%2, %3};\nadd.rn.f32x2 x, x, y;\nmov.b64 {%0, %1}, x;\n}" : "+f"(a), "+f"(b) : "f"(c), "f"(d));
+}
+// What rounding two floats to the fp16 pair h has left behind.
+__device__ __forceinline__ uint32_t rest_pair(float a, float b, uint32_t h)
+{
+    const float2 kept = float_pair(h);
+    const float2 rest = fma2(kept, make_float2(-1.0f, -1.0f), make_float2(a, b));
+    return half_pair(rest.x, rest.y);
 }
 __device__ __forceinline__ void store_terms(const float (&f)[8], __half *hi, __half *lo)
 {
@@ -278,8 +283,36 @@ __device__ __forceinline__ void halves(const uint4 (&w)[N], float (&v)[8 * N])
     }
 }
 
+// Element k of v, which stays in registers.
+template <int N>
+__device__ __forceinline__ float pick(const float (&v)[N], uint32_t k)
+{
+    if constexpr (N == 1) {
+        return v[0];
+    } else {
+        float half[N / 2];
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) half[i] = k & 1u ? v[2 * i + 1] : v[2 * i];
+        return pick(half, k / 2u);
+    }
+}
+// The element on the diagonal, kept apart, leaves a zero in row r and column c of a box.
+__device__ __forceinline__ void clear_half(uint32_t box, uint32_t r, uint32_t c)
+{
+    asm volatile("st.shared.u16 [%0], %1;" ::"r"(box_octet(box, r, c / 8u) + c % 8u * 2u), "h"((uint16_t)0) : "memory");
+}
+
 constexpr int TAKEN = 64 / (TAKERS / 4);   // columns of a box that a warp takes
 constexpr int OCTETS = TAKEN / 8;
+
+// s2 v + (s0 + s1 d) in on two elements
+__device__ __forceinline__ void poly(float &v, float &w, float in_v, float in_w, float d_v, float d_w, float s0, float s1, float s2)
+{
+    const float2 t = fma2(make_float2(d_v, d_w), make_float2(s1, s1), make_float2(s0, s0));
+    const float2 p = fma2(t, make_float2(in_v, in_w), fma2(make_float2(v, w), make_float2(s2, s2), make_float2(0.0f, 0.0f)));
+    v = p.x;
+    w = p.y;
+}
 
 // a X + B X as X is kept, from the sums of B X
 template <int N>
@@ -312,29 +345,24 @@ __device__ __forceinline__ void finish(float (&v)[TAKEN], uint32_t batch, uint32
         halves(w, in);
     }
     if (MODE == GRAM) {
-        float own = 0.0f;
+        if (diagonal && row < a.rows) a.d[batch * a.d_stride + row] = pick(v, row - c) * (1.0f / (XS * XS));
 #pragma unroll
-        for (int k = 0; k < TAKEN; ++k) {
-            own = c + k == row ? v[k] : own;
-            v[k] = c + k == row ? 0.0f : v[k] * (AS / (XS * XS));
-        }
-        if (diagonal && row < a.rows) a.d[batch * a.d_stride + row] = own * (1.0f / (XS * XS));
+        for (int k = 0; k < TAKEN; ++k) v[k] *= AS / (XS * XS);
     }
     if (MODE == POLY) {
         const float s2 = a.cc * BS / (AS * AS), s1 = a.cc * BS / AS, s0 = a.cb * BS / AS + s1 * linear;
-        float own = 0.0f;
+        if (diagonal && row < a.rows)
+            a.db[batch * a.d_stride + row] = a.cb * linear + a.cc * (pick(v, row - c) * (1.0f / (AS * AS)) + linear * linear);
 #pragma unroll
         for (int i = 0; i < TAKEN / 4; ++i) {
             const uint4 w = load_shared(across + i * 16);
             const float d[4] = {__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < 4; j += 2) {
                 const int k = 4 * i + j;
-                own = c + k == row ? v[k] : own;
-                v[k] = c + k == row ? 0.0f : s2 * v[k] + (s0 + s1 * d[j]) * in[k];
+                poly(v[k], v[k + 1], in[k], in[k + 1], d[j], d[j + 1], s0, s1, s2);
             }
         }
-        if (diagonal && row < a.rows) a.db[batch * a.d_stride + row] = a.cb * linear + a.cc * (own * (1.0f / (AS * AS)) + linear * linear);
     }
     if (MODE == UPDATE) {
         if (a.lo_in) {
@@ -344,7 +372,7 @@ __device__ __forceinline__ void finish(float (&v)[TAKEN], uint32_t batch, uint32
             for (int i = 0; i < OCTETS; ++i) w[i] = load_shared(box_octet(box + OPERAND_BYTES, r, o + i));
             halves(w, rest);
 #pragma unroll
-            for (int k = 0; k < TAKEN; ++k) in[k] += rest[k];
+            for (int k = 0; k < TAKEN; k += 2) add(in[k], in[k + 1], rest[k], rest[k + 1]);
         }
         update(v, in, linear);
         if (a.out) {
@@ -370,6 +398,7 @@ __device__ __forceinline__ void finish(float (&v)[TAKEN], uint32_t batch, uint32
     for (int k = 0; k < TAKEN / 2; ++k) h[k] = half_pair(v[2 * k], v[2 * k + 1]);
 #pragma unroll
     for (int i = 0; i < OCTETS; ++i) store_shared(box_octet(box, r, o + i), make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]));
+    if (diagonal) clear_half(box, r, o * 8u + row - c);
     if (MODE == UPDATE && a.lo_out) {
         uint32_t l[TAKEN / 2];
 #pragma unroll
@@ -723,11 +752,14 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
     const T *const g = static_cast<const T *>(a.x) + blockIdx.y * a.x_stride;
     float v[8][8];
     double sum = 0.0;
-    const uint32_t octets = a.turned ? WHOLE_ROWS / 8 : a.width / 8;
+    // rows of X in whole products, columns of A in whole loads; what lies behind them is not looked at
+    const uint32_t rows = (a.m + 15u) / 16u * 16u;
+    const uint32_t octets = a.turned ? rows / 8 : a.width / 8, all = rows * a.width / 8;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const uint32_t n = threadIdx.x + i * WHOLE_THREADS, line = n / octets, first = n % octets * 8;   // line: row of X, or column
-        const bool inside = n < WHOLE_ROWS * a.width / 8 && (a.turned ? c0 + line < a.n && first < a.m : line < a.m && c0 + first < a.n);
+        if (i * WHOLE_THREADS >= all) break;
+        const bool inside = n < all && (a.turned ? c0 + line < a.n && first < a.m : line < a.m && c0 + first < a.n);
         if (inside) {
             if (a.turned) values(load_octet(g + (c0 + line) * a.ldx, first, a.m, a.vec), v[i]);
             else values(load_octet(g + line * a.ldx, c0 + first, a.n, a.vec), v[i]);
@@ -756,7 +788,7 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const uint32_t n = threadIdx.x + i * WHOLE_THREADS, line = n / octets, first = n % octets * 8;
-        if (n >= WHOLE_ROWS * a.width / 8) break;
+        if (n >= all) break;
         uint32_t h[4], l[4];
         times(v[i], scale);
 #pragma unroll
@@ -795,20 +827,43 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
         __syncthreads();
         fence_after_sync();
     };
-    // rows of X in whole products, columns of A in whole loads; what lies behind them in tensor memory is not looked at
-    const uint32_t rows = (a.m + 15u) / 16u * 16u;
+    // Where there are few rows B's are laid down twice or four times, one copy under another: then the update of every row
+    // stands in several quarters of tensor memory, and their warps take some of its columns each.
+    const uint32_t copies = rows <= 32u ? 4u : rows <= 64u ? 2u : 1u, span = WHOLE_ROWS / copies;
+    const uint32_t ur = r % span, ustride = 64u * copies, ufirst = (quarter * 32u / span * 4u + part) * 16u;   // of the update
+    const bool uidle = ur / 32u * 32u >= rows;
     const bool idle = quarter * 32u >= rows;
+    // and each thread keeps its elements of X in 32 bits: 16 neighbours of its row, up to four times
+    float x[4][16];
+#pragma unroll
+    for (uint32_t n = 0; n < 4; ++n) {
+        const uint32_t c = ufirst + n * ustride, at = c / 64u * BOX_BYTES, o = c / 8u % 8u;
+        if (c >= a.width || uidle) break;
+        float rest[16];
+        uint4 q[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) q[i] = load_shared(box_octet(hi + at, ur, o + i));
+        halves(q, x[n]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) q[i] = load_shared(box_octet(lo + at, ur, o + i));
+        halves(q, rest);
+#pragma unroll
+        for (int k = 0; k < 16; k += 2) add(x[n][k], x[n][k + 1], rest[k], rest[k + 1]);
+    }
     const uint32_t square = 1u << 4 | (rows / 8) << 17 | (128u / 16) << 24;
+    // operands: addresses count in 16 bytes
+    const uint64_t hi_rows = swizzled_matrix(hi, 16u, 1024u), f_rows = swizzled_matrix(f, 16u, 1024u), hi_columns = swizzled_matrix(hi, BOX_BYTES, 1024u);
     for (uint32_t step = 0; step < a.steps; ++step) {
-        const bool last = step + 1 == a.steps, lo_in = step < ORTHO_LO_STEPS, lo_out = step + 1 < ORTHO_LO_STEPS;
+        const bool last = step + 1 == a.steps;
         // ---- A = X X^T ----
         if (warp == 0 && elect_one()) {
-            for (uint32_t b = 0; b < boxes; ++b)
 #pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) {
-                    const uint64_t x = swizzled_matrix(hi + b * BOX_BYTES + i * 32u, 16u, 1024u);
-                    mma_f16<false>(tmem + A_COLUMN, x, x, square, b > 0 || i > 0);
-                }
+            for (uint32_t b = 0; b < WHOLE_COLS / BOX_COLS; ++b) {
+                if (b >= boxes) break;
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i)
+                    mma_f16<false>(tmem + A_COLUMN, hi_rows + (b * BOX_BYTES + i * 32u) / 16u, hi_rows + (b * BOX_BYTES + i * 32u) / 16u, square, b > 0 || i > 0);
+            }
             mma_commit<false>(bar);
         }
         __syncwarp();
@@ -828,18 +883,16 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
                                  make_uint4(__float_as_uint(w[4 * i]), __float_as_uint(w[4 * i + 1]), __float_as_uint(w[4 * i + 2]), __float_as_uint(w[4 * i + 3])));
                 }
             } else {
-                float own = 0.0f;
+                const bool diagonal = r - c < 16u;
+                if (diagonal) asm volatile("st.shared.f32 [%0], %1;" ::"r"(d + r * 4u), "f"(pick(w, r - c) * (1.0f / (XS * XS))));
 #pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    own = c + k == r ? w[k] : own;
-                    w[k] = c + k == r ? 0.0f : w[k] * (AS / (XS * XS));
-                }
-                if (r - c < 16u) asm volatile("st.shared.f32 [%0], %1;" ::"r"(d + r * 4u), "f"(own * (1.0f / (XS * XS))));
+                for (int k = 0; k < 16; ++k) w[k] *= AS / (XS * XS);
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
                     store_shared(box_octet(f + c / 64u * BOX_BYTES, r, c / 8u % 8u + i),
                                  make_uint4(half_pair(w[8 * i], w[8 * i + 1]), half_pair(w[8 * i + 2], w[8 * i + 3]), half_pair(w[8 * i + 4], w[8 * i + 5]),
                                             half_pair(w[8 * i + 6], w[8 * i + 7])));
+                if (diagonal) clear_half(f + c / 64u * BOX_BYTES, r, r % 64u);
             }
         }
         if (CLUSTER) {
@@ -859,12 +912,9 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
                         w[4 * i + 3] += __uint_as_float(q.w);
                     }
                 }
-                float own = 0.0f;
+                const float own = pick(w, row % 8u);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    own = o * 8u + k == row ? w[k] : own;
-                    w[k] = o * 8u + k == row ? 0.0f : w[k] * (AS / (XS * XS));
-                }
+                for (int k = 0; k < 8; ++k) w[k] = o * 8u + k == row ? 0.0f : w[k] * (AS / (XS * XS));
                 const uint4 packed = make_uint4(half_pair(w[0], w[1]), half_pair(w[2], w[3]), half_pair(w[4], w[5]), half_pair(w[6], w[7]));
                 for (uint32_t p = 0; p < cluster; ++p) {
                     store_remote(map_shared(box_octet(f + o / 8u * BOX_BYTES, row, o % 8u), p), packed);
@@ -883,9 +933,10 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
         }
         // ---- B = b A + c A A ----
         if (warp == 0 && elect_one()) {
-            for (uint32_t i = 0; i < rows / 16u; ++i) {
-                const uint64_t x = swizzled_matrix(f + i / 4 * BOX_BYTES + i % 4 * 32u, 16u, 1024u);
-                mma_f16<false>(tmem + P_COLUMN, x, x, square, i > 0);
+#pragma unroll
+            for (uint32_t i = 0; i < WHOLE_ROWS / 16; ++i) {
+                if (i * 16u >= rows) break;
+                mma_f16<false>(tmem + P_COLUMN, f_rows + (i / 4 * BOX_BYTES + i % 4 * 32u) / 16u, f_rows + (i / 4 * BOX_BYTES + i % 4 * 32u) / 16u, square, i > 0);
             }
             mma_commit<false>(bar);
         }
@@ -904,68 +955,65 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
                 for (int i = 0; i < 2; ++i) q[i] = load_shared(box_octet(f + c / 64u * BOX_BYTES, r, c / 8u % 8u + i));
                 halves(q, in);
                 tmem_wait_load();
-                float own = 0.0f;
+                const bool diagonal = r - c < 16u;
+                if (diagonal) asm volatile("st.shared.f32 [%0], %1;" ::"r"(db + r * 4u), "f"(a.cb * dr + a.cc * (pick(w, r - c) * (1.0f / (AS * AS)) + dr * dr)));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const uint4 z = load_shared(d + c * 4u + i * 16u);
                     const float dc[4] = {__uint_as_float(z.x), __uint_as_float(z.y), __uint_as_float(z.z), __uint_as_float(z.w)};
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int k = 4 * i + j;
-                        own = c + k == r ? w[k] : own;
-                        w[k] = c + k == r ? 0.0f : s2 * w[k] + (s0 + s1 * dc[j]) * in[k];
-                    }
+                    for (int j = 0; j < 4; j += 2) poly(w[4 * i + j], w[4 * i + j + 1], in[4 * i + j], in[4 * i + j + 1], dc[j], dc[j + 1], s0, s1, s2);
                 }
-                if (r - c < 16u) asm volatile("st.shared.f32 [%0], %1;" ::"r"(db + r * 4u), "f"(a.cb * dr + a.cc * (own * (1.0f / (AS * AS)) + dr * dr)));
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    store_shared(box_octet(f + c / 64u * BOX_BYTES, r, c / 8u % 8u + i),
-                                 make_uint4(half_pair(w[8 * i], w[8 * i + 1]), half_pair(w[8 * i + 2], w[8 * i + 3]), half_pair(w[8 * i + 4], w[8 * i + 5]),
-                                            half_pair(w[8 * i + 6], w[8 * i + 7])));
+                for (int i = 0; i < 2; ++i) {
+                    const uint4 packed = make_uint4(half_pair(w[8 * i], w[8 * i + 1]), half_pair(w[8 * i + 2], w[8 * i + 3]),
+                                                    half_pair(w[8 * i + 4], w[8 * i + 5]), half_pair(w[8 * i + 6], w[8 * i + 7]));
+                    store_shared(box_octet(f + c / 64u * BOX_BYTES, r, c / 8u % 8u + i), packed);
+                    if (copies > 1u)
+                        for (uint32_t p = r + span; p < WHOLE_ROWS; p += span) store_shared(box_octet(f + c / 64u * BOX_BYTES, p, c / 8u % 8u + i), packed);
+                }
+                if (diagonal)
+                    for (uint32_t p = r; p < WHOLE_ROWS; p += span) clear_half(f + c / 64u * BOX_BYTES, p, r % 64u);
             }
         }
         settled();
         // ---- X' = a X + B X ----
         if (warp == 0 && elect_one()) {
             const uint32_t instruction = 1u << 4 | 1u << 16 | (a.width / 8) << 17 | (128u / 16) << 24;
-            for (uint32_t i = 0; i < rows / 16u; ++i)
-                mma_f16<false>(tmem + U_COLUMN, swizzled_matrix(f + i / 4 * BOX_BYTES + i % 4 * 32u, 16u, 1024u), swizzled_matrix(hi + i * 2048u, BOX_BYTES, 1024u),
-                               instruction, i > 0);
+#pragma unroll
+            for (uint32_t i = 0; i < WHOLE_ROWS / 16; ++i) {
+                if (i * 16u >= rows) break;
+                mma_f16<false>(tmem + U_COLUMN, f_rows + (i / 4 * BOX_BYTES + i % 4 * 32u) / 16u, hi_columns + i * 2048u / 16u, instruction, i > 0);
+            }
             mma_commit<false>(bar);
         }
         __syncwarp();
         products_done();
-        const float linear = a.ca + load_shared_float(db + r * 4u);
-#pragma unroll 1
-        for (uint32_t c = part * 16u; c < a.width && !idle; c += 64u) {
-            float w[16], in[16];
+        const float linear = a.ca + load_shared_float(db + ur * 4u);
+#pragma unroll
+        for (uint32_t n = 0; n < 4; ++n) {
+            const uint32_t c = ufirst + n * ustride, at = c / 64u * BOX_BYTES, o = c / 8u % 8u;
+            if (c >= a.width || uidle) break;
+            float w[16];
             __syncwarp();
             tmem_load16(tmem + (quarter * 32u << 16) + U_COLUMN + c, w);
-            const uint32_t at = c / 64u * BOX_BYTES, o = c / 8u % 8u;
-            uint4 q[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) q[i] = load_shared(box_octet(hi + at, r, o + i));
-            halves(q, in);
-            if (lo_in) {
-                float rest[16];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) q[i] = load_shared(box_octet(lo + at, r, o + i));
-                halves(q, rest);
-#pragma unroll
-                for (int k = 0; k < 16; ++k) in[k] += rest[k];
-            }
             tmem_wait_load();
-            update(w, in, linear);
+            update(w, x[n], linear);
             uint32_t h[8];
-            if (last) {
+            if (!last) {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) x[n][k] = w[k];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) h[k] = half_pair(w[2 * k], w[2 * k + 1]);
+            } else {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     const __nv_bfloat162 p = __floats2bfloat162_rn(w[2 * k] * (1.0f / XS), w[2 * k + 1] * (1.0f / XS));
                     h[k] = *reinterpret_cast<const uint32_t *>(&p);
                 }
                 if (a.turned) {
-                    __nv_bfloat16 *to = a.out + blockIdx.y * a.out_stride + (c0 + c) * a.ldo + r;
-                    if (r < a.m && ok)
+                    __nv_bfloat16 *to = a.out + blockIdx.y * a.out_stride + (c0 + c) * a.ldo + ur;
+                    if (ur < a.m && ok)
 #pragma unroll
                         for (int k = 0; k < 16; ++k, to += a.ldo)
                             if (c0 + c + k < a.n) {
@@ -974,19 +1022,9 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
                             }
                     continue;
                 }
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) h[k] = half_pair(w[2 * k], w[2 * k + 1]);
-                if (lo_out) {
-                    uint32_t l[8];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) l[k] = rest_pair(w[2 * k], w[2 * k + 1], h[k]);
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) store_shared(box_octet(lo + at, r, o + i), make_uint4(l[4 * i], l[4 * i + 1], l[4 * i + 2], l[4 * i + 3]));
-                }
             }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) store_shared(box_octet(hi + at, r, o + i), make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]));
+            for (int i = 0; i < 2; ++i) store_shared(box_octet(hi + at, ur, o + i), make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]));
         }
         __syncwarp();
         settled();
