@@ -159,11 +159,10 @@ __global__ __launch_bounds__(THREADS) void qesgd_ortho_start_kernel(const T *x, 
     const uint32_t across = (cols + 63) / 64, tiles = (rows + 63) / 64 * across;
     for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x) {
         const uint32_t r0 = t / across * 64, c0 = t % across * 64;
-        for (uint32_t i = threadIdx.x; i < 64 * 64; i += THREADS) {
-            const uint32_t r = r0 + i / 64, c = c0 + i % 64;
-            const float g = r < rows && c < cols ? to_float(m[r * ldx + c]) : 0.0f;
-            held[i / 64 * 65 + i % 64] = g;
-        }
+        const uint32_t c = c0 + threadIdx.x % 64u;
+#pragma unroll
+        for (uint32_t i = threadIdx.x / 64u; i < 64; i += THREADS / 64)
+            held[i * 65 + threadIdx.x % 64u] = r0 + i < rows && c < cols ? to_float(m[(uint64_t)(r0 + i) * ldx + c]) : 0.0f;
         __syncthreads();
         for (uint32_t i = threadIdx.x; i < 64 * 8; i += THREADS) {
             const uint32_t c = c0 + i / 8, r = r0 + i % 8 * 8;
@@ -1123,7 +1122,8 @@ cudaError_t start(const OrthoArgs &a, const OrthoLayout &l, cudaStream_t stream)
     cudaError_t e = qesgd_launch(qesgd_ortho_norm_kernel<T>, grid, dim3(THREADS), stream, x, rows, cols, a.ldx, a.x_stride, vec, parts);
     if (e != cudaSuccess) return e;
     const OrthoView v = {reinterpret_cast<__half *>(a.workspace + l.off_hi[0]), reinterpret_cast<__half *>(a.workspace + l.off_lo[0]), l.ld_x, l.x_stride};
-    return qesgd_launch(rows > cols ? qesgd_ortho_start_kernel<T, true> : qesgd_ortho_start_kernel<T, false>, grid, dim3(THREADS), stream, x, rows, cols,
+    const dim3 squares((unsigned)(qesgd_div_up(rows, 64) * qesgd_div_up(cols, 64)), (unsigned)a.batch);
+    return qesgd_launch(rows > cols ? qesgd_ortho_start_kernel<T, true> : qesgd_ortho_start_kernel<T, false>, rows > cols ? squares : grid, dim3(THREADS), stream, x, rows, cols,
                         a.ldx, a.x_stride, vec, (const double *)parts, l.parts, v, a.status);
 }
 
