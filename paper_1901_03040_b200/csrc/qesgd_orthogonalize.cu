@@ -506,12 +506,13 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
                 const uint32_t s = n % S::STAGES, to = base + s * S::STAGE_BYTES;
                 if (n >= S::STAGES && !pipe_wait(empty + 8 * s, (n / S::STAGES - 1u) & 1u, stop)) break;
                 const uint32_t at = (step0 + k) * DEPTH;
-                if (!PAIR || rank == 0) mbar_expect_at(full + 8 * s, (OPERAND_BYTES + S::Q_BYTES) * (PAIR ? 2u : 1u));
+                const bool own = MODE != UPDATE && !x.mirror;   // a square on the diagonal: Q's rows are among P's
+                if (!PAIR || rank == 0) mbar_expect_at(full + 8 * s, (OPERAND_BYTES + (own ? 0u : S::Q_BYTES)) * (PAIR ? 2u : 1u));
                 tma_load_3d<PAIR>(to, &maps.p, at, row, x.batch, full_lead + 8 * s);
                 if (MODE == UPDATE) {
                     tma_load_3d<PAIR>(to + OPERAND_BYTES, &maps.q, col, at, x.batch, full_lead + 8 * s);
                     if (!NARROW) tma_load_3d<PAIR>(to + OPERAND_BYTES + OPERAND_BYTES / 2, &maps.q, col + 64u, at, x.batch, full_lead + 8 * s);
-                } else {
+                } else if (!own) {
                     tma_load_3d<PAIR>(to + OPERAND_BYTES, &maps.q, at, col, x.batch, full_lead + 8 * s);
                 }
             }
@@ -523,6 +524,8 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
         uint32_t n = 0, done_tiles = 0;
         for (uint32_t t = group; t < all && !*stop; t += groups, ++done_tiles) {
             const uint32_t half = done_tiles & 1u, sums = tmem + half * S::WIDTH;
+            const Tile x = tile_of<MODE, S::SIDE, S::WIDTH>(t, a);
+            const uint32_t q_at = MODE == UPDATE || x.mirror ? OPERAND_BYTES : (x.col - x.row) * 128u;
             if (done_tiles >= 2 && !pipe_wait(free_ + 8 * half, (done_tiles / 2 - 1u) & 1u, stop)) break;
             fence_after_sync();
             bool ok = true;
@@ -535,7 +538,7 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
                 for (uint32_t i = 0; i < DEPTH / 16; ++i) {
                     const uint64_t p = swizzled_matrix(from + i * 32u, 16u, 1024u);
                     const uint64_t q = MODE == UPDATE ? swizzled_matrix(from + OPERAND_BYTES + i * 2048u, OPERAND_BYTES / 2, 1024u)
-                                                      : swizzled_matrix(from + OPERAND_BYTES + i * 32u, 16u, 1024u);
+                                                      : swizzled_matrix(from + q_at + i * 32u, 16u, 1024u);
                     mma_f16<PAIR>(sums, p, q, INSTRUCTION, k > 0 || i > 0);
                 }
                 mma_commit<PAIR>(empty + 8 * s);
