@@ -10,6 +10,8 @@
 // Memory is the floor; the instructions are what bounds it: 26 an element with draws (5 of them Philox's), 20 without and
 // for both axes.  4096 x 4096 fp32 with draws and its way back to bf16 27 us together, where the bytes take 18; 8192 x 8192
 // bf16 along both axes and both ways back 116 us, where they take 85.
+#include <type_traits>
+
 #include "qesgd_matrix.cuh"
 
 namespace {
@@ -200,31 +202,31 @@ __device__ __forceinline__ uint2 quantize_span(const Octet<T> (&x)[2], uint64_t 
 }
 
 // ------------------------------------------------------- blocks along rows ----
-// A CTA's tile: 64 rows, half of a tile of scales, by 256 columns, 16 for each lane, two rows for a warp at a time.
-constexpr int ROW_COLS = 256, HALF_ROWS = TILE_ROWS / 2;
+// A CTA's tile: 64 rows (or 32), part of a tile of scales, by 256 columns, 16 for each lane, two rows for a warp at a time.
+constexpr int ROW_COLS = 256;
 
-template <typename T, int FORMAT, bool SCALED, bool STOCHASTIC>
+template <typename T, int FORMAT, bool SCALED, bool STOCHASTIC, int ROWS>
 __global__ __launch_bounds__(THREADS, 4) void qesgd_fp4_quantize_rows_kernel(const __grid_constant__ Fp4QuantizeArgs a)
 {
     constexpr int BLOCK = Format<FORMAT>::BLOCK;
     constexpr int TILES = ROW_COLS / BLOCK / 4;        // of scales
     constexpr int UNROLL = sizeof(T) == 4 ? 1 : 2;
-    __shared__ __align__(16) uint8_t scales[TILES * SCALE_TILE];   // rows 0 to 63 in the first 8 of every 16 bytes
+    __shared__ __align__(16) uint8_t scales[TILES * SCALE_TILE];   // the first 8 (or 4) of every 16 bytes
     __shared__ float2 inverse[128];
     if (FORMAT == QESGD_FP4_NV) fill_inverse(inverse);
     qesgd_wait_for_previous();
     const uint32_t o = threadIdx.x % 16u, line = threadIdx.x / 16u;
     const uint32_t col_tiles = (uint32_t)((a.cols + ROW_COLS - 1) / ROW_COLS);
-    const uint64_t tiles = (uint64_t)col_tiles * ((a.rows + TILE_ROWS - 1) / TILE_ROWS * 2);
+    const uint64_t tiles = (uint64_t)col_tiles * ((a.rows + TILE_ROWS - 1) / TILE_ROWS * (TILE_ROWS / ROWS));
     const uint64_t padded = (a.cols + 31) / 32 * 32;
     const uint64_t scale_tiles = (a.cols + 4 * BLOCK - 1) / (4 * BLOCK);
     const float to_tensor = SCALED ? power_of_two(-tensor_exponent(a.tensor_exponent)) : 1.0f;
     bool bad = false;
     for (uint64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const uint64_t row0 = tile / col_tiles * HALF_ROWS;
+        const uint64_t row0 = tile / col_tiles * ROWS;
         const uint32_t col0 = (uint32_t)(tile % col_tiles) * ROW_COLS;
-        const uint32_t rows = row0 < a.rows ? (uint32_t)min((uint64_t)HALF_ROWS, a.rows - row0) : 0u;
-        if (rows < HALF_ROWS)
+        const uint32_t rows = row0 < a.rows ? (uint32_t)min((uint64_t)ROWS, a.rows - row0) : 0u;
+        if (rows < ROWS)
             for (uint32_t i = threadIdx.x; i < sizeof(scales) / 4; i += THREADS) reinterpret_cast<uint32_t *>(scales)[i] = 0u;
         __syncthreads();
         const uint64_t c = col0 + o * 16u;
@@ -264,9 +266,10 @@ __global__ __launch_bounds__(THREADS, 4) void qesgd_fp4_quantize_rows_kernel(con
         __syncthreads();
         const uint64_t at = col0 / (4 * BLOCK);
         const uint32_t have = (uint32_t)min((uint64_t)TILES, scale_tiles - at);
-        uint8_t *const out = a.scales + (row0 / TILE_ROWS * scale_tiles + at) * SCALE_TILE + row0 / HALF_ROWS % 2 * 8;
+        uint8_t *const out = a.scales + (row0 / TILE_ROWS * scale_tiles + at) * SCALE_TILE + row0 / 32 % 4 * 4;
+        using Rows = std::conditional_t<ROWS == 64, uint2, uint32_t>;   // rows 32 apart are neighbours
         for (uint32_t i = threadIdx.x; i < have * (SCALE_TILE / 16); i += THREADS)
-            *reinterpret_cast<uint2 *>(out + i * 16u) = *reinterpret_cast<const uint2 *>(scales + i * 16u);
+            *reinterpret_cast<Rows *>(out + i * 16u) = *reinterpret_cast<const Rows *>(scales + i * 16u);
         __syncthreads();
     }
     if (bad) atomicOr(a.status, QESGD_STATUS_NONFINITE);
@@ -575,11 +578,18 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_tensor_exponent_kernel(cons
 }
 
 template <typename T, int FORMAT, bool SCALED, bool STOCHASTIC>
-cudaError_t launch_quantize(const Fp4QuantizeArgs &a, cudaStream_t stream)
+cudaError_t launch_quantize(const Fp4QuantizeArgs &a, int sm_count, cudaStream_t stream)
 {
-    const uint64_t tiles = qesgd_div_up(a.rows, TILE_ROWS) * (a.codes_t ? qesgd_div_up(a.cols, SIDE) : 2 * qesgd_div_up(a.cols, ROW_COLS));
-    const dim3 grid((unsigned)(tiles < 0x7FFFFFFF ? tiles : 0x7FFFFFFF));
-    if (!a.codes_t) return qesgd_launch(qesgd_fp4_quantize_rows_kernel<T, FORMAT, SCALED, STOCHASTIC>, grid, dim3(THREADS), stream, a);
+    const auto grid_of = [](uint64_t tiles) { return dim3((unsigned)(tiles < 0x7FFFFFFF ? tiles : 0x7FFFFFFF)); };
+    if (!a.codes_t) {
+        // Tiles of 32 rows where those of 64 would all run at once (four to an SM), so that they spread evenly: 64 x 65536
+        // fp32 with draws and back 10.2 us in place of 12.5, 512 x 4096 6.6 in place of 7.0, but 4096 x 4096 28.7 in place of 27.1.
+        const uint64_t halves = qesgd_div_up(a.rows, TILE_ROWS) * 2 * qesgd_div_up(a.cols, ROW_COLS);
+        return halves <= 4 * (uint64_t)sm_count
+                   ? qesgd_launch(qesgd_fp4_quantize_rows_kernel<T, FORMAT, SCALED, STOCHASTIC, 32>, grid_of(2 * halves), dim3(THREADS), stream, a)
+                   : qesgd_launch(qesgd_fp4_quantize_rows_kernel<T, FORMAT, SCALED, STOCHASTIC, 64>, grid_of(halves), dim3(THREADS), stream, a);
+    }
+    const dim3 grid = grid_of(qesgd_div_up(a.rows, TILE_ROWS) * qesgd_div_up(a.cols, SIDE));
     const auto kernel = qesgd_fp4_quantize_columns_kernel<T, FORMAT, SCALED, STOCHASTIC>;
     const int smem = SIDE * SIDE * (int)sizeof(T);
     static std::atomic<uint64_t> told{0};
@@ -587,15 +597,15 @@ cudaError_t launch_quantize(const Fp4QuantizeArgs &a, cudaStream_t stream)
     return e != cudaSuccess ? e : qesgd_launch_smem(kernel, grid, dim3(THREADS), smem, stream, a);
 }
 template <typename T, bool STOCHASTIC>
-cudaError_t launch_quantize(const Fp4QuantizeArgs &a, uint32_t format, cudaStream_t stream)
+cudaError_t launch_quantize(const Fp4QuantizeArgs &a, uint32_t format, int sm_count, cudaStream_t stream)
 {
-    if (format == QESGD_FP4_MX) return launch_quantize<T, QESGD_FP4_MX, false, STOCHASTIC>(a, stream);
-    return a.tensor_exponent ? launch_quantize<T, QESGD_FP4_NV, true, STOCHASTIC>(a, stream) : launch_quantize<T, QESGD_FP4_NV, false, STOCHASTIC>(a, stream);
+    if (format == QESGD_FP4_MX) return launch_quantize<T, QESGD_FP4_MX, false, STOCHASTIC>(a, sm_count, stream);
+    return a.tensor_exponent ? launch_quantize<T, QESGD_FP4_NV, true, STOCHASTIC>(a, sm_count, stream) : launch_quantize<T, QESGD_FP4_NV, false, STOCHASTIC>(a, sm_count, stream);
 }
 template <typename T>
-cudaError_t launch_quantize(const Fp4QuantizeArgs &a, uint32_t format, bool stochastic, cudaStream_t stream)
+cudaError_t launch_quantize(const Fp4QuantizeArgs &a, uint32_t format, bool stochastic, int sm_count, cudaStream_t stream)
 {
-    return stochastic ? launch_quantize<T, true>(a, format, stream) : launch_quantize<T, false>(a, format, stream);
+    return stochastic ? launch_quantize<T, true>(a, format, sm_count, stream) : launch_quantize<T, false>(a, format, sm_count, stream);
 }
 template <typename T, int FORMAT>
 cudaError_t launch_dequantize(const Fp4DequantizeArgs &a, cudaStream_t stream)
@@ -621,12 +631,12 @@ cudaError_t launch_exponent(const void *x, uint64_t rows, uint64_t cols, uint64_
 
 }  // namespace
 
-int qesgd_launch_fp4_quantize(const Fp4QuantizeArgs &a, uint32_t dtype, uint32_t format, bool stochastic, cudaStream_t stream)
+int qesgd_launch_fp4_quantize(const Fp4QuantizeArgs &a, uint32_t dtype, uint32_t format, bool stochastic, int sm_count, cudaStream_t stream)
 {
     switch (dtype) {
-        case QESGD_F32: return (int)launch_quantize<float>(a, format, stochastic, stream);
-        case QESGD_BF16: return (int)launch_quantize<__nv_bfloat16>(a, format, stochastic, stream);
-        default: return (int)launch_quantize<__half>(a, format, stochastic, stream);
+        case QESGD_F32: return (int)launch_quantize<float>(a, format, stochastic, sm_count, stream);
+        case QESGD_BF16: return (int)launch_quantize<__nv_bfloat16>(a, format, stochastic, sm_count, stream);
+        default: return (int)launch_quantize<__half>(a, format, stochastic, sm_count, stream);
     }
 }
 int qesgd_launch_fp4_dequantize(const Fp4DequantizeArgs &a, uint32_t dtype, uint32_t format, cudaStream_t stream)

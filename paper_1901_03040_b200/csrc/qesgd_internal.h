@@ -219,7 +219,7 @@ struct OrthoArgs {
 inline uint64_t qesgd_div_up(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 int qesgd_launch_fp4_tensor_exponent(const void *x, uint32_t dtype, uint64_t rows, uint64_t cols, uint64_t ldx, bool vec,
                                      int32_t *out, uint32_t *status, int sm_count, cudaStream_t stream);
-int qesgd_launch_fp4_quantize(const Fp4QuantizeArgs &a, uint32_t dtype, uint32_t format, bool stochastic, cudaStream_t stream);
+int qesgd_launch_fp4_quantize(const Fp4QuantizeArgs &a, uint32_t dtype, uint32_t format, bool stochastic, int sm_count, cudaStream_t stream);
 int qesgd_launch_fp4_dequantize(const Fp4DequantizeArgs &a, uint32_t dtype, uint32_t format, cudaStream_t stream);
 int qesgd_launch_fp4_matmul(const Fp4MatmulArgs &a, uint32_t dtype, uint32_t format, int sm_count, cudaStream_t stream, int *launched);
 int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t stream, int *launched);

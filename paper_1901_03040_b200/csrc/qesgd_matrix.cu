@@ -86,7 +86,7 @@ int qesgd_fp4_quantize(qesgd_ctx *ctx, const void *x, uint32_t dtype, uint64_t r
     a.status = ctx->d_status;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return qesgd_cuda_fail(ctx, (int)cudaErrorInvalidDevice);
-    const int e = qesgd_launch_fp4_quantize(a, dtype, format, rounding == QESGD_ROUND_STOCHASTIC, ctx->stream);
+    const int e = qesgd_launch_fp4_quantize(a, dtype, format, rounding == QESGD_ROUND_STOCHASTIC, ctx->sm_count, ctx->stream);
     if (e != 0) return qesgd_cuda_fail(ctx, e);
     ctx->launches += 1;
     return QESGD_OK;

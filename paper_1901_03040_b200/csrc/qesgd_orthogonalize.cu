@@ -697,10 +697,16 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
 
 // ---------------------------------------------------- a whole matrix at once ----
 // Matrices with up to 128 rows (of the smaller side) and 4096 columns: all steps in one kernel.  A cluster of 1 to 16 CTAs
-// has a matrix, each up to 256 of its columns: X in two terms, and F, then B in its place, stay in shared memory; all sums
-// stay in tensor memory.  A step exchanges the parts of A among the CTAs: each adds up some of its columns, in the order
-// of the CTAs, and writes F's share of them into every CTA.  The fifteen products as kernels of their own take 5 us each
-// here, most of it for starting, waiting for the first copies and storing what the next one loads.
+// has a matrix, each up to 256 of its columns: X stays in registers in 32 bits and in shared memory in 16, where the
+// products read it, beside F, then B in its place; all sums stay in tensor memory.  A step exchanges the parts of A among
+// the CTAs: each adds up some of its columns, in the order of the CTAs, and writes F's share of them into every CTA.  The
+// fifteen products as kernels of their own take 5 us each here, most of it for starting, waiting for the first copies
+// and storing what the next one loads.
+// 64 x 256 takes 21 us: 3.5 to load and divide by the norm, then 3.1 a step, half of it from a product's first instruction
+// to its sums' arrival (sixteen instructions deep for A), half to take the sums out and settle what the next one reads.
+// Two terms of X in shared memory in place of 32 bits: 21.9, and 25.9 with half of the warps idle at the update's
+// end.  128 x 4096 takes 68 us, half of it for the exchange.  (A begun with the columns that are done, while others are still
+// taken out, made it 21.8 and 72: each part costs one more barrier.)
 constexpr uint32_t WHOLE_ROWS = 128, WHOLE_COLS = 256, WHOLE_MAX_CLUSTER = 16;
 constexpr uint32_t BOX_BYTES = OPERAND_BYTES;              // 128 rows of 64 columns
 constexpr uint32_t WHOLE_EXTRA = 1152;                     // diagonals, barrier and the like

@@ -83,6 +83,17 @@ def test_quantize_stochastic(fmt, dtype, rows, cols):
         _check_held(held, _np(x)[:, :cols], fmt, 0, seed, 3, 0xFFFFFFFF)
 
 
+@pytest.mark.parametrize("seed", [None, 11])
+@pytest.mark.parametrize("rows,cols,dtype", [(129, 40001, qesgd.BF16), (1000, 4800, qesgd.F32)])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_quantize_of_many_tiles(fmt, rows, cols, dtype, seed):
+    """More tiles of 64 rows than run at once: smaller matrices take tiles of 32."""
+    x = _x(rows, cols, dtype, 21, 3)
+    held, status = _quantize(x, cols, fmt, "r", seed, 1, 2, dtype=dtype)
+    assert status == 0
+    _check_held(held, _np(x)[:, :cols], fmt, 0, seed, 1, 2)
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_every_border_of_the_grid_and_of_the_scales(fmt):
     """Blocks whose largest magnitude runs over all scale borders (6 times a scale and its neighbours in fp32), with
@@ -374,6 +385,17 @@ def test_orthogonalize_of_few_rows(rows, cols):
     for i in range(2):
         want = ref.orthogonalize(_np(x[i]))
         assert np.linalg.norm(got[i] - want) <= ORTHO_TOLERANCE * np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("rows,cols", [(48, 500), (500, 40), (32, 4000), (33, 257), (3000, 20), (64, 64), (16, 200), (10, 256), (65, 190)])
+def test_orthogonalize_where_quarters_share_rows(rows, cols):
+    """Up to 32 and up to 64 rows of the smaller side, for which the update of a row is taken out by several warps."""
+    x = _gradient(3, rows, cols, qesgd.F32, 6, 2)
+    for steps in (1, 2, 5):
+        got = _np(_orthogonalize(x, qesgd.F32, rows, cols, 3, steps))
+        for i in range(3):
+            want = ref.orthogonalize(_np(x[i, :, :cols]), steps)
+            assert np.linalg.norm(got[i] - want) <= ORTHO_TOLERANCE * np.linalg.norm(want)
 
 
 def test_orthogonalize_steps_and_coefficients():
