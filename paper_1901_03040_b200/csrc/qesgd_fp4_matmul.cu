@@ -176,7 +176,7 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const _
     const uint32_t every = (q_rows + parts - 1u) / parts;            // rows of A that a CTA sums up, at most
     bool joined = PAIR || parts == 1;                                // has this warp seen that all of the cluster are there?
     if (!joined) cluster_arrive();
-    const uint32_t first = (uint32_t)((uint64_t)a.steps * part / parts), steps = (uint32_t)((uint64_t)a.steps * (part + 1) / parts) - first;
+    const uint32_t steps = (a.steps - part + parts - 1u) / parts;    // dealt out in turn, so that neighbours read neighbouring bytes
     qesgd_wait_for_previous();
 
     if (warp == 0 && elect_one()) {
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const _
         const uint32_t bytes = (LANES + (PAIR ? S::HELD_Q : q_rows)) * 128u + SCALE_TILES * SCALE_TILE * (1u + S::MOST_Q / 128u);
         for (uint32_t t = group; t < a.tiles && !*stop; t += groups) {
             const uint32_t p0 = t % a.tiles_n * (PAIR ? 256u : 128u) + (PAIR ? rank * 128u : 0u), q0 = t / a.tiles_n * q_rows;
-            for (uint32_t k = first; k < first + steps; ++k) {
+            for (uint32_t k = part; k < a.steps; k += parts) {
                 const uint32_t to = base + s * S::STAGE_BYTES, bar = full_lead + 8 * s;
                 if (turn > 0 && !pipe_wait(empty + 8 * s, (turn - 1u) & 1u, stop)) break;
                 if (!PAIR || rank == 0)
@@ -336,7 +336,7 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_fp4_matmul_kernel(const _
                     sum[k][0] = old[k][0] = 0.0f;
                     if (ACCUMULATE && row < rows) load_column<T>(old[k], m0 + row, n, a);
                 }
-                for (uint32_t r = 0; r < parts; ++r)   // in the order of the contraction
+                for (uint32_t r = 0; r < parts; ++r)   // in the order of the CTAs
 #pragma unroll
                     for (uint32_t k = 0; k < ROWS; ++k) {
                         const uint32_t i = min(i0 + k * GROUPS, every - 1u);
