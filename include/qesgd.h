@@ -404,7 +404,7 @@ int qesgd_fp4_matmul(qesgd_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_sc
  * x: `batch` matrices of rows x cols (row stride ldx, matrix stride x_stride, in elements of type
  * dtype); out: the same in BF16 (ldo, out_stride), which may be x itself where the layouts agree.
  * The products take fp16 operands (scaled by powers of two) and accumulate in fp32; the term a X of
- * the first three steps carries 22 bits.  Five usual steps end 2e-3 of the result from the exact
+ * the first three steps carries 22 bits or more.  Five usual steps end 2e-3 of the result from the exact
  * one, of which 1.7e-3 is the final rounding to BF16.  a, b, c finite, |a| <= 16, |b|, |c| <= 32; where they let
  * singular values grow beyond 3, intermediates are cut off at fp16's largest number.  A matrix of zeros gives zeros; one with a
  * non-finite element gives zeros and QESGD_STATUS_NONFINITE, the others of the batch are not

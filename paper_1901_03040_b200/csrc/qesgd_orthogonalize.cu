@@ -196,10 +196,10 @@ __global__ __launch_bounds__(THREADS) void qesgd_ortho_start_kernel(const T *x, 
 // by the warps themselves, a row for each lane, the update of 12 x 512 x 2048 took 63 us, three times what its products
 // take: 32 rows' segments in one instruction are 32 passes through the load-store unit.)
 //
-// Five steps on 4096 x 8192 take 2.16 ms, 1.1 PFLOP/s: a stage of GRAM or POLY takes 513 clocks of the tensor cores' 512, so
+// Five steps on 4096 x 8192 take 2.15 ms, 1.1 PFLOP/s: a stage of GRAM or POLY takes 513 clocks of the tensor cores' 512, so
 // the clock under the power cap and whole waves of tiles (136 on 74 pairs) bound it.  An update's contraction is as short
 // as the smaller side: at 512 its tiles' ends, which move three terms of X, come to as many bytes of shared memory as its
-// stages.  With few tiles it is the chain of fifteen launches, some 6 to 8 us each (500 x 500: 119 us).
+// stages.  With few tiles it is the chain of fifteen launches, some 6 to 8 us each (500 x 500: 117 us).
 enum Product { GRAM, POLY, UPDATE };
 
 constexpr int TAKERS = 16;                    // warps that take tiles out: four for each quarter of tensor memory
