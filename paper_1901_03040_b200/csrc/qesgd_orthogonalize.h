@@ -37,7 +37,7 @@ inline OrthoLayout qesgd_ortho_layout(uint64_t rows, uint64_t cols, uint64_t bat
     l.x_stride = (l.m * l.ld_x + 63) / 64 * 64;
     l.a_stride = (l.m * l.ld_a + 63) / 64 * 64;
     const uint64_t parts = qesgd_div_up(l.m * l.n, 4096);
-    // as many CTAs as run at once: 12 x 512 x 2048 with 3072 of them, start and norm took 28 us, and 22 with a third of them
+    // as many CTAs as run at once: norm and start of 12 x 512 x 2048 took 28 us with three times as many, and 22 so
     const uint64_t most = batch < 64 ? 1024 / batch : 16;
     l.parts = (uint32_t)(parts < most ? parts : most);
     uint64_t at = (batch * l.parts * sizeof(double) + 255) / 256 * 256;
