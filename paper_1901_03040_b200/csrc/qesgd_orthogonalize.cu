@@ -93,6 +93,13 @@ __device__ __forceinline__ uint32_t half_pair(float a, float b)
     asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
     return r;
 }
+// The same without the rounding.
+__device__ __forceinline__ float cut_off(float v)
+{
+    float r;
+    asm("min.xorsign.abs.f32 %0, %1, %2;" : "=f"(r) : "f"(v), "f"(65504.0f));
+    return r;
+}
 __device__ __forceinline__ float2 float_pair(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2 *>(&h)); }
 // a * b + c on two floats at once
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
@@ -1011,7 +1018,7 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
             uint32_t h[8];
             if (!last) {
 #pragma unroll
-                for (int k = 0; k < 16; ++k) x[n][k] = w[k];
+                for (int k = 0; k < 16; ++k) x[n][k] = cut_off(w[k]);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) h[k] = half_pair(w[2 * k], w[2 * k + 1]);
             } else {

@@ -407,6 +407,17 @@ def test_orthogonalize_steps_and_coefficients():
         assert np.linalg.norm(got - want) <= (2.0 ** -8 + steps * 2 * 2.0 ** -11) * np.linalg.norm(want)
 
 
+@pytest.mark.parametrize("rows,cols", [(8, 16), (60, 250), (128, 700), (200, 300)])
+def test_orthogonalize_of_growing_singular_values_stays_finite(rows, cols):
+    """Coefficients that multiply by 16 a step: what is kept between steps is cut off at 65504 / 256, so that the last step's
+    terms are at most |a + b d + c (A A + d d)| 256 with d below cols 256^2, far inside bf16's range."""
+    x = _gradient(2, rows, cols, qesgd.F32, 9)
+    for a, b, c in ((16.0, 0.0, 0.0), (16.0, 32.0, 32.0), (-16.0, -32.0, -32.0)):
+        got = _orthogonalize(x, qesgd.F32, rows, cols, 2, 16, a=a, b=b, c=c)
+        assert torch.isfinite(got).all() and (got != 0).any()
+    assert G.ctx().qesgd_status() == 0
+
+
 def test_orthogonalize_with_far_singular_values():
     """Sixteen directions 160 times as strong as the rest: the rest has to come out right too."""
     g = torch.Generator().manual_seed(0)
