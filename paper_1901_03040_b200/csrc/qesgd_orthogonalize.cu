@@ -705,8 +705,9 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
 
 // ---------------------------------------------------- a whole matrix at once ----
 // Matrices with up to 128 rows (of the smaller side) and 4096 columns: all steps in one kernel.  A cluster of 1 to 16 CTAs
-// has a matrix, each up to 256 of its columns: X stays in registers in 32 bits and in shared memory in 16, where the
-// products read it, beside F, then B in its place; all sums stay in tensor memory.  A step exchanges the parts of A among
+// has a matrix, each up to 256 of its columns: X stays in registers in 32 bits and in shared memory as one fp16 term, for the
+// updates of the first ORTHO_TERMS_STEPS steps as two, where the products read it, beside F, then B in its place; all sums
+// stay in tensor memory.  A step exchanges the parts of A among
 // the CTAs: each adds up some of its columns, in the order of the CTAs, and writes F's share of them into every CTA.  The
 // fifteen products as kernels of their own take 5 us each here, most of it for starting, waiting for the first copies
 // and storing what the next one loads.
@@ -868,7 +869,8 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
     }
     const uint32_t square = 1u << 4 | (rows / 8) << 17 | (128u / 16) << 24;
     // operands: addresses count in 16 bytes
-    const uint64_t hi_rows = swizzled_matrix(hi, 16u, 1024u), f_rows = swizzled_matrix(f, 16u, 1024u), hi_columns = swizzled_matrix(hi, BOX_BYTES, 1024u);
+    const uint64_t hi_rows = swizzled_matrix(hi, 16u, 1024u), f_rows = swizzled_matrix(f, 16u, 1024u);
+    const uint64_t hi_columns = swizzled_matrix(hi, BOX_BYTES, 1024u), lo_columns = swizzled_matrix(lo, BOX_BYTES, 1024u);
     for (uint32_t step = 0; step < a.steps; ++step) {
         const bool last = step + 1 == a.steps;
         // ---- A = X X^T ----
@@ -1001,6 +1003,11 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
                 if (i * 16u >= rows) break;
                 mma_f16<false>(tmem + U_COLUMN, f_rows + (i / 4 * BOX_BYTES + i % 4 * 32u) / 16u, hi_columns + i * 2048u / 16u, instruction, i > 0);
             }
+#pragma unroll
+            for (uint32_t i = 0; i < WHOLE_ROWS / 16; ++i) {
+                if (i * 16u >= rows || step >= ORTHO_TERMS_STEPS) break;
+                mma_f16<false>(tmem + U_COLUMN, f_rows + (i / 4 * BOX_BYTES + i % 4 * 32u) / 16u, lo_columns + i * 2048u / 16u, instruction, true);
+            }
             mma_commit<false>(bar);
         }
         __syncwarp();
@@ -1021,6 +1028,13 @@ __global__ __launch_bounds__(WHOLE_THREADS, 1) void qesgd_ortho_whole_kernel(con
                 for (int k = 0; k < 16; ++k) x[n][k] = cut_off(w[k]);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) h[k] = half_pair(w[2 * k], w[2 * k + 1]);
+                if (step + 1 < ORTHO_TERMS_STEPS) {
+                    uint32_t l[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) l[k] = rest_pair(x[n][2 * k], x[n][2 * k + 1], h[k]);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) store_shared(box_octet(lo + at, ur, o + i), make_uint4(l[4 * i], l[4 * i + 1], l[4 * i + 2], l[4 * i + 3]));
+                }
             } else {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {

@@ -14,6 +14,13 @@ constexpr float ORTHO_X_SCALE = 256.0f, ORTHO_A_SCALE = 4096.0f, ORTHO_B_SCALE =
 // falling as 1 / i (512 x 512) five steps end 3.3e-3 off without, 1.9e-3 with two steps of it, 1.8e-3 with three (of which
 // 1.7e-3 is the result's rounding to bf16); from the fourth on it gains nothing.
 constexpr uint32_t ORTHO_LO_STEPS = 3;
+// Where singular values lie far apart, B X takes both terms of X in the first steps.  What rounding X to one term leaves
+// behind are new directions, as large as weak ones: |b s^2 + c s^4| = 2.8 times them enters X', and each later step enlarges
+// it by 3.4.  (B's own rounding only mixes the rows that X has: a second term of B changes nothing.)  Five steps, worst of 1 to
+// 64 strong directions 10 to 10^5 times the rest, before the result's rounding: 8 x 8 4e-2 off with one term, 8e-3 with two
+// in the first step, 3e-3 in two steps, 1e-3 in three; 64 x 1000 8e-3, 4e-3, 3e-3, 1e-3; 128 x 128 4e-3, 2e-3, 2e-3, 1e-3.
+// Both terms in all steps gain nothing on three.
+constexpr uint32_t ORTHO_TERMS_STEPS = 3;
 
 struct OrthoView {
     __half *hi, *lo;

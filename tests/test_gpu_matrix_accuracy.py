@@ -1,0 +1,75 @@
+"""How near the orthogonalised update is to the exact one, whatever its spectrum."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():
+    pytest.skip("no CUDA device", allow_module_level=True)
+
+from paper_1901_03040_b200 import qesgd                     # noqa: E402
+from tests import gpu_helpers as G                          # noqa: E402
+
+# What five usual steps may be off, as a share of the result's 2-norm.
+#   The result's rounding to bf16: an element is off by at most 2^-8 of it, 0.425 * 2^-8 = 1.66e-3 in the mean of squares over
+#   mantissas spread evenly over their logarithm (uniform error within a unit, whose share of the value falls from 2^-8 to 2^-9).
+#   A and B off their diagonals are kept in fp16, three bits finer: r = 2.08e-4 in the same mean.  With p(s) / s = a + b s^2 + c s^4,
+#   an error of A enters X' as (b + 2 c s^2) s^2 / (p(s) / s) of it, at most 1.33 times (s^2 = 0.8), one of B as
+#   (b s^2 + c s^4) / (p(s) / s), at most 4.4 times (s^2 = 1.17): 4.6 r = 9.6e-4 a step, and sqrt(5) of that, 2.2e-3, for
+#   five steps of independent roundings.
+#   Together sqrt(1.66^2 + 2.2^2) = 2.75e-3.
+ROUNDING = 0.425 * 2.0 ** -8
+STEP = 4.6 * 0.425 * 2.0 ** -11
+WIDE_TOLERANCE = float(np.hypot(ROUNDING, np.sqrt(5.0) * STEP))
+
+
+def _orthogonalize(x, steps=5, **coefficients):
+    batch, rows, cols = x.shape
+    need = qesgd.orthogonalize_workspace(rows, cols, batch)
+    work = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")           # NaN in every type
+    out = torch.empty((batch, rows, cols), dtype=torch.bfloat16, device="cuda")
+    G.ctx().qesgd_orthogonalize(x, qesgd.F32, rows, cols, x.stride(1), batch, x.stride(0) if batch > 1 else 0, steps, out, cols,
+                                rows * cols, work, need, **coefficients)
+    return out
+
+
+def _exact(x, steps=5, a=3.4445, b=-4.7750, c=2.0315):
+    x = x.double()
+    turned = x.shape[1] > x.shape[2]
+    x = x.mT if turned else x
+    x = x / torch.linalg.matrix_norm(x, keepdim=True)
+    for _ in range(steps):
+        g = x @ x.mT
+        x = a * x + (b * g + c * (g @ g)) @ x
+    return x.mT if turned else x
+
+
+def _off(got, want):
+    norm = torch.linalg.matrix_norm
+    return (norm(got.double() - want) / norm(want)).tolist()
+
+
+def _strong(rows, cols, strong, rest, seed):
+    """`strong` directions over noise `rest` times as large."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((rows, strong), generator=g) @ torch.randn((strong, cols), generator=g) / strong ** 0.5
+    return (x + rest * torch.randn((rows, cols), generator=g)).cuda()
+
+
+def _spectra(rows, cols):
+    k = min(rows, cols)
+    return torch.stack([_strong(rows, cols, r, rest, 7 * i + r)
+                        for r in sorted({1, 4, 16, k // 4, k // 2}) if 2 * r <= k
+                        for i, rest in enumerate((1e-1, 1e-2, 1e-3, 1e-5))])
+
+
+@pytest.mark.parametrize("rows,cols", [(16, 64), (1000, 16), (32, 512), (48, 48), (64, 256), (64, 1000), (100, 1000), (128, 128), (700, 120),
+                                       (128, 4096)])
+def test_far_singular_values_in_one_kernel(rows, cols):
+    x = _spectra(rows, cols)
+    for part in x.split(8):
+        part = part.contiguous()
+        off = _off(_orthogonalize(part), _exact(part))
+        assert max(off) <= WIDE_TOLERANCE, off
+    assert G.ctx().qesgd_status() == 0
