@@ -399,13 +399,14 @@ int qesgd_fp4_matmul(qesgd_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_sc
  * applies O instead of the averaged delta G: with X = G / ||G||_F, `steps` times
  *   A = X X^T,  X <- a X + (b A + c A A) X        (on the side with fewer rows)
  * which takes every singular value s of X to p(s) = a s + b s^3 + c s^5, step by step.  The usual
- * a, b, c = 3.4445, -4.7750, 2.0315 and five steps bring singular values between 0.01 and 1 of
- * the largest into about [0.7, 1.2].
+ * a, b, c = 3.4445, -4.7750, 2.0315 and five steps bring singular values of X between 0.0015 and 1
+ * (of the matrix's norm, which is that of all of them) into [0.68, 1.21].
  * x: `batch` matrices of rows x cols (row stride ldx, matrix stride x_stride, in elements of type
  * dtype); out: the same in BF16 (ldo, out_stride), which may be x itself where the layouts agree.
- * The products take fp16 operands (scaled by powers of two) and accumulate in fp32; the term a X of
- * the first three steps carries 22 bits or more.  Five usual steps end 2e-3 of the result from the exact
- * one, of which 1.7e-3 is the final rounding to BF16.  a, b, c finite, |a| <= 16, |b|, |c| <= 32; where they let
+ * The products take fp16 operands (scaled by powers of two) and accumulate in fp32; X is carried in 22 bits or more from step
+ * to step.  Five usual steps end at most 2.7e-3 of the result from the exact one, whatever its spectrum (tested from equal
+ * singular values to one 10^5 times the rest), of which 1.7e-3 is the final rounding to BF16; 6e-3 with fewer than 16 rows or
+ * columns, where single elements' roundings count.  a, b, c finite, |a| <= 16, |b|, |c| <= 32; where they let
  * singular values grow beyond 3, intermediates are cut off at fp16's largest number.  A matrix of zeros gives zeros; one with a
  * non-finite element gives zeros and QESGD_STATUS_NONFINITE, the others of the batch are not
  * touched by it.

@@ -190,7 +190,8 @@ __global__ __launch_bounds__(THREADS) void qesgd_ortho_start_kernel(const T *x, 
 // The three products of a step, C = P Q with fp32 sums in tensor memory, by persistent CTAs (or pairs of them):
 //   GRAM    A = X X^T: both operands are rows of X.  What is off the diagonal goes to F (fp16), the diagonal to d (fp32).
 //   POLY    B = b A + c A A = b (D + F) + c (F F + D F + F D + D D): the product is F F, both operands rows of F (F = F^T).
-//   UPDATE  X' = a X + B X: rows of B's part off the diagonal, and X with the contraction across its rows.
+//   UPDATE  X' = a X + B X: rows of B's part off the diagonal, and X with the contraction across its rows (with `terms` = 2
+//           once for each of X's terms, one after the other).
 // Diagonals stay in fp32 because a matrix with few rows is nearly orthogonal to begin with: then A and B are nearly
 // diagonal, and rounding that to fp16 moves all singular values of a row alike (20 x 2000: 2.4e-3 off instead of 1.0e-3,
 // before the result's own rounding).  A and B are symmetric: tiles below the diagonal are not computed, the ones above
@@ -220,7 +221,7 @@ struct ProductArgs {
     uint32_t tiles_m, tiles;                  // tiles along the rows of one matrix, and of all of it
     __half *mirror;                           // GRAM: F, POLY: B, for the elements below the diagonal
     float *d, *db;                            // diagonals of A and of B
-    uint32_t lo_in, lo_out;                   // UPDATE: whether X and X' have a second term
+    uint32_t terms;                           // of Q: 2 where UPDATE's product takes X's second one too
     __nv_bfloat16 *out;                       // UPDATE: the result, of the last step; else null
     uint64_t ld_a, a_stride, d_stride, ldo, out_stride;
     uint32_t split;                           // CTAs of a cluster that share a tile's contraction, one tile for each cluster
@@ -230,7 +231,7 @@ struct ProductArgs {
 };
 // P and Q; what the end of a tile reads (F, or X and its second term) and writes
 struct ProductMaps {
-    CUtensorMap p, q, in, in_lo, out, out_lo;
+    CUtensorMap p, q, q_lo, in, in_lo, out, out_lo;
     CUtensorMap q_narrow;   // Q of narrow tiles, for the launch to choose
 };
 
@@ -372,15 +373,13 @@ __device__ __forceinline__ void finish(float (&v)[TAKEN], uint32_t batch, uint32
         }
     }
     if (MODE == UPDATE) {
-        if (a.lo_in) {
-            uint4 w[OCTETS];
-            float rest[TAKEN];
+        uint4 w[OCTETS];
+        float rest[TAKEN];
 #pragma unroll
-            for (int i = 0; i < OCTETS; ++i) w[i] = load_shared(box_octet(box + OPERAND_BYTES, r, o + i));
-            halves(w, rest);
+        for (int i = 0; i < OCTETS; ++i) w[i] = load_shared(box_octet(box + OPERAND_BYTES, r, o + i));
+        halves(w, rest);
 #pragma unroll
-            for (int k = 0; k < TAKEN; k += 2) add(in[k], in[k + 1], rest[k], rest[k + 1]);
-        }
+        for (int k = 0; k < TAKEN; k += 2) add(in[k], in[k + 1], rest[k], rest[k + 1]);
         update(v, in, linear);
         if (a.out) {
             __nv_bfloat162 h[TAKEN / 2];
@@ -406,7 +405,7 @@ __device__ __forceinline__ void finish(float (&v)[TAKEN], uint32_t batch, uint32
 #pragma unroll
     for (int i = 0; i < OCTETS; ++i) store_shared(box_octet(box, r, o + i), make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]));
     if (diagonal) clear_half(box, r, o * 8u + row - c);
-    if (MODE == UPDATE && a.lo_out) {
+    if (MODE == UPDATE) {
         uint32_t l[TAKEN / 2];
 #pragma unroll
         for (int k = 0; k < TAKEN / 2; ++k) l[k] = rest_pair(v[2 * k], v[2 * k + 1], h[k]);
@@ -500,7 +499,7 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
     __syncthreads();
     fence_after_sync();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(raw + (slot - smem_u32(raw)));
-    const uint32_t all = a.tiles * a.batch, every = (a.depth + DEPTH - 1) / DEPTH;
+    const uint32_t all = a.tiles * a.batch, once = (a.depth + DEPTH - 1) / DEPTH, every = MODE == UPDATE ? once * a.terms : once;
     const uint32_t step0 = every * part_k / parts, steps = every * (part_k + 1) / parts - step0;
     qesgd_wait_for_previous();
 
@@ -513,13 +512,15 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
             for (uint32_t k = 0; k < steps; ++k, ++n) {
                 const uint32_t s = n % S::STAGES, to = base + s * S::STAGE_BYTES;
                 if (n >= S::STAGES && !pipe_wait(empty + 8 * s, (n / S::STAGES - 1u) & 1u, stop)) break;
-                const uint32_t at = (step0 + k) * DEPTH;
+                const bool second = MODE == UPDATE && step0 + k >= once;   // the contraction over X's second term
+                const uint32_t at = (step0 + k - (second ? once : 0u)) * DEPTH;
                 const bool own = MODE != UPDATE && !x.mirror;   // a square on the diagonal: Q's rows are among P's
                 if (!PAIR || rank == 0) mbar_expect_at(full + 8 * s, (OPERAND_BYTES + (own ? 0u : S::Q_BYTES)) * (PAIR ? 2u : 1u));
                 tma_load_3d<PAIR>(to, &maps.p, at, row, x.batch, full_lead + 8 * s);
                 if (MODE == UPDATE) {
-                    tma_load_3d<PAIR>(to + OPERAND_BYTES, &maps.q, col, at, x.batch, full_lead + 8 * s);
-                    if (!NARROW) tma_load_3d<PAIR>(to + OPERAND_BYTES + OPERAND_BYTES / 2, &maps.q, col + 64u, at, x.batch, full_lead + 8 * s);
+                    const CUtensorMap *const q = second ? &maps.q_lo : &maps.q;
+                    tma_load_3d<PAIR>(to + OPERAND_BYTES, q, col, at, x.batch, full_lead + 8 * s);
+                    if (!NARROW) tma_load_3d<PAIR>(to + OPERAND_BYTES + OPERAND_BYTES / 2, q, col + 64u, at, x.batch, full_lead + 8 * s);
                 } else if (!own) {
                     tma_load_3d<PAIR>(to + OPERAND_BYTES, &maps.q, at, col, x.batch, full_lead + 8 * s);
                 }
@@ -567,10 +568,9 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
                     continue;
                 }
                 const uint32_t col = x.col + b * BOX_COLS, row = x.row + own_rows;
-                const bool lo = MODE == UPDATE && a.lo_in;
-                mbar_expect_at(filled + 8 * s, lo ? 2 * OPERAND_BYTES : OPERAND_BYTES);
+                mbar_expect_at(filled + 8 * s, S::SLOT_BYTES);
                 tma_load_3d<false>(to, &maps.in, col, row, x.batch, filled + 8 * s);
-                if (lo) tma_load_3d<false>(to + OPERAND_BYTES, &maps.in_lo, col, row, x.batch, filled + 8 * s);
+                if (MODE == UPDATE) tma_load_3d<false>(to + OPERAND_BYTES, &maps.in_lo, col, row, x.batch, filled + 8 * s);
             }
         }
         if (*stop) drain();
@@ -592,7 +592,7 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
                     const uint32_t col = x.col + b * BOX_COLS, row = x.row + own_rows;
                     if (store && col < a.cols && row < a.rows) {
                         tma_store_3d(&maps.out, col, row, x.batch, from);
-                        if (MODE == UPDATE && a.lo_out) tma_store_3d(&maps.out_lo, col, row, x.batch, from + OPERAND_BYTES);
+                        if (MODE == UPDATE && !a.out) tma_store_3d(&maps.out_lo, col, row, x.batch, from + OPERAND_BYTES);
                     }
                     store_commit();
                     store_wait_read<0>();
@@ -1191,7 +1191,7 @@ cudaError_t launch_product(const ProductArgs &a, ProductMaps maps, int sm_count,
         const uint64_t m = (a.rows + side - 1) / side, n = (a.cols + side - 1) / side;
         return (MODE == UPDATE ? m * n : m * (m + 1) / 2) * a.batch;
     };
-    const double steps = (a.depth + DEPTH - 1) / DEPTH, sms = sm_count;
+    const double steps = (a.depth + DEPTH - 1) / DEPTH * a.terms, sms = sm_count;
     const double singles = (double)tiles(128), pairs = (double)tiles(256);
     // clocks: a stage of one CTA takes 450 (few CTAs) to 650 (all SMs) to arrive, one of a pair 512 to 690
     const auto stage = [&](double ctas, double few, double many) { return few + (many - few) * (ctas < sms ? ctas / sms : 1.0); };
@@ -1234,14 +1234,15 @@ int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t st
     }
     const OrthoLayout l = qesgd_ortho_layout(a.rows, a.cols, a.batch);
     const auto at = [&](uint64_t off) { return reinterpret_cast<__half *>(a.workspace + off); };
-    CUtensorMap hi[2], lo[2], across[2], f, b, hi_64[2], f_64;   // X by rows and its second term, X across its rows, F, B; 64 rows of them
+    CUtensorMap hi[2], lo[2], across[2], across_lo[2], f, b, hi_64[2], f_64;   // X's terms by rows, and across them, F, B; 64 rows of them
     bool ok = half_map(&f, at(l.off_a), l.m, l.m, l.ld_a, a.batch, l.a_stride, 128) && half_map(&b, at(l.off_b), l.m, l.m, l.ld_a, a.batch, l.a_stride, 128) &&
               half_map(&f_64, at(l.off_a), l.m, l.m, l.ld_a, a.batch, l.a_stride, 64);
     for (int i = 0; i < 2; ++i)
         ok = ok && half_map(&hi[i], at(l.off_hi[i]), l.m, l.n, l.ld_x, a.batch, l.x_stride, 128) &&
              half_map(&hi_64[i], at(l.off_hi[i]), l.m, l.n, l.ld_x, a.batch, l.x_stride, 64) &&
              half_map(&lo[i], at(l.off_lo[i]), l.m, l.n, l.ld_x, a.batch, l.x_stride, 128) &&
-             half_map(&across[i], at(l.off_hi[i]), l.m, l.n, l.ld_x, a.batch, l.x_stride, DEPTH);
+             half_map(&across[i], at(l.off_hi[i]), l.m, l.n, l.ld_x, a.batch, l.x_stride, DEPTH) &&
+             half_map(&across_lo[i], at(l.off_lo[i]), l.m, l.n, l.ld_x, a.batch, l.x_stride, DEPTH);
     if (!ok) return (int)cudaErrorInvalidValue;
     cudaError_t e = a.dtype == QESGD_F32 ? start<float>(a, l, stream) : a.dtype == QESGD_BF16 ? start<__nv_bfloat16>(a, l, stream) : start<__half>(a, l, stream);
     if (e != cudaSuccess) return (int)e;
@@ -1261,18 +1262,18 @@ int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t st
         p.status = a.status;
         p.rows = p.cols = (uint32_t)l.m;
         p.depth = (uint32_t)l.n;
+        p.terms = 1;
         p.mirror = at(l.off_a);
-        e = launch_product<GRAM>(p, {hi[now], hi[now], f, f, f, f, hi_64[now]}, sm_count, stream);
+        e = launch_product<GRAM>(p, {hi[now], hi[now], hi[now], f, f, f, f, hi_64[now]}, sm_count, stream);
         if (e != cudaSuccess) return (int)e;
         *launched += 1;
         p.depth = (uint32_t)l.m;
         p.mirror = at(l.off_b);
-        e = launch_product<POLY>(p, {f, f, f, f, b, b, f_64}, sm_count, stream);
+        e = launch_product<POLY>(p, {f, f, f, f, f, b, b, f_64}, sm_count, stream);
         if (e != cudaSuccess) return (int)e;
         *launched += 1;
         p.cols = (uint32_t)l.n;
-        p.lo_in = step < ORTHO_LO_STEPS;
-        p.lo_out = step + 1 < ORTHO_LO_STEPS && step + 1 < a.steps;
+        p.terms = step < ORTHO_TERMS_STEPS && l.m < ORTHO_TERMS_SIDE ? 2 : 1;
         if (step + 1 == a.steps) {
             p.out = static_cast<__nv_bfloat16 *>(a.out);
             p.ldo = a.ldo;
@@ -1283,7 +1284,7 @@ int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t st
             p.out_tiled = !p.turned && qesgd_aligned(a.out, 16) && a.ldo % 8 == 0 && stride % 8 == 0 &&
                           half_map(&hi[next], a.out, l.m, l.n, a.ldo, a.batch, stride, 128, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16);
         }
-        e = launch_product<UPDATE>(p, {b, across[now], hi[now], lo[now], hi[next], lo[next], across[now]}, sm_count, stream);
+        e = launch_product<UPDATE>(p, {b, across[now], across_lo[now], hi[now], lo[now], hi[next], lo[next], across[now]}, sm_count, stream);
         if (e != cudaSuccess) return (int)e;
         *launched += 1;
     }

@@ -9,11 +9,9 @@
 // start near 1 / n and end near 1 / sqrt(n), those of A near n^-1.5: unscaled they would fall below fp16's normal
 // numbers (6e-5) from n = 128 on.  In magnitude X may reach 255, A 15, B 63.
 constexpr float ORTHO_X_SCALE = 256.0f, ORTHO_A_SCALE = 4096.0f, ORTHO_B_SCALE = 1024.0f;
-// What rounding X to fp16 leaves behind is kept beside X, in fp16 too, for the term a X of the first steps.  There the
-// rounding error of the large singular values is as large as small ones and grows with them: for singular values
-// falling as 1 / i (512 x 512) five steps end 3.3e-3 off without, 1.9e-3 with two steps of it, 1.8e-3 with three (of which
-// 1.7e-3 is the result's rounding to bf16); from the fourth on it gains nothing.
-constexpr uint32_t ORTHO_LO_STEPS = 3;
+// What rounding X to fp16 leaves behind is kept beside X, in fp16 too, for the term a X of every step: the rounding errors of
+// strong directions are as large as weak ones and grow with them.  512 x 512, 16 directions over 10^-4 of them, five steps:
+// 4.4e-2 off without (before the result's rounding), 1.1e-2 with it in two steps, 2.7e-3 in three, 1.2e-3 in four, 8.5e-4 in all.
 // Where singular values lie far apart, B X takes both terms of X in the first steps.  What rounding X to one term leaves
 // behind are new directions, as large as weak ones: |b s^2 + c s^4| = 2.8 times them enters X', and each later step enlarges
 // it by 3.4.  (B's own rounding only mixes the rows that X has: a second term of B changes nothing.)  Five steps, worst of 1 to
@@ -21,6 +19,10 @@ constexpr uint32_t ORTHO_LO_STEPS = 3;
 // in the first step, 3e-3 in two steps, 1e-3 in three; 64 x 1000 8e-3, 4e-3, 3e-3, 1e-3; 128 x 128 4e-3, 2e-3, 2e-3, 1e-3.
 // Both terms in all steps gain nothing on three.
 constexpr uint32_t ORTHO_TERMS_STEPS = 3;
+// Products of their own (more than 128 rows) take one term where the smaller side has at least this many: the errors fall
+// with its square root, 4e-3 at 129, 3e-3 at 256, 1.9e-3 at 512, 1.4e-3 at 1024, against 1e-3 to 1.3e-3 with both terms, and a second
+// term doubles an update's contraction.
+constexpr uint32_t ORTHO_TERMS_SIDE = 512;
 
 struct OrthoView {
     __half *hi, *lo;

@@ -60,7 +60,7 @@ def _strong(rows, cols, strong, rest, seed):
 def _spectra(rows, cols):
     k = min(rows, cols)
     return torch.stack([_strong(rows, cols, r, rest, 7 * i + r)
-                        for r in sorted({1, 4, 16, k // 4, k // 2}) if 2 * r <= k
+                        for r in sorted({1, 4, 16, k // 4, k // 2}) if 0 < 2 * r <= k
                         for i, rest in enumerate((1e-1, 1e-2, 1e-3, 1e-5))])
 
 
@@ -73,3 +73,32 @@ def test_far_singular_values_in_one_kernel(rows, cols):
         off = _off(_orthogonalize(part), _exact(part))
         assert max(off) <= WIDE_TOLERANCE, off
     assert G.ctx().qesgd_status() == 0
+
+
+@pytest.mark.parametrize("rows,cols", [(2, 3), (4, 16), (8, 8), (100, 8), (12, 300)])
+def test_far_singular_values_of_few_rows(rows, cols):
+    """So few elements that the result's rounding may be near its most, 2^-8, in the ones that count."""
+    x = _spectra(rows, cols)
+    off = _off(_orthogonalize(x), _exact(x))
+    assert max(off) <= 2.0 ** -8 + np.sqrt(5.0) * STEP, off
+    assert G.ctx().qesgd_status() == 0
+
+
+@pytest.mark.parametrize("rows,cols", [(129, 130), (129, 1000), (1000, 200), (256, 512), (300, 1500), (500, 500), (512, 512), (512, 2048), (700, 700)])
+def test_far_singular_values_in_products_of_their_own(rows, cols):
+    for x in _spectra(rows, cols):
+        off = _off(_orthogonalize(x[None]), _exact(x[None]))
+        assert max(off) <= WIDE_TOLERANCE, off
+    x = _spectra(rows, cols)[::5][:4].contiguous()                # and as a batch
+    off = _off(_orthogonalize(x), _exact(x))
+    assert max(off) <= WIDE_TOLERANCE, off
+    assert G.ctx().qesgd_status() == 0
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 6, 9])
+@pytest.mark.parametrize("rows,cols", [(60, 200), (140, 400), (600, 700)])
+def test_far_singular_values_after_other_numbers_of_steps(rows, cols, steps):
+    """X's second term and the products that take it, from the first step to behind the third."""
+    x = _strong(rows, cols, 4, 1e-3, steps)[None]
+    off = _off(_orthogonalize(x, steps), _exact(x, steps))
+    assert max(off) <= float(np.hypot(ROUNDING, np.sqrt(steps) * STEP)), off
