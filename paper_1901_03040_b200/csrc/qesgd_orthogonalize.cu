@@ -399,6 +399,10 @@ __device__ __forceinline__ void finish(float (&v)[TAKEN], uint32_t batch, uint32
             return;
         }
     }
+    if (MODE == UPDATE) {   // both terms together are cut off where one alone would be
+#pragma unroll
+        for (int k = 0; k < TAKEN; ++k) v[k] = cut_off(v[k]);
+    }
     uint32_t h[TAKEN / 2];
 #pragma unroll
     for (int k = 0; k < TAKEN / 2; ++k) h[k] = half_pair(v[2 * k], v[2 * k + 1]);

@@ -102,3 +102,35 @@ def test_far_singular_values_after_other_numbers_of_steps(rows, cols, steps):
     x = _strong(rows, cols, 4, 1e-3, steps)[None]
     off = _off(_orthogonalize(x, steps), _exact(x, steps))
     assert max(off) <= float(np.hypot(ROUNDING, np.sqrt(steps) * STEP)), off
+
+
+@pytest.mark.parametrize("steps", [3, 4])
+@pytest.mark.parametrize("rows,cols", [(100, 300), (128, 2000), (129, 200), (300, 200), (200, 1030), (140, 4200)])
+def test_what_is_kept_between_steps_is_cut_off(rows, cols, steps):
+    """One element to a row, each in a column of its own: rows stay apart, and x' = x (a + b x^2 + c x^4) for each, cut off at
+    65504 / 256 between steps.  With a, b, c > 0 a relative error of x enters x' at most fivefold, and x^4 is that of the
+    fp16 operand, whose rounding, 2^-11, counts four times: e' <= 5 e + 2^-9.  Cut off after the second or third step, where it is
+    exact, an element has the last step's error, or the last two's: 6 * 2^-9, and 2^-8 for the result's rounding."""
+    k = min(rows, cols)
+    v = torch.linspace(0.5, 1.5, k, dtype=torch.float32)
+    x = torch.zeros((2, rows, cols))
+    at = torch.arange(k) * (cols // k if rows <= cols else 1)
+    if rows <= cols:
+        x[:, torch.arange(k), at] = v
+    else:
+        x[:, torch.arange(k) * (rows // k), torch.arange(k)] = v
+    a, b, c = 16.0, 32.0, 32.0
+    got = _orthogonalize(x.cuda(), steps, a=a, b=b, c=c).cpu().double()
+    kept = x.double() / torch.linalg.matrix_norm(x.double(), keepdim=True)
+    most = 65504.0 / 256.0
+    cut = torch.zeros_like(kept, dtype=torch.bool)
+    for step in range(steps):
+        kept = kept * (a + b * kept ** 2 + c * kept ** 4)
+        if step + 1 < steps:
+            cut |= kept.abs() > most
+            kept = kept.clamp(-most, most)
+    assert cut.any()
+    off = ((got - kept).abs() / kept.abs().clamp_min(1e-30))[cut]
+    assert float(off.max()) <= 6 * 2.0 ** -9 + 2.0 ** -8, float(off.max())
+    assert (got[x == 0] == 0).all()
+    assert G.ctx().qesgd_status() == 0
