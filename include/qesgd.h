@@ -31,7 +31,10 @@
  *     operators do nothing but launch kernels (or set memory) on that stream, so they may be recorded by CUDA stream capture
  *     and replayed as a graph (worth it when a launch is as short as a host call).
  *   - Return value: QESGD_OK or a negative error code.  Nothing is enqueued
- *     when an error is returned.  No call aborts or throws.
+ *     when arguments are refused, or when the first of a call's kernels cannot be
+ *     launched; where the device or the driver refuses a later one of several
+ *     (QESGD_ECUDA), the ones before it stay enqueued, and qesgd_launch_count
+ *     counts them.  No call aborts or throws.
  *   - Data problems (a non-finite value in a bucket) never fail a call: the
  *     bucket is encoded as scale 0 / codes 0 and QESGD_STATUS_NONFINITE is set
  *     in the context's status word, read with qesgd_status.

@@ -472,11 +472,11 @@ int launch(const Fp4MatmulArgs &a, uint32_t format, int sm_count, cudaStream_t s
 
 int qesgd_launch_fp4_matmul(const Fp4MatmulArgs &a, uint32_t dtype, uint32_t format, int sm_count, cudaStream_t stream, int *launched)
 {
-    *launched = 1;
-    if (a.K == 0) return (int)(dtype == QESGD_F32 ? launch_zeros<uint32_t>(a, stream) : launch_zeros<uint16_t>(a, stream));
-    switch (dtype) {
-        case QESGD_F32: return launch<float>(a, format, sm_count, stream);
-        case QESGD_BF16: return launch<__nv_bfloat16>(a, format, sm_count, stream);
-        default: return launch<__half>(a, format, sm_count, stream);
-    }
+    int e;
+    if (a.K == 0) e = (int)(dtype == QESGD_F32 ? launch_zeros<uint32_t>(a, stream) : launch_zeros<uint16_t>(a, stream));
+    else if (dtype == QESGD_F32) e = launch<float>(a, format, sm_count, stream);
+    else if (dtype == QESGD_BF16) e = launch<__nv_bfloat16>(a, format, sm_count, stream);
+    else e = launch<__half>(a, format, sm_count, stream);
+    *launched = e == 0 ? 1 : 0;
+    return e;
 }

@@ -1113,7 +1113,7 @@ bool takes_whole(uint64_t m, uint64_t n, uint64_t batch)
     return batch <= 2 * qesgd_active_clusters(known, kernel, WHOLE_THREADS, WHOLE_MOST_SMEM, cluster);
 }
 template <typename T>
-cudaError_t launch_whole(const OrthoArgs &o, cudaStream_t stream)
+cudaError_t launch_whole(const OrthoArgs &o, cudaStream_t stream, int *launched)
 {
     WholeArgs a = {};
     a.x = o.x;
@@ -1141,13 +1141,15 @@ cudaError_t launch_whole(const OrthoArgs &o, cudaStream_t stream)
     if (smem < WHOLE_MIN_SMEM) smem = WHOLE_MIN_SMEM;
     const auto kernel = cluster > 1 ? qesgd_ortho_whole_kernel<T, true> : qesgd_ortho_whole_kernel<T, false>;
     static std::atomic<uint64_t> told[2];
-    const cudaError_t e = qesgd_prepare(told[cluster > 1], (const void *)kernel, WHOLE_MOST_SMEM, cluster > 1);
+    cudaError_t e = qesgd_prepare(told[cluster > 1], (const void *)kernel, WHOLE_MOST_SMEM, cluster > 1);
     if (e != cudaSuccess) return e;
-    return qesgd_launch_cluster(kernel, dim3(cluster, (unsigned)o.batch), dim3(WHOLE_THREADS), smem, cluster, stream, a);
+    e = qesgd_launch_cluster(kernel, dim3(cluster, (unsigned)o.batch), dim3(WHOLE_THREADS), smem, cluster, stream, a);
+    if (e == cudaSuccess) *launched = 1;
+    return e;
 }
 
 template <typename T>
-cudaError_t start(const OrthoArgs &a, const OrthoLayout &l, cudaStream_t stream)
+cudaError_t start(const OrthoArgs &a, const OrthoLayout &l, cudaStream_t stream, int *launched)
 {
     const T *const x = static_cast<const T *>(a.x);
     const bool vec = qesgd_aligned(x, 16) && a.ldx * sizeof(T) % 16 == 0 && a.x_stride * sizeof(T) % 16 == 0;
@@ -1156,10 +1158,13 @@ cudaError_t start(const OrthoArgs &a, const OrthoLayout &l, cudaStream_t stream)
     double *const parts = reinterpret_cast<double *>(a.workspace);
     cudaError_t e = qesgd_launch(qesgd_ortho_norm_kernel<T>, grid, dim3(THREADS), stream, x, rows, cols, a.ldx, a.x_stride, vec, parts);
     if (e != cudaSuccess) return e;
+    *launched += 1;
     const OrthoView v = {reinterpret_cast<__half *>(a.workspace + l.off_hi[0]), reinterpret_cast<__half *>(a.workspace + l.off_lo[0]), l.ld_x, l.x_stride};
     const dim3 squares((unsigned)(qesgd_div_up(rows, 64) * qesgd_div_up(cols, 64)), (unsigned)a.batch);
-    return qesgd_launch(rows > cols ? qesgd_ortho_start_kernel<T, true> : qesgd_ortho_start_kernel<T, false>, rows > cols ? squares : grid, dim3(THREADS), stream, x, rows, cols,
-                        a.ldx, a.x_stride, vec, (const double *)parts, l.parts, v, a.status);
+    e = qesgd_launch(rows > cols ? qesgd_ortho_start_kernel<T, true> : qesgd_ortho_start_kernel<T, false>, rows > cols ? squares : grid, dim3(THREADS), stream, x, rows, cols,
+                     a.ldx, a.x_stride, vec, (const double *)parts, l.parts, v, a.status);
+    if (e == cudaSuccess) *launched += 1;
+    return e;
 }
 
 // 16-bit matrices [batch][rows][ld] of `cols` columns; a box is 64 columns of `box_rows` rows, 128-byte rows swizzled.
@@ -1173,23 +1178,27 @@ bool half_map(CUtensorMap *map, const void *p, uint64_t rows, uint64_t cols, uin
                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int MODE, bool PAIR, bool DEEP, bool NARROW>
-cudaError_t launch_product(ProductArgs a, const ProductMaps &maps, uint32_t split, int sm_count, cudaStream_t stream)
+// How a product is launched: by single CTAs, of which 1, 2 or 4 share a contraction, by ones with narrow tiles, by pairs, or by pairs with
+// the deep ring.
+enum ProductShape : uint32_t { SINGLES = 1, SHARED_BY_2 = 2, SHARED_BY_4 = 4, NARROW_TILES = 8, PAIRS = 16, DEEP_PAIRS = 17 };
+
+// f with the kernel of a shape, as an instance of Kernel.
+template <int MODE_, bool PAIR_, bool DEEP_, bool NARROW_>
+struct Kernel {
+    static constexpr int MODE = MODE_;
+    static constexpr bool PAIR = PAIR_, DEEP = DEEP_, NARROW = NARROW_;
+};
+template <int MODE, typename F>
+cudaError_t with_kernel(uint32_t shape, const F &f)
 {
-    using S = Shape<MODE, PAIR, DEEP, NARROW>;
-    const auto kernel = qesgd_ortho_product_kernel<MODE, PAIR, DEEP, NARROW>;
-    a.tiles_m = (a.rows + S::SIDE - 1) / S::SIDE;
-    a.tiles = MODE == UPDATE ? a.tiles_m * ((a.cols + S::WIDTH - 1) / S::WIDTH) : a.tiles_m * (a.tiles_m + 1) / 2 * (S::SIDE / S::WIDTH);
-    a.split = split;
-    static std::atomic<uint64_t> told{0};
-    const cudaError_t e = qesgd_prepare(told, (const void *)kernel, S::SMEM, false);
-    if (e != cudaSuccess) return e;
-    const uint32_t share = PAIR ? 2u : split, all = a.tiles * a.batch, most = (uint32_t)sm_count / share;
-    return qesgd_launch_cluster(kernel, dim3((split > 1 || all < most ? all : most) * share), dim3(WARPS * 32), S::SMEM, share, stream, a, maps);
+    if (shape == NARROW_TILES) return f(Kernel<MODE, false, false, true>());
+    if (shape == PAIRS) return f(Kernel<MODE, true, false, false>());
+    if (shape == DEEP_PAIRS) return f(Kernel<MODE, true, MODE == UPDATE, false>());
+    return f(Kernel<MODE, false, false, false>());
 }
-// Pairs or single CTAs, and how many CTAs share a contraction: by modelled time.
+// Chooses the shape by modelled time, and tells its kernel what it needs.  Nothing is enqueued.
 template <int MODE>
-cudaError_t launch_product(const ProductArgs &a, ProductMaps maps, int sm_count, cudaStream_t stream)
+cudaError_t plan_product(const ProductArgs &a, int sm_count, uint32_t &shape)
 {
     const auto tiles = [&](uint64_t side) {
         const uint64_t m = (a.rows + side - 1) / side, n = (a.cols + side - 1) / side;
@@ -1201,7 +1210,7 @@ cudaError_t launch_product(const ProductArgs &a, ProductMaps maps, int sm_count,
     const auto stage = [&](double ctas, double few, double many) { return few + (many - few) * (ctas < sms ? ctas / sms : 1.0); };
     const auto waves = [&](double n, double most) { return (double)(uint64_t)((n + most - 1) / most); };
     double best = waves(pairs, (double)(sm_count / 2)) * steps * stage(2 * pairs, 512, 690) + 5000;
-    uint32_t split = 0;
+    shape = MODE == UPDATE && a.depth >= 2048 ? DEEP_PAIRS : PAIRS;
     for (uint32_t s = 1; s <= 4; s *= 2) {
         if (s > 1 && (singles * s > sms || steps < 4 * s)) break;
         static QesgdClusters known;
@@ -1213,29 +1222,43 @@ cudaError_t launch_product(const ProductArgs &a, ProductMaps maps, int sm_count,
         const double t = waves(singles, active) * (double)(uint64_t)((steps + s - 1) / s) * stage(singles * s, 450, 650) + 2500 + (s > 1 ? 2000 : 0);
         if (t < best) {
             best = t;
-            split = s;
+            shape = s;
         }
     }
     // narrow tiles: 350 to 500 clocks a stage, and 1200 less at the end
     const double strips = MODE == UPDATE ? (double)(((uint64_t)a.rows + 127) / 128 * ((a.cols + 63) / 64) * a.batch) : 2 * singles;
-    const bool narrow = waves(strips, sms) * steps * stage(strips, 350, 500) + 1300 < best;
-    if (narrow) {
-        if (MODE != UPDATE) maps.q = maps.q_narrow;
-        return launch_product<MODE, false, false, true>(a, maps, 1, sm_count, stream);
-    }
-    if (split != 0) return launch_product<MODE, false, false, false>(a, maps, split, sm_count, stream);
-    if (MODE == UPDATE && a.depth >= 2048) return launch_product<MODE, true, MODE == UPDATE, false>(a, maps, 1, sm_count, stream);
-    return launch_product<MODE, true, false, false>(a, maps, 1, sm_count, stream);
+    if (waves(strips, sms) * steps * stage(strips, 350, 500) + 1300 < best) shape = NARROW_TILES;
+    return with_kernel<MODE>(shape, [](auto k) {
+        using K = decltype(k);
+        static std::atomic<uint64_t> told{0};
+        return qesgd_prepare(told, (const void *)qesgd_ortho_product_kernel<MODE, K::PAIR, K::DEEP, K::NARROW>, Shape<MODE, K::PAIR, K::DEEP, K::NARROW>::SMEM, false);
+    });
+}
+template <int MODE>
+cudaError_t launch_product(ProductArgs a, ProductMaps maps, uint32_t shape, int sm_count, cudaStream_t stream)
+{
+    return with_kernel<MODE>(shape, [&](auto k) {
+        using K = decltype(k);
+        using S = Shape<MODE, K::PAIR, K::DEEP, K::NARROW>;
+        if (K::NARROW && MODE != UPDATE) maps.q = maps.q_narrow;
+        a.tiles_m = (a.rows + S::SIDE - 1) / S::SIDE;
+        a.tiles = MODE == UPDATE ? a.tiles_m * ((a.cols + S::WIDTH - 1) / S::WIDTH) : a.tiles_m * (a.tiles_m + 1) / 2 * (S::SIDE / S::WIDTH);
+        a.split = K::PAIR || K::NARROW ? 1u : shape;
+        const uint32_t share = K::PAIR ? 2u : a.split, all = a.tiles * a.batch, most = (uint32_t)sm_count / share;
+        return qesgd_launch_cluster(qesgd_ortho_product_kernel<MODE, K::PAIR, K::DEEP, K::NARROW>, dim3((a.split > 1 || all < most ? all : most) * share), dim3(WARPS * 32),
+                                    S::SMEM, share, stream, a, maps);
+    });
 }
 
 }  // namespace
 
 int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t stream, int *launched)
 {
-    if (takes_whole(a.rows < a.cols ? a.rows : a.cols, a.rows < a.cols ? a.cols : a.rows, a.batch)) {
-        *launched = 1;
-        return (int)(a.dtype == QESGD_F32 ? launch_whole<float>(a, stream) : a.dtype == QESGD_BF16 ? launch_whole<__nv_bfloat16>(a, stream) : launch_whole<__half>(a, stream));
-    }
+    *launched = 0;
+    if (takes_whole(a.rows < a.cols ? a.rows : a.cols, a.rows < a.cols ? a.cols : a.rows, a.batch))
+        return (int)(a.dtype == QESGD_F32    ? launch_whole<float>(a, stream, launched)
+                     : a.dtype == QESGD_BF16 ? launch_whole<__nv_bfloat16>(a, stream, launched)
+                                             : launch_whole<__half>(a, stream, launched));
     const OrthoLayout l = qesgd_ortho_layout(a.rows, a.cols, a.batch);
     const auto at = [&](uint64_t off) { return reinterpret_cast<__half *>(a.workspace + off); };
     CUtensorMap hi[2], lo[2], across[2], across_lo[2], f, b, hi_64[2], f_64;   // X's terms by rows, and across them, F, B; 64 rows of them
@@ -1248,36 +1271,47 @@ int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t st
              half_map(&across[i], at(l.off_hi[i]), l.m, l.n, l.ld_x, a.batch, l.x_stride, DEPTH) &&
              half_map(&across_lo[i], at(l.off_lo[i]), l.m, l.n, l.ld_x, a.batch, l.x_stride, DEPTH);
     if (!ok) return (int)cudaErrorInvalidValue;
-    cudaError_t e = a.dtype == QESGD_F32 ? start<float>(a, l, stream) : a.dtype == QESGD_BF16 ? start<__nv_bfloat16>(a, l, stream) : start<__half>(a, l, stream);
+    ProductArgs gram = {};
+    gram.batch = (uint32_t)a.batch;
+    gram.d = reinterpret_cast<float *>(a.workspace + l.off_d);
+    gram.db = gram.d + a.batch * l.d_stride;
+    gram.ld_a = l.ld_a;
+    gram.a_stride = l.a_stride;
+    gram.d_stride = l.d_stride;
+    gram.ca = a.a;
+    gram.cb = a.b;
+    gram.cc = a.c;
+    gram.status = a.status;
+    gram.rows = gram.cols = (uint32_t)l.m;
+    gram.depth = (uint32_t)l.n;
+    gram.terms = 1;
+    gram.mirror = at(l.off_a);
+    ProductArgs poly = gram, update[2];   // an update of one term of X, and of both
+    poly.depth = (uint32_t)l.m;
+    poly.mirror = at(l.off_b);
+    update[0] = poly;
+    update[0].cols = (uint32_t)l.n;
+    update[1] = update[0];
+    update[1].terms = 2;
+    const uint32_t both = l.m < ORTHO_TERMS_SIDE ? ORTHO_TERMS_STEPS : 0;   // steps whose update takes both
+    uint32_t by_gram, by_poly, by_update[2] = {0, 0};
+    cudaError_t e = plan_product<GRAM>(gram, sm_count, by_gram);
+    if (e == cudaSuccess) e = plan_product<POLY>(poly, sm_count, by_poly);
+    if (e == cudaSuccess && both < a.steps) e = plan_product<UPDATE>(update[0], sm_count, by_update[0]);
+    if (e == cudaSuccess && both > 0) e = plan_product<UPDATE>(update[1], sm_count, by_update[1]);
     if (e != cudaSuccess) return (int)e;
-    *launched = 2;
+
+    e = a.dtype == QESGD_F32 ? start<float>(a, l, stream, launched) : a.dtype == QESGD_BF16 ? start<__nv_bfloat16>(a, l, stream, launched) : start<__half>(a, l, stream, launched);
+    if (e != cudaSuccess) return (int)e;
     for (uint32_t step = 0; step < a.steps; ++step) {
         const uint32_t now = step % 2, next = 1 - now;
-        ProductArgs p = {};
-        p.batch = (uint32_t)a.batch;
-        p.d = reinterpret_cast<float *>(a.workspace + l.off_d);
-        p.db = p.d + a.batch * l.d_stride;
-        p.ld_a = l.ld_a;
-        p.a_stride = l.a_stride;
-        p.d_stride = l.d_stride;
-        p.ca = a.a;
-        p.cb = a.b;
-        p.cc = a.c;
-        p.status = a.status;
-        p.rows = p.cols = (uint32_t)l.m;
-        p.depth = (uint32_t)l.n;
-        p.terms = 1;
-        p.mirror = at(l.off_a);
-        e = launch_product<GRAM>(p, {hi[now], hi[now], hi[now], f, f, f, f, hi_64[now]}, sm_count, stream);
+        e = launch_product<GRAM>(gram, {hi[now], hi[now], hi[now], f, f, f, f, hi_64[now]}, by_gram, sm_count, stream);
         if (e != cudaSuccess) return (int)e;
         *launched += 1;
-        p.depth = (uint32_t)l.m;
-        p.mirror = at(l.off_b);
-        e = launch_product<POLY>(p, {f, f, f, f, f, b, b, f_64}, sm_count, stream);
+        e = launch_product<POLY>(poly, {f, f, f, f, f, b, b, f_64}, by_poly, sm_count, stream);
         if (e != cudaSuccess) return (int)e;
         *launched += 1;
-        p.cols = (uint32_t)l.n;
-        p.terms = step < ORTHO_TERMS_STEPS && l.m < ORTHO_TERMS_SIDE ? 2 : 1;
+        ProductArgs p = update[step < both];
         if (step + 1 == a.steps) {
             p.out = static_cast<__nv_bfloat16 *>(a.out);
             p.ldo = a.ldo;
@@ -1288,7 +1322,7 @@ int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t st
             p.out_tiled = !p.turned && qesgd_aligned(a.out, 16) && a.ldo % 8 == 0 && stride % 8 == 0 &&
                           half_map(&hi[next], a.out, l.m, l.n, a.ldo, a.batch, stride, 128, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16);
         }
-        e = launch_product<UPDATE>(p, {b, across[now], across_lo[now], hi[now], lo[now], hi[next], lo[next], across[now]}, sm_count, stream);
+        e = launch_product<UPDATE>(p, {b, across[now], across_lo[now], hi[now], lo[now], hi[next], lo[next], across[now]}, by_update[step < both], sm_count, stream);
         if (e != cudaSuccess) return (int)e;
         *launched += 1;
     }
