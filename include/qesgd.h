@@ -297,6 +297,21 @@ int qesgd_debug_drop_signal(qesgd_ctx *ctx, int64_t cta);
 #define QESGD_LR_GROUP 3u      /* a group of a cooperative grid for each worker, minibatches in registers */
 #define QESGD_LR_PLAIN 4u      /* one minibatch by a grid that is launched plainly */
 int qesgd_debug_lr_plan(const qesgd_ctx *ctx, uint32_t plan[8]);
+/* The same for the context's last quantisation, 4-bit product or orthogonalisation.  plan[0] is one of QESGD_MATRIX_* (0 before
+ * the first, or for a product over nothing); then, what does not apply being 0,
+ *   QUANTIZE_ROWS       [1] rows of a tile
+ *   PRODUCT_SINGLES     [1] CTAs that share a contraction, [2] rows of A of a tile
+ *   ORTHO_WHOLE         [1] CTAs of a matrix
+ *   ORTHO_PRODUCTS      shapes of the three products: [1] X X^T, [2] b A + c A A, [3] the update that takes both terms of X, [4] that of
+ *                       one term; 1, 2, 4 = CTAs that share a contraction, 8 = narrow tiles, 16 = pairs of SMs, 17 = pairs with the
+ *                       deep ring; 0 = not called for */
+#define QESGD_MATRIX_QUANTIZE_ROWS 1u    /* blocks along rows alone */
+#define QESGD_MATRIX_QUANTIZE_COLUMNS 2u /* along columns, or both */
+#define QESGD_MATRIX_PRODUCT_SINGLES 3u
+#define QESGD_MATRIX_PRODUCT_PAIRS 4u
+#define QESGD_MATRIX_ORTHO_WHOLE 5u      /* all steps in one kernel */
+#define QESGD_MATRIX_ORTHO_PRODUCTS 6u   /* three products a step */
+int qesgd_debug_matrix_plan(const qesgd_ctx *ctx, uint32_t plan[8]);
 
 /*
  * The paper has no counterpart for this entry point; it exists for callers that are

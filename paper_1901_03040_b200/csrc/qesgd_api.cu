@@ -52,6 +52,7 @@ int qesgd_create(qesgd_ctx **out, int device, void *cuda_stream)
     ctx->wait_ns = QESGD_DEFAULT_WAIT_NS;
     ctx->drop_cta = 0xFFFFFFFFu;
     for (uint32_t &v : ctx->lr_plan) v = 0u;
+    for (uint32_t &v : ctx->matrix_plan) v = 0u;
     DeviceGuard guard(device);
     if (!guard.ok) { delete ctx; return QESGD_ECUDA; }
     cudaError_t e = cudaMalloc((void **)&ctx->d_status, 256);
@@ -112,6 +113,13 @@ int qesgd_debug_lr_plan(const qesgd_ctx *ctx, uint32_t plan[8])
 {
     if (!ctx || !plan) return QESGD_EINVAL;
     for (int i = 0; i < 8; ++i) plan[i] = ctx->lr_plan[i];
+    return QESGD_OK;
+}
+
+int qesgd_debug_matrix_plan(const qesgd_ctx *ctx, uint32_t plan[8])
+{
+    if (!ctx || !plan) return QESGD_EINVAL;
+    for (int i = 0; i < 8; ++i) plan[i] = ctx->matrix_plan[i];
     return QESGD_OK;
 }
 

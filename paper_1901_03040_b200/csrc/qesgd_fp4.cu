@@ -578,17 +578,20 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_tensor_exponent_kernel(cons
 }
 
 template <typename T, int FORMAT, bool SCALED, bool STOCHASTIC>
-cudaError_t launch_quantize(const Fp4QuantizeArgs &a, int sm_count, cudaStream_t stream)
+cudaError_t launch_quantize(const Fp4QuantizeArgs &a, int sm_count, cudaStream_t stream, uint32_t *plan)
 {
     const auto grid_of = [](uint64_t tiles) { return dim3((unsigned)(tiles < 0x7FFFFFFF ? tiles : 0x7FFFFFFF)); };
     if (!a.codes_t) {
         // Tiles of 32 rows where those of 64 would all run at once (four to an SM), so that they spread evenly: 64 x 65536
         // fp32 with draws and back 10.2 us in place of 12.5, 512 x 4096 6.6 in place of 7.0, but 4096 x 4096 28.7 in place of 27.1.
         const uint64_t halves = qesgd_div_up(a.rows, TILE_ROWS) * 2 * qesgd_div_up(a.cols, ROW_COLS);
-        return halves <= 4 * (uint64_t)sm_count
+        plan[0] = QESGD_MATRIX_QUANTIZE_ROWS;
+        plan[1] = halves <= 4 * (uint64_t)sm_count ? 32 : 64;
+        return plan[1] == 32
                    ? qesgd_launch(qesgd_fp4_quantize_rows_kernel<T, FORMAT, SCALED, STOCHASTIC, 32>, grid_of(2 * halves), dim3(THREADS), stream, a)
                    : qesgd_launch(qesgd_fp4_quantize_rows_kernel<T, FORMAT, SCALED, STOCHASTIC, 64>, grid_of(halves), dim3(THREADS), stream, a);
     }
+    plan[0] = QESGD_MATRIX_QUANTIZE_COLUMNS;
     const dim3 grid = grid_of(qesgd_div_up(a.rows, TILE_ROWS) * qesgd_div_up(a.cols, SIDE));
     const auto kernel = qesgd_fp4_quantize_columns_kernel<T, FORMAT, SCALED, STOCHASTIC>;
     const int smem = SIDE * SIDE * (int)sizeof(T);
@@ -597,15 +600,15 @@ cudaError_t launch_quantize(const Fp4QuantizeArgs &a, int sm_count, cudaStream_t
     return e != cudaSuccess ? e : qesgd_launch_smem(kernel, grid, dim3(THREADS), smem, stream, a);
 }
 template <typename T, bool STOCHASTIC>
-cudaError_t launch_quantize(const Fp4QuantizeArgs &a, uint32_t format, int sm_count, cudaStream_t stream)
+cudaError_t launch_quantize(const Fp4QuantizeArgs &a, uint32_t format, int sm_count, cudaStream_t stream, uint32_t *plan)
 {
-    if (format == QESGD_FP4_MX) return launch_quantize<T, QESGD_FP4_MX, false, STOCHASTIC>(a, sm_count, stream);
-    return a.tensor_exponent ? launch_quantize<T, QESGD_FP4_NV, true, STOCHASTIC>(a, sm_count, stream) : launch_quantize<T, QESGD_FP4_NV, false, STOCHASTIC>(a, sm_count, stream);
+    if (format == QESGD_FP4_MX) return launch_quantize<T, QESGD_FP4_MX, false, STOCHASTIC>(a, sm_count, stream, plan);
+    return a.tensor_exponent ? launch_quantize<T, QESGD_FP4_NV, true, STOCHASTIC>(a, sm_count, stream, plan) : launch_quantize<T, QESGD_FP4_NV, false, STOCHASTIC>(a, sm_count, stream, plan);
 }
 template <typename T>
-cudaError_t launch_quantize(const Fp4QuantizeArgs &a, uint32_t format, bool stochastic, int sm_count, cudaStream_t stream)
+cudaError_t launch_quantize(const Fp4QuantizeArgs &a, uint32_t format, bool stochastic, int sm_count, cudaStream_t stream, uint32_t *plan)
 {
-    return stochastic ? launch_quantize<T, true>(a, format, sm_count, stream) : launch_quantize<T, false>(a, format, sm_count, stream);
+    return stochastic ? launch_quantize<T, true>(a, format, sm_count, stream, plan) : launch_quantize<T, false>(a, format, sm_count, stream, plan);
 }
 template <typename T, int FORMAT>
 cudaError_t launch_dequantize(const Fp4DequantizeArgs &a, cudaStream_t stream)
@@ -631,12 +634,12 @@ cudaError_t launch_exponent(const void *x, uint64_t rows, uint64_t cols, uint64_
 
 }  // namespace
 
-int qesgd_launch_fp4_quantize(const Fp4QuantizeArgs &a, uint32_t dtype, uint32_t format, bool stochastic, int sm_count, cudaStream_t stream)
+int qesgd_launch_fp4_quantize(const Fp4QuantizeArgs &a, uint32_t dtype, uint32_t format, bool stochastic, int sm_count, cudaStream_t stream, uint32_t *plan)
 {
     switch (dtype) {
-        case QESGD_F32: return (int)launch_quantize<float>(a, format, stochastic, sm_count, stream);
-        case QESGD_BF16: return (int)launch_quantize<__nv_bfloat16>(a, format, stochastic, sm_count, stream);
-        default: return (int)launch_quantize<__half>(a, format, stochastic, sm_count, stream);
+        case QESGD_F32: return (int)launch_quantize<float>(a, format, stochastic, sm_count, stream, plan);
+        case QESGD_BF16: return (int)launch_quantize<__nv_bfloat16>(a, format, stochastic, sm_count, stream, plan);
+        default: return (int)launch_quantize<__half>(a, format, stochastic, sm_count, stream, plan);
     }
 }
 int qesgd_launch_fp4_dequantize(const Fp4DequantizeArgs &a, uint32_t dtype, uint32_t format, cudaStream_t stream)

@@ -431,7 +431,7 @@ int launch(const Fp4MatmulArgs &f, uint32_t q, uint32_t split, int sm_count, cud
 }
 
 template <typename T, bool MX, bool ACCUMULATE>
-int launch(const Fp4MatmulArgs &a, int sm_count, cudaStream_t stream)
+int launch(const Fp4MatmulArgs &a, int sm_count, cudaStream_t stream, uint32_t *plan)
 {
     static QesgdClusters known;
     // By modelled clocks: a stage of a pair takes about 700 to arrive and be multiplied, one of a single CTA 450 where others
@@ -457,26 +457,29 @@ int launch(const Fp4MatmulArgs &a, int sm_count, cudaStream_t stream)
             split = s;
         }
     }
+    plan[0] = by_pairs < best ? QESGD_MATRIX_PRODUCT_PAIRS : QESGD_MATRIX_PRODUCT_SINGLES;
+    plan[1] = by_pairs < best ? 2 : split;
+    plan[2] = by_pairs < best ? 256 : q;
     if (by_pairs < best) return launch<T, true, MX, ACCUMULATE>(a, 256, 1, sm_count, stream);
     return launch<T, false, MX, ACCUMULATE>(a, q, split, sm_count, stream);
 }
 
 template <typename T>
-int launch(const Fp4MatmulArgs &a, uint32_t format, int sm_count, cudaStream_t stream)
+int launch(const Fp4MatmulArgs &a, uint32_t format, int sm_count, cudaStream_t stream, uint32_t *plan)
 {
-    if (format == QESGD_FP4_MX) return a.accumulate ? launch<T, true, true>(a, sm_count, stream) : launch<T, true, false>(a, sm_count, stream);
-    return a.accumulate ? launch<T, false, true>(a, sm_count, stream) : launch<T, false, false>(a, sm_count, stream);
+    if (format == QESGD_FP4_MX) return a.accumulate ? launch<T, true, true>(a, sm_count, stream, plan) : launch<T, true, false>(a, sm_count, stream, plan);
+    return a.accumulate ? launch<T, false, true>(a, sm_count, stream, plan) : launch<T, false, false>(a, sm_count, stream, plan);
 }
 
 }  // namespace
 
-int qesgd_launch_fp4_matmul(const Fp4MatmulArgs &a, uint32_t dtype, uint32_t format, int sm_count, cudaStream_t stream, int *launched)
+int qesgd_launch_fp4_matmul(const Fp4MatmulArgs &a, uint32_t dtype, uint32_t format, int sm_count, cudaStream_t stream, int *launched, uint32_t *plan)
 {
     int e;
     if (a.K == 0) e = (int)(dtype == QESGD_F32 ? launch_zeros<uint32_t>(a, stream) : launch_zeros<uint16_t>(a, stream));
-    else if (dtype == QESGD_F32) e = launch<float>(a, format, sm_count, stream);
-    else if (dtype == QESGD_BF16) e = launch<__nv_bfloat16>(a, format, sm_count, stream);
-    else e = launch<__half>(a, format, sm_count, stream);
+    else if (dtype == QESGD_F32) e = launch<float>(a, format, sm_count, stream, plan);
+    else if (dtype == QESGD_BF16) e = launch<__nv_bfloat16>(a, format, sm_count, stream, plan);
+    else e = launch<__half>(a, format, sm_count, stream, plan);
     *launched = e == 0 ? 1 : 0;
     return e;
 }

@@ -30,6 +30,7 @@ struct qesgd_ctx {
     uint64_t wait_ns;       // limit of each wait inside the local-epoch kernel
     uint32_t drop_cta;      // give-up-path test hook of the local-epoch kernels (none: ~0)
     uint32_t lr_plan[8];    // qesgd_debug_lr_plan
+    uint32_t matrix_plan[8];   // qesgd_debug_matrix_plan
 };
 
 inline bool qesgd_aligned(const void *p, uintptr_t a) { return ((uintptr_t)p % a) == 0; }
@@ -219,10 +220,11 @@ struct OrthoArgs {
 inline uint64_t qesgd_div_up(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 int qesgd_launch_fp4_tensor_exponent(const void *x, uint32_t dtype, uint64_t rows, uint64_t cols, uint64_t ldx, bool vec,
                                      int32_t *out, uint32_t *status, int sm_count, cudaStream_t stream);
-int qesgd_launch_fp4_quantize(const Fp4QuantizeArgs &a, uint32_t dtype, uint32_t format, bool stochastic, int sm_count, cudaStream_t stream);
+// plan: see qesgd_debug_matrix_plan; zeros on entry
+int qesgd_launch_fp4_quantize(const Fp4QuantizeArgs &a, uint32_t dtype, uint32_t format, bool stochastic, int sm_count, cudaStream_t stream, uint32_t *plan);
 int qesgd_launch_fp4_dequantize(const Fp4DequantizeArgs &a, uint32_t dtype, uint32_t format, cudaStream_t stream);
-int qesgd_launch_fp4_matmul(const Fp4MatmulArgs &a, uint32_t dtype, uint32_t format, int sm_count, cudaStream_t stream, int *launched);
-int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t stream, int *launched);
+int qesgd_launch_fp4_matmul(const Fp4MatmulArgs &a, uint32_t dtype, uint32_t format, int sm_count, cudaStream_t stream, int *launched, uint32_t *plan);
+int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t stream, int *launched, uint32_t *plan);
 
 // Launchers.  Return a cudaError_t as int.  qesgd_codec.cu is compiled once per code width
 // and defines the *_2, *_4, *_8 functions; the width-dispatching wrappers are inline here.

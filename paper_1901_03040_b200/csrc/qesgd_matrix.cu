@@ -6,6 +6,18 @@ namespace {
 
 inline uint64_t element_bytes(uint32_t dtype) { return dtype == QESGD_F32 ? 4 : 2; }
 
+// A call's plan becomes the context's where the call went through.
+struct Plan {
+    qesgd_ctx *ctx;
+    uint32_t words[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    int keep(int e)
+    {
+        if (e == 0)
+            for (int i = 0; i < 8; ++i) ctx->matrix_plan[i] = words[i];
+        return e;
+    }
+};
+
 // A matrix of elements: pointer, row stride.  (rows, cols > 0 here.)
 inline bool valid_matrix(const void *p, uint32_t dtype, uint64_t cols, uint64_t ld)
 {
@@ -86,7 +98,8 @@ int qesgd_fp4_quantize(qesgd_ctx *ctx, const void *x, uint32_t dtype, uint64_t r
     a.status = ctx->d_status;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return qesgd_cuda_fail(ctx, (int)cudaErrorInvalidDevice);
-    const int e = qesgd_launch_fp4_quantize(a, dtype, format, rounding == QESGD_ROUND_STOCHASTIC, ctx->sm_count, ctx->stream);
+    Plan plan = {ctx};
+    const int e = plan.keep(qesgd_launch_fp4_quantize(a, dtype, format, rounding == QESGD_ROUND_STOCHASTIC, ctx->sm_count, ctx->stream, plan.words));
     if (e != 0) return qesgd_cuda_fail(ctx, e);
     ctx->launches += 1;
     return QESGD_OK;
@@ -132,7 +145,8 @@ int qesgd_fp4_matmul(qesgd_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_sc
     if (!guard.ok) return qesgd_cuda_fail(ctx, (int)cudaErrorInvalidDevice);
     const Fp4MatmulArgs a = {a_codes, a_scales, b_codes, b_scales, a_exponent, b_exponent, M, N, K, ldc, c, accumulate ? 1u : 0u, ctx->d_status};
     int launched = 0;
-    const int e = qesgd_launch_fp4_matmul(a, dtype, format, ctx->sm_count, ctx->stream, &launched);
+    Plan plan = {ctx};
+    const int e = plan.keep(qesgd_launch_fp4_matmul(a, dtype, format, ctx->sm_count, ctx->stream, &launched, plan.words));
     ctx->launches += (uint64_t)launched;
     if (e != 0) return qesgd_cuda_fail(ctx, e);
     return QESGD_OK;
@@ -163,7 +177,8 @@ int qesgd_orthogonalize(qesgd_ctx *ctx, const void *x, uint32_t dtype, uint64_t 
     const OrthoArgs o = {x, dtype, rows, cols, ldx, batch, batch > 1 ? x_stride : 0, steps, a, b, c, out, ldo,
                          batch > 1 ? out_stride : 0, static_cast<uint8_t *>(workspace), ctx->d_status};
     int launched = 0;
-    const int e = qesgd_launch_orthogonalize(o, ctx->sm_count, ctx->stream, &launched);
+    Plan plan = {ctx};
+    const int e = plan.keep(qesgd_launch_orthogonalize(o, ctx->sm_count, ctx->stream, &launched, plan.words));
     ctx->launches += (uint64_t)launched;
     if (e != 0) return qesgd_cuda_fail(ctx, e);
     return QESGD_OK;

@@ -1113,7 +1113,7 @@ bool takes_whole(uint64_t m, uint64_t n, uint64_t batch)
     return batch <= 2 * qesgd_active_clusters(known, kernel, WHOLE_THREADS, WHOLE_MOST_SMEM, cluster);
 }
 template <typename T>
-cudaError_t launch_whole(const OrthoArgs &o, cudaStream_t stream, int *launched)
+cudaError_t launch_whole(const OrthoArgs &o, cudaStream_t stream, int *launched, uint32_t *plan)
 {
     WholeArgs a = {};
     a.x = o.x;
@@ -1145,6 +1145,8 @@ cudaError_t launch_whole(const OrthoArgs &o, cudaStream_t stream, int *launched)
     if (e != cudaSuccess) return e;
     e = qesgd_launch_cluster(kernel, dim3(cluster, (unsigned)o.batch), dim3(WHOLE_THREADS), smem, cluster, stream, a);
     if (e == cudaSuccess) *launched = 1;
+    plan[0] = QESGD_MATRIX_ORTHO_WHOLE;
+    plan[1] = cluster;
     return e;
 }
 
@@ -1179,7 +1181,7 @@ bool half_map(CUtensorMap *map, const void *p, uint64_t rows, uint64_t cols, uin
 }
 
 // How a product is launched: by single CTAs, of which 1, 2 or 4 share a contraction, by ones with narrow tiles, by pairs, or by pairs with
-// the deep ring.
+// the deep ring.  (qesgd_debug_matrix_plan tells.)
 enum ProductShape : uint32_t { SINGLES = 1, SHARED_BY_2 = 2, SHARED_BY_4 = 4, NARROW_TILES = 8, PAIRS = 16, DEEP_PAIRS = 17 };
 
 // f with the kernel of a shape, as an instance of Kernel.
@@ -1252,13 +1254,13 @@ cudaError_t launch_product(ProductArgs a, ProductMaps maps, uint32_t shape, int 
 
 }  // namespace
 
-int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t stream, int *launched)
+int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t stream, int *launched, uint32_t *plan)
 {
     *launched = 0;
     if (takes_whole(a.rows < a.cols ? a.rows : a.cols, a.rows < a.cols ? a.cols : a.rows, a.batch))
-        return (int)(a.dtype == QESGD_F32    ? launch_whole<float>(a, stream, launched)
-                     : a.dtype == QESGD_BF16 ? launch_whole<__nv_bfloat16>(a, stream, launched)
-                                             : launch_whole<__half>(a, stream, launched));
+        return (int)(a.dtype == QESGD_F32    ? launch_whole<float>(a, stream, launched, plan)
+                     : a.dtype == QESGD_BF16 ? launch_whole<__nv_bfloat16>(a, stream, launched, plan)
+                                             : launch_whole<__half>(a, stream, launched, plan));
     const OrthoLayout l = qesgd_ortho_layout(a.rows, a.cols, a.batch);
     const auto at = [&](uint64_t off) { return reinterpret_cast<__half *>(a.workspace + off); };
     CUtensorMap hi[2], lo[2], across[2], across_lo[2], f, b, hi_64[2], f_64;   // X's terms by rows, and across them, F, B; 64 rows of them
@@ -1300,6 +1302,11 @@ int qesgd_launch_orthogonalize(const OrthoArgs &a, int sm_count, cudaStream_t st
     if (e == cudaSuccess && both < a.steps) e = plan_product<UPDATE>(update[0], sm_count, by_update[0]);
     if (e == cudaSuccess && both > 0) e = plan_product<UPDATE>(update[1], sm_count, by_update[1]);
     if (e != cudaSuccess) return (int)e;
+    plan[0] = QESGD_MATRIX_ORTHO_PRODUCTS;
+    plan[1] = by_gram;
+    plan[2] = by_poly;
+    plan[3] = by_update[1];
+    plan[4] = by_update[0];
 
     e = a.dtype == QESGD_F32 ? start<float>(a, l, stream, launched) : a.dtype == QESGD_BF16 ? start<__nv_bfloat16>(a, l, stream, launched) : start<__half>(a, l, stream, launched);
     if (e != cudaSuccess) return (int)e;

@@ -22,6 +22,8 @@ ROUND_NEAREST, ROUND_STOCHASTIC = 0, 1
 STATUS_NONFINITE = 1
 STATUS_TIMEOUT = 2
 STATUS_RANGE = 4
+(MATRIX_QUANTIZE_ROWS, MATRIX_QUANTIZE_COLUMNS, MATRIX_PRODUCT_SINGLES, MATRIX_PRODUCT_PAIRS, MATRIX_ORTHO_WHOLE,
+ MATRIX_ORTHO_PRODUCTS) = range(1, 7)
 LR_TWO_PASSES, LR_PERSISTENT, LR_CLUSTER, LR_GROUP, LR_PLAIN = range(5)
 OK, EINVAL, ECUDA, ENOMEM, ELIMIT = 0, -1, -2, -3, -4
 MAX_WORKERS, MIN_BUCKET, MAX_BUCKET, MAX_LR_BATCH = 64, 64, 8192, 1024
@@ -44,6 +46,7 @@ SIGNATURES = {
     "qesgd_set_wait_limit": (_int, [_vp, _u64]),
     "qesgd_debug_drop_signal": (_int, [_vp, C.c_int64]),
     "qesgd_debug_lr_plan": (_int, [_vp, C.POINTER(_u32)]),
+    "qesgd_debug_matrix_plan": (_int, [_vp, C.POINTER(_u32)]),
     "qesgd_num_buckets": (_u64, [_u64, _u32]),
     "qesgd_code_bytes": (_u64, [_u64, _u32, _u32]),
     "qesgd_encode": (_int, [_vp, _vp, _vp, _u64, _u32, _u32, _u32, _u32, _f32, _u64, _u32, _u32,
@@ -171,6 +174,12 @@ class Context:
         """How the last local epoch, step or gradient was launched: LR_*, then the seven words that describe it."""
         plan = (_u32 * 8)()
         self._check(lib.qesgd_debug_lr_plan(self._h, plan))
+        return tuple(plan)
+
+    def qesgd_debug_matrix_plan(self):
+        """How the last quantisation, 4-bit product or orthogonalisation was launched: MATRIX_*, then what describes it."""
+        plan = (_u32 * 8)()
+        self._check(lib.qesgd_debug_matrix_plan(self._h, plan))
         return tuple(plan)
 
     # -- worker side ---------------------------------------------------------
