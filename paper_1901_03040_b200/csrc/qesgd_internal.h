@@ -70,18 +70,6 @@ static const uint32_t QESGD_LR_EPOCH_ROWS = 2048;
 static const uint64_t QESGD_LR_EPOCH_FLOATS = QESGD_MAX_WORKERS * 16ull + 8ull * QESGD_LR_EPOCH_ROWS * 14ull;
 static const uint64_t QESGD_LR_WORK_FLOATS = (1ull << 20) - QESGD_LR_EPOCH_FLOATS;
 
-// Kernels that go through qesgd_launch may be set up while the kernel before them in the stream drains
-// (programmatic dependent launch), and begin with qesgd_wait_for_previous: nothing is read or written
-// before that one is done and its writes are visible (qesgd_lr_tile.cu launches its clusters and its grids of one
-// minibatch the same way).  The cooperative local-epoch kernels and the debug build's range self-test do not: they are
-// launched plainly, start when all before them is done and contain
-// no such wait, so they must not be given the attribute without one (in the epoch kernel ahead of the
-// producers' first copy and the consumers' loads of u).  No kernel lets its successor
-// start earlier than at its own end: a waiting grid would take resident slots.  Without the overlap a
-// kernel costs a whole number of about 2.05 us in a stream: encode + decode-average-apply of 4 x 30000
-// 11.3 -> 5.9 us, of 8 x 10^6 18.5 -> 14.4, decode of 2^24 13.9 -> 11.3, a logistic step of 64 x 2^22
-// 319 -> 311, and no grid was found that is slower.  (With griddepcontrol.launch_dependents at the top of
-// every kernel the successor's CTAs come early: 461 instead of 353 us for an encode of 400 000 CTAs.)
 // What a kernel needs to be told once on every device: dynamic shared memory beyond 48 KB, clusters of more than eight CTAs.
 // `told` is one bit for each device; two threads may both tell, to the same effect.
 inline cudaError_t qesgd_prepare(std::atomic<uint64_t> &told, const void *kernel, int smem, bool large_clusters)
@@ -96,6 +84,19 @@ inline cudaError_t qesgd_prepare(std::atomic<uint64_t> &told, const void *kernel
     if (e == cudaSuccess && device < 64) told.fetch_or(bit, std::memory_order_relaxed);
     return e;
 }
+
+// Kernels that go through qesgd_launch may be set up while the kernel before them in the stream drains
+// (programmatic dependent launch), and begin with qesgd_wait_for_previous: nothing is read or written
+// before that one is done and its writes are visible (qesgd_lr_tile.cu launches its clusters and its grids of one
+// minibatch the same way).  The cooperative local-epoch kernels and the debug build's range self-test do not: they are
+// launched plainly, start when all before them is done and contain
+// no such wait, so they must not be given the attribute without one (in the epoch kernel ahead of the
+// producers' first copy and the consumers' loads of u).  No kernel lets its successor
+// start earlier than at its own end: a waiting grid would take resident slots.  Without the overlap a
+// kernel costs a whole number of about 2.05 us in a stream: encode + decode-average-apply of 4 x 30000
+// 11.3 -> 5.9 us, of 8 x 10^6 18.5 -> 14.4, decode of 2^24 13.9 -> 11.3, a logistic step of 64 x 2^22
+// 319 -> 311, and no grid was found that is slower.  (With griddepcontrol.launch_dependents at the top of
+// every kernel the successor's CTAs come early: 461 instead of 353 us for an encode of 400 000 CTAs.)
 template <typename... Params, typename... Args>
 inline cudaError_t qesgd_launch_cluster(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, uint32_t cluster, cudaStream_t stream,
                                         const Args &...args)

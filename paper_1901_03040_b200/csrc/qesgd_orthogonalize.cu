@@ -729,7 +729,7 @@ constexpr uint32_t WHOLE_MIN_SMEM = 120 * 1024;            // one CTA of an SM: 
 
 struct WholeArgs {
     const void *x;
-    uint64_t rows, cols, ldx, x_stride, ldo, out_stride;
+    uint64_t ldx, x_stride, ldo, out_stride;
     uint32_t m, n, width, steps, turned, vec, out_vec;     // width: columns of a CTA
     float ca, cb, cc;
     __nv_bfloat16 *out;
@@ -1117,8 +1117,6 @@ cudaError_t launch_whole(const OrthoArgs &o, cudaStream_t stream, int *launched,
 {
     WholeArgs a = {};
     a.x = o.x;
-    a.rows = o.rows;
-    a.cols = o.cols;
     a.ldx = o.ldx;
     a.x_stride = o.x_stride;
     a.ldo = o.ldo;
