@@ -34,6 +34,8 @@ UNITS = [
     ("qesgd_mma.cu", "qesgd_mma.o", []),
     ("qesgd_matrix.cu", "qesgd_matrix.o", []),
 ]
+# the units that QESGD_DEBUG changes; the debug library shares the other ones' objects
+CHECKED = {"qesgd_codec.cu", "qesgd_api.cu"}
 
 
 def _nvcc():
@@ -62,7 +64,7 @@ def build_py_module(force: bool = False) -> str:
 
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
     """Builds libqesgd.so, or with debug=True libqesgd_debug.so: the same library compiled with
-    -DQESGD_DEBUG (the codec kernels check their indices and set QESGD_STATUS_RANGE)."""
+    -DQESGD_DEBUG (the codec kernels check their indices and set QESGD_STATUS_RANGE; no other unit differs)."""
     os.makedirs(OBJ, exist_ok=True)
     build_py_module(force)
     headers = [os.path.join(CSRC, "qesgd_internal.h"), os.path.join(CSRC, "qesgd_lr_device.cuh"),
@@ -77,7 +79,7 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     lib = LIB_DEBUG if debug else LIB
     for name, objname, extra in UNITS:
         src = os.path.join(CSRC, name)
-        if debug:
+        if debug and name in CHECKED:
             objname, extra = "debug_" + objname, extra + ["-DQESGD_DEBUG"]
         obj = os.path.join(OBJ, objname)
         objs.append(obj)
