@@ -204,10 +204,11 @@ __global__ __launch_bounds__(THREADS) void qesgd_ortho_start_kernel(const T *x, 
 // by the warps themselves, a row for each lane, the update of 12 x 512 x 2048 took 63 us, three times what its products
 // take: 32 rows' segments in one instruction are 32 passes through the load-store unit.)
 //
-// Five steps on 4096 x 8192 take 2.15 ms, 1.1 PFLOP/s: a stage of GRAM or POLY takes 513 clocks of the tensor cores' 512, so
+// Five steps on 4096 x 8192 take 2.2 ms, 1.1 PFLOP/s: a stage of GRAM or POLY takes 513 clocks of the tensor cores' 512, so
 // the clock under the power cap and whole waves of tiles (136 on 74 pairs) bound it.  An update's contraction is as short
 // as the smaller side: at 512 its tiles' ends, which move three terms of X, come to as many bytes of shared memory as its
-// stages.  With few tiles it is the chain of fifteen launches, some 6 to 8 us each (500 x 500: 117 us).
+// stages.  With few tiles it is the chain of fifteen launches, some 6 to 8 us each (500 x 500: 127 us, with three updates' contractions
+// taken twice, once for each term of X, and 118 without).
 enum Product { GRAM, POLY, UPDATE };
 
 constexpr int TAKERS = 16;                    // warps that take tiles out: four for each quarter of tensor memory
@@ -438,8 +439,8 @@ __device__ __forceinline__ void store_rows(uint32_t batch, uint32_t row0, uint32
 }
 
 // DEEP: an update whose contraction is long has five stages, and two slots in the second ring, in place of four and three.
-// Pairs: 4096 x 8192 2062 us in place of 2090 (five steps), 2048 x 2048 338 in place of 360; 12 x 512 x 2048 261 in place of 250,
-// 4 x 1024 x 4096 413 in place of 403: from contractions of 2048 on.
+// Pairs: 4096 x 8192 2.08 ms in place of 2.16 (five steps), 2048 x 2048 260 us in place of 268; 12 x 512 x 2048 293 in place of 284,
+// 4 x 1024 x 4096 398 in place of 394: from contractions of 2048 on.
 // NARROW: a single CTA's tile has 64 columns in place of 128.
 template <int MODE, bool PAIR, bool DEEP, bool NARROW>
 struct Shape {
@@ -715,11 +716,11 @@ __global__ __launch_bounds__(WARPS * 32, 1) void qesgd_ortho_product_kernel(cons
 // the CTAs: each adds up some of its columns, in the order of the CTAs, and writes F's share of them into every CTA.  The
 // fifteen products as kernels of their own take 5 us each here, most of it for starting, waiting for the first copies
 // and storing what the next one loads.
-// 64 x 256 takes 21 us: 3.5 to load and divide by the norm, then 3.1 a step, half of it from a product's first instruction
-// to its sums' arrival (sixteen instructions deep for A), half to take the sums out and settle what the next one reads.
-// Two terms of X in shared memory in place of 32 bits: 21.9, and 25.9 with half of the warps idle at the update's
-// end.  128 x 4096 takes 68 us, half of it for the exchange.  (A begun with the columns that are done, while others are still
-// taken out, made it 21.8 and 72: each part costs one more barrier.)
+// 64 x 256 takes 23 us: 3.5 to load and divide by the norm, then 3.7 for each of the first three steps (3.1 with one term of X) and 3.1
+// for the others, half of it from a product's first instruction to its sums' arrival (sixteen instructions deep for A), half to take
+// the sums out and settle what the next one reads.  128 x 4096 takes 72 us, half of it for the exchange.  With one term of X in all
+// steps (21 and 70): X as two terms in shared memory in place of 32 bits 1 us slower, half of the warps idle at the update's end 4 us,
+// A begun with the columns that are done, while others are still taken out, 0.5 and 3 us: each part costs one more barrier.
 constexpr uint32_t WHOLE_ROWS = 128, WHOLE_COLS = 256, WHOLE_MAX_CLUSTER = 16;
 constexpr uint32_t BOX_BYTES = OPERAND_BYTES;              // 128 rows of 64 columns
 constexpr uint32_t WHOLE_EXTRA = 1152;                     // diagonals, barrier and the like
