@@ -462,7 +462,7 @@ __global__ __launch_bounds__(THREADS) void qesgd_fp4_dequantize_kernel(const __g
         const uint32_t rows = (uint32_t)min((uint64_t)BACK_ROWS, a.rows - row0);
         const uint32_t cols = (uint32_t)min((uint64_t)BACK_COLS, a.cols - col0);   // of this tile
         const uint32_t c = lane * 8u, block = c / BLOCK;                           // col0 begins a tile of scales
-        const uint8_t *const at = scales + (col0 / (4u * BLOCK) + block / 4u) * SCALE_TILE + block % 4u + warp * 16u;
+        const uint8_t *const at = scales + (uint64_t)(col0 / (4u * BLOCK) + block / 4u) * SCALE_TILE + block % 4u + warp * 16u;
         const uint8_t *const codes = a.codes + ((row0 + warp) * padded + col0 + c) / 2;
         T *out = static_cast<T *>(a.out) + (row0 + warp) * a.ldo + col0;
         uint32_t w[UNROLL], byte[UNROLL];
