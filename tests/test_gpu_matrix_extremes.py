@@ -12,6 +12,7 @@ if not torch.cuda.is_available():
 from oracle import matrix_ref as ref                        # noqa: E402
 from paper_1901_03040_b200 import qesgd                     # noqa: E402
 from tests import gpu_helpers as G                          # noqa: E402
+from tests.test_gpu_matrix_accuracy import WIDE_TOLERANCE  # noqa: E402
 
 DTYPE = {qesgd.F32: torch.float32, qesgd.BF16: torch.bfloat16, qesgd.F16: torch.float16}
 FORMATS = [qesgd.FP4_MX, qesgd.FP4_NV]
@@ -116,3 +117,37 @@ def test_the_exponent_leaves_non_finite_elements_out(dtype, rows, cols, pad):
     x[rows // 2, cols // 3] = torch.finfo(DTYPE[dtype]).max
     ctx.qesgd_fp4_tensor_exponent(x.cuda(), dtype, rows, cols, cols + pad, e[1:])
     assert int(e[1]) == ref.tensor_exponent(x[:, :cols].double().numpy()) and ctx.qesgd_status() == 0
+
+
+@pytest.mark.parametrize("dtype", list(DTYPE))
+@pytest.mark.parametrize("rows,cols", [(40, 72), (100, 1000), (150, 300), (300, 150), (600, 530)])
+def test_orthogonalize_of_zeros_non_finite_and_far_scales(rows, cols, dtype):
+    """In the one-kernel form, alone and by clusters, and as products of their own: a matrix of a batch that is not finite, or
+    zero, gives zeros and leaves the others alone; elements near the type's ends are divided by their norm as any; what lies behind a
+    row's end is not looked at."""
+    pad, batch = 3, 7
+    info = torch.finfo(DTYPE[dtype])
+    x = _matrix(batch * rows, cols + pad, dtype, 3).view(batch, rows, cols + pad)
+    x[0] = 0.0
+    x[1, rows - 1, cols - 1] = float("nan")
+    x[2, 0, cols // 2] = float("-inf")
+    x[3] = (x[3].double().clamp(-1, 1) * info.max).to(DTYPE[dtype])
+    x[4] = (x[4].double() * info.tiny * 4).to(DTYPE[dtype])                 # subnormal for the most part
+    x[5] = 0.0
+    x[5, rows // 2, cols // 3] = info.smallest_normal * info.eps            # the smallest number there is
+    x[:, :, cols:] = float("nan")
+    dev = x.cuda()
+    out = torch.full((batch, rows, cols + 1), 9.0, dtype=torch.bfloat16, device="cuda")
+    need = qesgd.orthogonalize_workspace(rows, cols, batch)
+    work = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    ctx = G.ctx()
+    ctx.qesgd_orthogonalize(dev, dtype, rows, cols, cols + pad, batch, x.stride(0), 5, out, cols + 1, rows * (cols + 1), work, need)
+    assert ctx.qesgd_status() == qesgd.STATUS_NONFINITE
+    assert (out[:, :, cols:] == 9.0).all() and (out[:3, :, :cols] == 0).all()
+    for i in (3, 4, 5, 6):
+        want = ref.orthogonalize(x[i, :, :cols].double().numpy())
+        off = np.linalg.norm(out[i, :, :cols].double().cpu().numpy() - want) / np.linalg.norm(want)
+        assert off <= WIDE_TOLERANCE, (i, off)
+    x[1:3] = 0.0
+    ctx.qesgd_orthogonalize(x.cuda(), dtype, rows, cols, cols + pad, batch, x.stride(0), 5, out, cols + 1, rows * (cols + 1), work, need)
+    assert ctx.qesgd_status() == 0
