@@ -423,8 +423,9 @@ int qesgd_fp4_matmul(qesgd_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_sc
  * dtype); out: the same in BF16 (ldo, out_stride), which may be x itself where the layouts agree.
  * The products take fp16 operands (scaled by powers of two) and accumulate in fp32; X is carried in 22 bits or more from step
  * to step.  Five usual steps end at most 2.7e-3 of the result from the exact one, whatever its spectrum (tested from equal
- * singular values to one 10^5 times the rest), of which 1.7e-3 is the final rounding to BF16; 6e-3 with fewer than 16 rows or
- * columns, where single elements' roundings count.  a, b, c finite, |a| <= 16, |b|, |c| <= 32.  What is kept in
+ * singular values to one 10^5 times the rest), of which 1.7e-3 is the final rounding to BF16; 8e-3 with fewer than 64 rows or
+ * columns, where errors average less (the steps themselves enlarge a relative error that equal singular values
+ * share up to 18 times).  a, b, c finite, |a| <= 16, |b|, |c| <= 32.  What is kept in
  * fp16 is cut off at its largest number: elements of X at 255.8 (between steps), of A and of B off their diagonals at 15.9 and
  * 63.9, none of which the usual a, b, c come near.  A matrix of zeros gives zeros; one with a
  * non-finite element gives zeros and QESGD_STATUS_NONFINITE, the others of the batch are not

@@ -158,3 +158,47 @@ def test_nearly_orthogonal_rows(rows, cols):
         errors = np.sqrt(5.0) * STEP * (share + 2.0 / max(rows, cols) ** 0.5)
         off = _off(_orthogonalize(x), want)[0]
         assert off <= np.hypot(rounding, errors), (seed, off, rounding, errors)
+
+
+def _shared_errors(m, n, r):
+    """What fp16 operands leave of five steps on an m x n matrix, m <= n, with r equal singular values s and nothing else, as a share
+    of the result, before its rounding: X = s U V^T, q = p(s) / s, all errors independent with mean square (rho x value)^2.
+      A = X X^T of rounded X: U^T dA U has r^2 entries of 2 (rho s^2)^2 r / (m n): 2 rho^2 r^2 / (m n) of |A|^2.
+      A's rounding off the diagonal: r^2 / m^2 rho^2 of |A|^2 between the U, rho^2 elsewhere.  B's: the same of |B|^2.
+    An error of A enters X' by (b + 2 c s^2) s^2 / q, one of B by (b s^2 + c s^4) / q.  Between the U, later steps enlarge it by
+    g = s p'(s) / p(s) each; elsewhere it turns U, which p leaves as it is (by 1)."""
+    a, b, c, rho, s, steps = 3.4445, -4.7750, 2.0315, 0.425 * 2.0 ** -11, r ** -0.5, []
+    for _ in range(5):
+        q = a + b * s ** 2 + c * s ** 4
+        steps.append(((b + 2 * c * s ** 2) * s ** 2 / q, (b * s ** 2 + c * s ** 4) / q, (a + 3 * b * s ** 2 + 5 * c * s ** 4) / q))
+        s *= q
+    square = 0.0
+    for i, (by_a, by_b, _) in enumerate(steps):
+        g2 = float(np.prod([g for _, _, g in steps[i + 1:]])) ** 2
+        square += (by_a * rho) ** 2 * (g2 * (2 * r * r / (m * n) + r * r / (m * m)) + 1) + (by_b * rho) ** 2 * (g2 * r * r / (m * m) + 1)
+    return square ** 0.5
+
+
+@pytest.mark.parametrize("rows,cols", [(4, 4), (8, 8), (16, 16), (16, 64), (24, 30), (32, 32), (40, 40), (300, 64), (100, 300), (128, 128), (200, 200), (300, 520), (640, 640)])
+def test_equal_strong_singular_values(rows, cols):
+    """r equal singular values, the rest 10^-3 of them.  What the r share is enlarged by the steps that follow, s p'(s) / p(s)
+    each, up to 18 times in all, which WIDE_TOLERANCE leaves out; _shared_errors has it."""
+    k = min(rows, cols)
+    xs, bounds = [], []
+    for i, strong in enumerate(sorted({k // 8, k // 4, k // 2, k - k // 8, k} - {0})):
+        g = torch.Generator(device="cuda").manual_seed(i)
+        u = torch.linalg.qr(torch.randn((rows, k), generator=g, device="cuda", dtype=torch.float64))[0]
+        v = torch.linalg.qr(torch.randn((cols, k), generator=g, device="cuda", dtype=torch.float64))[0]
+        s = torch.full((k,), 1e-3, device="cuda", dtype=torch.float64)
+        s[:strong] = 1.0
+        xs.append(((u * s) @ v.T).float())
+        want = _exact(xs[-1][None])
+        # r^2 errors make up the shared ones: their mean square is off by sqrt(2 / r^2) of itself, three times that at most
+        bounds.append(np.hypot(_off(want.to(torch.bfloat16), want)[0], (1.0 + 2.1 / strong) * _shared_errors(k, max(rows, cols), strong)))
+    x = torch.stack(xs)
+    off = _off(_orthogonalize(x), _exact(x))
+    if k < 512:
+        assert (np.array(off) <= np.array(bounds)).all(), (off, bounds)
+    if k >= 64:
+        assert max(off) <= WIDE_TOLERANCE, off
+    assert G.ctx().qesgd_status() == 0
